@@ -472,6 +472,221 @@ int helios_batch_ticks(helios_ctx *ctx, helios_role_ticks *out, int32_t cap, int
 int helios_gather_times(helios_ctx *ctx, float *hbm_ms, float *host_ms,
                         float *hbm_event_ms, float *host_event_ms);
 
+/* ------------------------------------------------------------------------
+ * Operators of a model's layer on the rows of a prepared mini-batch
+ * (`out` of helios_prepare_batch, blocks of helios_make_blocks): the mean over
+ * a block's sampled neighbours, a matrix product with bias, activation and
+ * residual, a root-mean-square norm, their gradients, and product and norm in
+ * 8 bits for serving.  They need neither a graph nor a cache.
+ *
+ *  - A matrix is a device pointer to its first element and the distance `ld`
+ *    from one row to the next in elements; a row's elements are neighbours.
+ *    Any ld of at least the width will do, and for what is only read 0, which
+ *    repeats one row.  Pointers are aligned to their element, nothing more;
+ *    rows of 16-byte multiples at 16-byte addresses are read quickest.
+ *  - Sums, statistics and the steps between them are held in 32 bits, and
+ *    results rounded once (to nearest, ties to even) to their type, except
+ *    where an argument below says otherwise.
+ *  - n_rows bounds the rows; if n_rows_dev (device-accessible int64, e.g. a
+ *    batch's sizes) is not NULL the count is read from it on the device, at
+ *    most n_rows; rows behind it are neither read nor written.
+ *  - What is written must not share memory with anything else that the call
+ *    reads or writes, but where an argument says that it may be the very same
+ *    matrix (pointer, ld and type).  Two matrices may lie in one wider array
+ *    side by side (same ld in bytes).
+ *  - Results do not depend on the launch: the same call gives the same bits.
+ *  - Scratch is allocated by the first call that needs as much and kept until
+ *    the context is destroyed (also what a larger call has outgrown), so a HIP
+ *    graph stays valid.  In a capture nothing is allocated: a call that would
+ *    have to is HELIOS_ESTATE; make it once outside before. */
+typedef enum {
+    HELIOS_F32 = 0,
+    HELIOS_F16 = 1,
+    HELIOS_BF16 = 2,
+    HELIOS_E4M3 = 3     /* 8 bits: 4 of exponent, 3 of mantissa, no infinities, largest 448 */
+} helios_dtype;
+typedef enum {
+    HELIOS_ACT_NONE = 0,
+    HELIOS_ACT_RELU = 1,
+    HELIOS_ACT_GELU = 2, /* z * Phi(z), with the error function */
+    HELIOS_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} helios_act;
+
+/* z = x w^T + bias, y = act(z) + residual.  x [n_rows x n_in] and w [n_out x
+ * n_in] are of x_type; bias [n_out], residual, pre and y [n_rows x n_out] of
+ * out_type, which is x_type or HELIOS_F32 (for HELIOS_E4M3: any of the other
+ * three).  With HELIOS_E4M3, x and w stand for their values times x_scale
+ * [n_rows] and w_scale [n_out] (float; else both NULL), z = x w^T x_scale
+ * w_scale + bias.  bias, residual and pre are nullable; pre receives z, which
+ * helios_linear_grad needs if there is an activation.  y may be residual's
+ * matrix. */
+typedef struct {
+    int64_t n_rows;
+    const int64_t *n_rows_dev;
+    int64_t n_in, n_out;
+    int32_t act, x_type, out_type, reserved;
+    const void *x;
+    int64_t x_ld;
+    const float *x_scale;
+    const void *w;
+    int64_t w_ld;
+    const float *w_scale;
+    const void *bias;
+    const void *residual;
+    int64_t residual_ld;
+    void *pre;
+    int64_t pre_ld;
+    void *y;
+    int64_t y_ld;
+} helios_linear_args;
+int helios_linear(helios_ctx *ctx, const helios_linear_args *args);
+
+/* Gradients of helios_linear: dz = dy * act'(pre), dx = dz w, dw = dz^T x,
+ * dbias = the sum of dz's rows.  x, w and dx, dw are of x_type (not
+ * HELIOS_E4M3), dy, pre and dbias of out_type.  pre is needed only with an
+ * activation (relu's slope at 0 is 0); dx, dw and dbias are nullable.  The residual's gradient is
+ * dy itself.  For the two products dz is rounded to x_type (it is what the
+ * matrix instructions take; dbias is summed from the unrounded values). */
+typedef struct {
+    int64_t n_rows;
+    const int64_t *n_rows_dev;
+    int64_t n_in, n_out;
+    int32_t act, x_type, out_type, reserved;
+    const void *x;
+    int64_t x_ld;
+    const void *w;
+    int64_t w_ld;
+    const void *dy;
+    int64_t dy_ld;
+    const void *pre;
+    int64_t pre_ld;
+    void *dx;
+    int64_t dx_ld;
+    void *dw;
+    int64_t dw_ld;
+    void *dbias;
+} helios_linear_grad_args;
+int helios_linear_grad(helios_ctx *ctx, const helios_linear_grad_args *args);
+
+/* total = x + residual, y = total * gain / sqrt(mean(total^2) + eps), row by
+ * row (rows of 1 to HELIOS_NORM_MAX_WIDTH elements).  x, residual, gain [width]
+ * and total are of x_type.  y is of y_type = x_type, or HELIOS_E4M3: then
+ * y_scale [n_rows] (float) receives s = max(max|y| / 448, 2^-126) and y the
+ * values y / s.  residual, gain (ones), total and inv_rms (float [n_rows]: 1 /
+ * sqrt(mean + eps), for helios_rms_norm_grad) are nullable.  y is made from the
+ * unrounded total.  total and y (if of x_type) may each be the matrix of x or
+ * of residual, but not both the same. */
+#define HELIOS_NORM_MAX_WIDTH 32768
+typedef struct {
+    int64_t n_rows;
+    const int64_t *n_rows_dev;
+    int64_t width;
+    int32_t x_type, y_type;
+    float eps;
+    int32_t reserved;
+    const void *x;
+    int64_t x_ld;
+    const void *residual;
+    int64_t residual_ld;
+    const void *gain;
+    void *total;
+    int64_t total_ld;
+    void *y;
+    int64_t y_ld;
+    float *y_scale;
+    float *inv_rms;
+} helios_rms_norm_args;
+int helios_rms_norm(helios_ctx *ctx, const helios_rms_norm_args *args);
+
+/* Gradients of helios_rms_norm: with q = 1 / sqrt(mean(total^2) + eps) and u =
+ * dy * gain, dx = dtotal + q (u - total q^2 mean(u total)), which is also the
+ * residual's gradient, and dgain = the sum over the rows of dy total q.  All of
+ * x_type; dtotal (the gradient that reaches total by other ways), gain, dgain
+ * and inv_rms (q as helios_rms_norm left it; else it is computed) are nullable.
+ * dx may be the matrix of dy, total or dtotal. */
+typedef struct {
+    int64_t n_rows;
+    const int64_t *n_rows_dev;
+    int64_t width;
+    int32_t x_type;
+    float eps;
+    const void *total;
+    int64_t total_ld;
+    const void *gain;
+    const float *inv_rms;
+    const void *dy;
+    int64_t dy_ld;
+    const void *dtotal;
+    int64_t dtotal_ld;
+    void *dx;
+    int64_t dx_ld;
+    void *dgain;
+} helios_rms_norm_grad_args;
+int helios_rms_norm_grad(helios_ctx *ctx, const helios_rms_norm_grad_args *args);
+
+/* Rows in 8 bits, as helios_linear takes them (weights laid out once, or
+ * inputs): q_scale[i] = max(max|x_i| / 448, 2^-126), q_i = e4m3(x_i /
+ * q_scale[i]).  x is of x_type (16 or 32 bits), rows as in helios_rms_norm. */
+int helios_quantize_rows(helios_ctx *ctx, int64_t n_rows, const int64_t *n_rows_dev, int64_t width, int32_t x_type,
+                         const void *x, int64_t x_ld, void *q, int64_t q_ld, float *q_scale);
+
+/* Mean over the sampled neighbours of a block's rows: mean[i] = the mean of
+ * x[col[e]] over e in [indptr[i], indptr[i+1]), zeros for a row without samples,
+ * and own[i] = x[row[i]] (own nullable; row NULL: row i's own source is i).  x
+ * [n_src x width], mean and own [n_rows x width] are of x_type (16 or 32
+ * bits); indptr int64[n_rows + 1], col int32[n_col], row int32[n_rows].  For a
+ * hop of a prepared batch: indptr of the hop, col_local, row_local, x = out.
+ * mean and own may be halves of one array, the next product's input.  A list
+ * outside col or an index outside x counts as zeros and is reported as
+ * HELIOS_EDATA by the next helios_sync. */
+typedef struct {
+    int64_t n_rows;
+    const int64_t *n_rows_dev;
+    int64_t width, n_src, n_col;
+    int32_t x_type, reserved;
+    const void *x;
+    int64_t x_ld;
+    const int64_t *indptr;
+    const int32_t *col;
+    const int32_t *row;
+    void *mean;
+    int64_t mean_ld;
+    void *own;
+    int64_t own_ld;
+} helios_block_mean_args;
+int helios_block_mean(helios_ctx *ctx, const helios_block_mean_args *args);
+
+/* A block's entries by source, for helios_block_mean_grad: those of source u
+ * are src_entry[src_indptr[u] .. src_indptr[u+1]), a row i where a sample of
+ * row i is u (in the order of col), then ~i where row[i] is u (row NULL: no
+ * such entries).  src_indptr int32[n_src + 1]; src_entry int32 with room for
+ * n_col entries, and n_rows more if row is given (fewer than 2^31 in all). */
+int helios_block_transpose(helios_ctx *ctx, int64_t n_rows, const int64_t *n_rows_dev, const int64_t *indptr,
+                           const int32_t *col, int64_t n_col, const int32_t *row, int64_t n_src,
+                           int32_t *src_indptr, int32_t *src_entry);
+
+/* Gradient of helios_block_mean: dx[u] = the sum over the samples equal to u
+ * of dmean[i] / (samples of row i), plus that of down[i] over the rows whose own
+ * source is u; zeros where there are none.  indptr as in helios_block_mean,
+ * src_indptr and src_entry (n_entries: its room) from helios_block_transpose;
+ * down is needed if that was given `row`.  dmean, down and dx [n_src x width]
+ * are of x_type.  Entries that fit no row are left out and reported as
+ * HELIOS_EDATA. */
+typedef struct {
+    int64_t n_rows, width, n_src, n_entries;
+    int32_t x_type, reserved;
+    const int64_t *indptr;
+    const int32_t *src_indptr;
+    const int32_t *src_entry;
+    const void *dmean;
+    int64_t dmean_ld;
+    const void *down;
+    int64_t down_ld;
+    void *dx;
+    int64_t dx_ld;
+} helios_block_mean_grad_args;
+int helios_block_mean_grad(helios_ctx *ctx, const helios_block_mean_grad_args *args);
+
 #ifdef __cplusplus
 }
 #endif

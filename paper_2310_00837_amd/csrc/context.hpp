@@ -144,6 +144,13 @@ struct helios_ctx {
     size_t hot_temp_bytes = 0;
     uint32_t* map_cursors = nullptr;           // device [kMapCursors], behind the scan tickets: zero between calls
     bool map_cursors_used = false;             // a build of the map has failed half way
+
+    // scratch of the operators of a layer: what a larger call has outgrown stays, since a HIP graph may hold it (every
+    // growth at least doubles it, so there are few)
+    void* layer_scratch = nullptr;
+    size_t layer_scratch_bytes = 0;
+    void* layer_outgrown[64] = {nullptr};
+    int n_layer_outgrown = 0;
 };
 
 namespace helios {

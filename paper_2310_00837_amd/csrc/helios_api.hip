@@ -947,6 +947,8 @@ int helios_destroy(helios_ctx* c) {
     (void)hipFree(c->scan_ticket);
     (void)hipFree(c->batches_run);
     (void)hipFree(c->hot_temp);
+    (void)hipFree(c->layer_scratch);
+    for (int k = 0; k < c->n_layer_outgrown; ++k) (void)hipFree(c->layer_outgrown[k]);
     if (c->vars_ring) (void)hipHostFree(c->vars_ring);
     (void)hipFree(c->clock);
     if (c->clock_host) (void)hipHostFree(c->clock_host);

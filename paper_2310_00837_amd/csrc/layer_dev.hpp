@@ -1,0 +1,176 @@
+// Device-side helpers of the operators of a model's layer: element types, rows of any alignment, activations.
+#pragma once
+#include "common.hpp"
+
+namespace helios {
+
+// element types, same values as helios_dtype
+constexpr int kF32 = 0, kF16 = 1, kBF16 = 2, kE4M3 = 3;
+// activations, same values as helios_act
+constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3;
+
+__host__ __device__ constexpr int type_bytes(int type) { return type == kF32 ? 4 : type == kE4M3 ? 1 : 2; }
+
+struct E4M3 {                                             // storage of an 8-bit float (4 exponent bits, 3 of mantissa, no infinities)
+    uint8_t bits;
+};
+template <int TYPE> struct ElementOf;
+template <> struct ElementOf<kF32> { typedef float type; };
+template <> struct ElementOf<kF16> { typedef _Float16 type; };
+template <> struct ElementOf<kBF16> { typedef __bf16 type; };
+template <> struct ElementOf<kE4M3> { typedef E4M3 type; };
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// 16 bytes at any address: rows may start anywhere an element may (the loads are the same, an unaligned one takes
+// the memory pipe a little longer).
+typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+__device__ __forceinline__ i32x4 load_16(const void* p) { return *static_cast<const i32x4_any*>(p); }
+__device__ __forceinline__ void store_16(void* p, i32x4 v) { *static_cast<i32x4_any*>(p) = v; }
+
+// 16 bytes of a row of which `valid` elements of BYTES bytes exist; zeros in the place of the others
+template <int BYTES>
+__device__ __forceinline__ i32x4 load_16_of(const void* p, int64_t valid) {
+    constexpr int N = 16 / BYTES;
+    if (valid >= N) return load_16(p);
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < N - 1; ++e) {
+        if (e >= valid) break;
+        if (BYTES == 4) w[e] = static_cast<const uint32_t*>(p)[e];
+        else if (BYTES == 2) w[e / 2] |= static_cast<uint32_t>(static_cast<const uint16_t*>(p)[e]) << (16 * (e & 1));
+        else w[e / 4] |= static_cast<uint32_t>(static_cast<const uint8_t*>(p)[e]) << (8 * (e & 3));
+    }
+    return i32x4{static_cast<int32_t>(w[0]), static_cast<int32_t>(w[1]), static_cast<int32_t>(w[2]), static_cast<int32_t>(w[3])};
+}
+
+// Eight neighbouring elements, widened to 32 bits (TYPE: one of the floating types of 16 or 32 bits).
+template <int TYPE>
+__device__ __forceinline__ void load_8(const void* base, int64_t at, float (&v)[8]) {
+    if constexpr (TYPE == kF32) {
+        const float* p = static_cast<const float*>(base) + at;
+        const f32x4 a = __builtin_bit_cast(f32x4, load_16(p)), b = __builtin_bit_cast(f32x4, load_16(p + 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+    } else if constexpr (TYPE == kF16) {
+        const f16x8 a = __builtin_bit_cast(f16x8, load_16(static_cast<const _Float16*>(base) + at));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(a[e]);
+    } else {
+        const i32x4 a = load_16(static_cast<const uint16_t*>(base) + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __builtin_bit_cast(float, a[e] << 16);
+            v[2 * e + 1] = __builtin_bit_cast(float, a[e] & static_cast<int32_t>(0xffff0000));
+        }
+    }
+}
+template <int TYPE>
+__device__ __forceinline__ float load_1(const void* base, int64_t at) {
+    typedef typename ElementOf<TYPE>::type T;
+    return static_cast<float>(static_cast<const T*>(base)[at]);
+}
+// ... of which the first `valid` exist; 0 in the place of the others
+template <int TYPE>
+__device__ __forceinline__ void load_8_of(const void* base, int64_t at, int valid, float (&v)[8]) {
+    if (valid >= 8) {
+        load_8<TYPE>(base, at, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < valid ? load_1<TYPE>(base, at + e) : 0.0f;
+}
+// Rounding to 16 bits is to nearest, ties to even.
+template <int TYPE>
+__device__ __forceinline__ void store_8_of(void* base, int64_t at, int valid, const float (&v)[8]) {
+    typedef typename ElementOf<TYPE>::type T;
+    T* p = static_cast<T*>(base) + at;
+    if (valid >= 8) {
+        if constexpr (TYPE == kF32) {
+            store_16(p, __builtin_bit_cast(i32x4, f32x4{v[0], v[1], v[2], v[3]}));
+            store_16(p + 4, __builtin_bit_cast(i32x4, f32x4{v[4], v[5], v[6], v[7]}));
+        } else {
+            typedef T tx8 __attribute__((ext_vector_type(8)));
+            tx8 a;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] = static_cast<T>(v[e]);
+            store_16(p, __builtin_bit_cast(i32x4, a));
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < valid) p[e] = static_cast<T>(v[e]);
+}
+// the same for a type that is an argument of the kernel (the branches are the same for all lanes)
+__device__ __forceinline__ void load_8_of(int type, const void* base, int64_t at, int valid, float (&v)[8]) {
+    if (type == kF32) load_8_of<kF32>(base, at, valid, v);
+    else if (type == kF16) load_8_of<kF16>(base, at, valid, v);
+    else load_8_of<kBF16>(base, at, valid, v);
+}
+__device__ __forceinline__ void store_8_of(int type, void* base, int64_t at, int valid, const float (&v)[8]) {
+    if (type == kF32) store_8_of<kF32>(base, at, valid, v);
+    else if (type == kF16) store_8_of<kF16>(base, at, valid, v);
+    else store_8_of<kBF16>(base, at, valid, v);
+}
+__device__ __forceinline__ void store_1(int type, void* base, int64_t at, float v) {
+    if (type == kF32) static_cast<float*>(base)[at] = v;
+    else if (type == kF16) static_cast<_Float16*>(base)[at] = static_cast<_Float16>(v);
+    else static_cast<__bf16*>(base)[at] = static_cast<__bf16>(v);
+}
+
+__device__ __forceinline__ float act_of(int act, float z) {
+    if (act == kActRelu) return z < 0.0f ? 0.0f : z;                                   // NaN stays NaN
+    if (act == kActGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    if (act == kActSilu) return z / (1.0f + __expf(-z));
+    return z;
+}
+__device__ __forceinline__ float act_slope(int act, float z) {
+    if (act == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
+    if (act == kActGelu) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
+    if (act == kActSilu) {
+        const float p = 1.0f / (1.0f + __expf(-z));
+        return p * (1.0f + z * (1.0f - p));
+    }
+    return 1.0f;
+}
+
+// Sum over the lanes of a group of G (a power of two, up to a wave), the same value in all of them.
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int d = G / 2; d >= 1; d >>= 1) v += __shfl_xor(v, d, kWave);
+    return v;
+}
+template <int G>
+__device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+    for (int d = G / 2; d >= 1; d >>= 1) {
+        const float o = __shfl_xor(v, d, kWave);
+        v = o > v || o != o ? o : v;                                                   // NaN stays
+    }
+    return v;
+}
+
+// out[c] = the sum over p of part[p][c], p < n_parts, for the 16 columns from `first` on, by a workgroup of kBlock threads: 16 of
+// them share a column, each with every 16th part, and the sixteen sums are added in order.
+constexpr int kSumColumns = 16;
+__device__ __forceinline__ void sum_columns(const float* part, int n_parts, int32_t n, int32_t first, void* out, int type) {
+    __shared__ float s[kBlock / kSumColumns][kSumColumns + 1];
+    const int c = threadIdx.x % kSumColumns, sub = threadIdx.x / kSumColumns;
+    float t = 0;
+    if (first + c < n)
+        for (int p = sub; p < n_parts; p += kBlock / kSumColumns) t += part[static_cast<int64_t>(p) * n + first + c];
+    s[sub][c] = t;
+    __syncthreads();
+    if (sub == 0 && first + c < n) {
+#pragma unroll
+        for (int k = 1; k < kBlock / kSumColumns; ++k) t += s[k][c];
+        store_1(type, out, first + c, t);
+    }
+}
+
+}  // namespace helios

@@ -1,0 +1,550 @@
+// Matrix products of a layer: y = act(x w^T + bias) + residual, and their gradients.
+//
+// All three products are D[M][N] = sum over k of A[m][k] B[n][k], in tiles that a workgroup stages through LDS:
+//   forward   A = x  (rows of k),           B = w (rows of k)
+//   dx        A = dz (rows of k = n_out),   B = w (k-strided: [k][n])
+//   dw        A = dz (k-strided, k = rows), B = x (k-strided)
+// A stage of an operand is 128 bytes of k for every row (64 elements of 16 bits, 32 of 32 bits, 128 of 8 bits), or
+// as many k-strided rows.  Chunks of 16 bytes lie in LDS where a swizzle puts them, so that the 16 lanes that read a
+// column of a tile hit different banks; k-strided tiles of 16-bit elements are transposed by the read (ds_read_b64_tr_b16).
+// Sums are held in 32 bits (MFMA accumulators); the epilogue works on 32-bit sums and rounds once.
+#include "layer.hpp"
+#include "layer_dev.hpp"
+
+#include <algorithm>
+
+namespace helios {
+
+namespace {
+
+constexpr uint32_t kMostBlocks = 1u << 22;        // of a launch
+constexpr int kStageBytes = 128;                  // of k, per row of a tile
+
+// What one 16-byte chunk of A and one of B contribute to a tile of 16 x 16: their elements as the matrix instructions take
+// them, and the instructions (swapped, so that a lane holds one row of A and four neighbouring columns).
+// e4m3 goes to 16 bits first, which is exact: the matrix instructions for 8 bits lose the sum's lower bits (measured: off by
+// up to 2^-13 of the sum of the products' magnitudes, 2^-22 by way of 16 bits).
+template <int TYPE> struct Mma;
+template <> struct Mma<kF16> {
+    typedef f16x8 Part;
+    static __device__ __forceinline__ Part part(i32x4 v) { return __builtin_bit_cast(f16x8, v); }
+    static __device__ __forceinline__ f32x4 run(const Part& a, const Part& b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(b, a, c, 0, 0, 0); }
+};
+template <> struct Mma<kBF16> {
+    typedef bf16x8 Part;
+    static __device__ __forceinline__ Part part(i32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+    static __device__ __forceinline__ f32x4 run(const Part& a, const Part& b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, c, 0, 0, 0); }
+};
+template <> struct Mma<kF32> {
+    typedef f32x4 Part;
+    static __device__ __forceinline__ Part part(i32x4 v) { return __builtin_bit_cast(f32x4, v); }
+    static __device__ __forceinline__ f32x4 run(const Part& a, const Part& b, f32x4 c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j], a[j], c, 0, 0, 0);
+        return c;
+    }
+};
+template <> struct Mma<kE4M3> {
+    struct Part {
+        f16x8 half[2];
+    };
+    static __device__ __forceinline__ Part part(i32x4 v) {
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        Part p;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const f16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[k], 1.0f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[k], 1.0f, true);
+            const int at = k % 2 * 4;
+            p.half[k / 2][at] = lo.x, p.half[k / 2][at + 1] = lo.y, p.half[k / 2][at + 2] = hi.x, p.half[k / 2][at + 3] = hi.y;
+        }
+        return p;
+    }
+    static __device__ __forceinline__ f32x4 run(const Part& a, const Part& b, f32x4 c) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(b.half[k], a.half[k], c, 0, 0, 0);
+        return c;
+    }
+};
+
+struct Operand {
+    const char* data;
+    int64_t ld;                                   // bytes from one row to the next
+    int64_t rows, cols;                           // of the array in memory, in elements; what lies outside counts as zeros
+};
+
+// One operand's share of a stage: WIDTH rows of 128 bytes of k, or (STRIDED) the k-strided rows of WIDTH columns.
+template <int TYPE, int WIDTH, bool STRIDED, int THREADS>
+struct Stage {
+    static constexpr int kBytes = type_bytes(TYPE);
+    static constexpr int kPer = 16 / kBytes;      // elements of a chunk
+    static constexpr int kK = kStageBytes / kBytes;
+    static constexpr int kChunks = WIDTH * (kStageBytes / 16);
+    static constexpr int kLoads = kChunks / THREADS;
+    static constexpr int kRowChunks = STRIDED ? WIDTH * kBytes / 16 : kStageBytes / 16;
+    static_assert(kChunks % THREADS == 0, "every thread stages as many chunks");
+
+    static __device__ __forceinline__ uint32_t swizzle(uint32_t row) {
+        if (!STRIDED) return (row >> 1) & 7;
+        if (kBytes == 4) return ((row >> 2) & 3) << 2;
+        return ((row & 3) | (((row >> 3) & 1) << 2)) % (kRowChunks / 2) << 1;
+    }
+    // the chunks that thread t stages, from the tile whose first row (or column) is `first` and whose first k is k0
+    static __device__ __forceinline__ void load(const Operand& o, int64_t first, int64_t k0, i32x4 (&regs)[kLoads]) {
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const uint32_t q = threadIdx.x + l * THREADS, row = q / kRowChunks, chunk = (q % kRowChunks) ^ swizzle(row);
+            const int64_t r = (STRIDED ? k0 : first) + row, c = (STRIDED ? first : k0) + chunk * kPer;
+            regs[l] = i32x4{0, 0, 0, 0};
+            if (r < o.rows && c < o.cols) regs[l] = load_16_of<kBytes>(o.data + r * o.ld + c * kBytes, o.cols - c);
+        }
+    }
+    static __device__ __forceinline__ void put(char* lds, const i32x4 (&regs)[kLoads]) {
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) *reinterpret_cast<i32x4*>(lds + (threadIdx.x + l * THREADS) * 16) = regs[l];
+    }
+    // A lane's chunk of the 16 rows (or columns) from `at` on: lane r of group g holds row at + r, and of k the 16 bytes at
+    // 16 (g + 4 half).  k-strided 32-bit elements come one by one, 16-bit ones as two transposed reads.
+    static __device__ __forceinline__ i32x4 fragment(const char* lds, int at, int half) {
+        const uint32_t lane = threadIdx.x & (kWave - 1), r = lane & 15, g = lane >> 4;
+        if (!STRIDED) {
+            const uint32_t row = at + r;
+            return *reinterpret_cast<const i32x4*>(lds + row * kStageBytes + (((g + 4 * half) ^ swizzle(row)) << 4));
+        }
+        if (kBytes == 4) {
+            i32x4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t k = 16 * half + 4 * g + j;
+                v[j] = *reinterpret_cast<const int32_t*>(lds + k * (WIDTH * 4) + ((((at + r) >> 2) ^ swizzle(k)) << 4) + (r & 3) * 4);
+            }
+            return v;
+        }
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
+        i32x2 part[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t k = 32 * half + 8 * g + 4 * j + (r >> 2), column = at + 4 * (r & 3);
+            const char* p = lds + k * (WIDTH * 2) + (((column >> 3) ^ swizzle(k)) << 4) + ((column >> 2) & 1) * 8;
+            part[j] = __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)));
+        }
+        return i32x4{part[0].x, part[0].y, part[1].x, part[1].y};
+    }
+};
+
+// The epilogues: eight neighbouring sums of a row.
+struct ForwardOut {
+    const float *x_scale, *w_scale;
+    const void *bias, *residual;
+    int64_t residual_ld;
+    void* pre;
+    int64_t pre_ld;
+    void* y;
+    int64_t y_ld;
+    int act, type;
+    __device__ __forceinline__ void operator()(int64_t row, int col, int valid, float (&v)[8], int) const {
+        if (x_scale) {
+            const float s = x_scale[row];
+            float t[8];
+            load_8_of<kF32>(w_scale, col, valid, t);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= s * t[e];
+        }
+        if (bias) {
+            float b[8];
+            load_8_of(type, bias, col, valid, b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += b[e];
+        }
+        if (pre) store_8_of(type, pre, row * pre_ld + col, valid, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = act_of(act, v[e]);
+        if (residual) {
+            float r[8];
+            load_8_of(type, residual, row * residual_ld + col, valid, r);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += r[e];
+        }
+        store_8_of(type, y, row * y_ld + col, valid, v);
+    }
+};
+struct PlainOut {                                 // (slice: which part of k the sums are of)
+    void* y;
+    int64_t ld, slice_stride;
+    int type;
+    __device__ __forceinline__ void operator()(int64_t row, int col, int valid, float (&v)[8], int slice) const {
+        store_8_of(type, y, slice * slice_stride + row * ld + col, valid, v);
+    }
+};
+
+template <class OUT>
+struct ProductArgs {
+    Operand a, b;
+    int64_t m, k;                                 // the most; `rows` limits m, or k where that runs over rows
+    int32_t n;
+    Count rows;
+    uint32_t tiles_n, tiles;
+    int slices;                                   // parts that k is cut into, each with sums of its own
+    OUT out;
+};
+
+// Tile of a workgroup.  Workgroups go round the eight XCDs, each of which has an L2 of its own: the tiles that share rows of A are
+// neighbours on one XCD.
+__device__ __forceinline__ void tile_of(uint32_t block, uint32_t tiles_n, uint32_t* tile_m, uint32_t* tile_n) {
+    const uint32_t xcd = block % 8, at = block / 8;
+    *tile_m = at / tiles_n * 8 + xcd;
+    *tile_n = at % tiles_n;
+}
+
+template <int TYPE, int BM, int BN, int WAVES_M, int WAVES_N, bool A_STRIDED, bool B_STRIDED, class OUT>
+__global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void product_kernel(ProductArgs<OUT> p) {
+    constexpr int kThreads = WAVES_M * WAVES_N * kWave;
+    constexpr int kTm = BM / WAVES_M / 16, kTn = BN / WAVES_N / 16;      // 16 x 16 tiles of a wave
+    typedef Stage<TYPE, BM, A_STRIDED, kThreads> StageA;
+    typedef Stage<TYPE, BN, B_STRIDED, kThreads> StageB;
+    constexpr int kStage = (BM + BN) * kStageBytes;
+    constexpr int kOutLd = BN + 4;
+    constexpr int kLds = 2 * kStage > BM * kOutLd * 4 ? 2 * kStage : BM * kOutLd * 4;
+    __shared__ __align__(16) char lds[kLds];
+
+    const int64_t count = p.rows.get();
+    const bool rows_are_k = A_STRIDED;
+    const int64_t m_end = rows_are_k ? p.m : count, k_end = rows_are_k ? count : p.k;
+    if (rows_are_k) p.a.rows = p.b.rows = count;
+    else p.a.rows = count;
+    const int slice = blockIdx.y;
+    const int64_t steps_all = (k_end + StageA::kK - 1) / StageA::kK, per = (steps_all + p.slices - 1) / p.slices;
+    const int64_t step0 = slice * per, step1 = step0 + per < steps_all ? step0 + per : steps_all;
+
+    const int wave = threadIdx.x / kWave, wave_m = wave / WAVES_N, wave_n = wave % WAVES_N;
+    for (uint32_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {      // (once round, but for the longest lists)
+        uint32_t tile_m, tile_n;
+        tile_of(tile, p.tiles_n, &tile_m, &tile_n);
+        const int64_t m0 = static_cast<int64_t>(tile_m) * BM;
+        const int32_t n0 = static_cast<int32_t>(tile_n) * BN;
+        if (m0 >= m_end) continue;
+        f32x4 acc[kTm][kTn];
+    #pragma unroll
+        for (int i = 0; i < kTm; ++i)
+    #pragma unroll
+            for (int j = 0; j < kTn; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+
+        i32x4 ra[StageA::kLoads], rb[StageB::kLoads];
+        if (step0 < step1) {
+            StageA::load(p.a, m0, step0 * StageA::kK, ra);
+            StageB::load(p.b, n0, step0 * StageA::kK, rb);
+        }
+        for (int64_t step = step0; step < step1; ++step) {
+            char* stage = lds + (step & 1) * kStage;
+            StageA::put(stage, ra);
+            StageB::put(stage + BM * kStageBytes, rb);
+            __syncthreads();                          // (the other stage's readers are done when its writers come round again)
+            if (step + 1 < step1) {
+                StageA::load(p.a, m0, (step + 1) * StageA::kK, ra);
+                StageB::load(p.b, n0, (step + 1) * StageA::kK, rb);
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                typename Mma<TYPE>::Part fa[kTm], fb[kTn];
+#pragma unroll
+                for (int i = 0; i < kTm; ++i) fa[i] = Mma<TYPE>::part(StageA::fragment(stage, (wave_m * kTm + i) * 16, half));
+#pragma unroll
+                for (int j = 0; j < kTn; ++j) fb[j] = Mma<TYPE>::part(StageB::fragment(stage + BM * kStageBytes, (wave_n * kTn + j) * 16, half));
+#pragma unroll
+                for (int i = 0; i < kTm; ++i)
+#pragma unroll
+                    for (int j = 0; j < kTn; ++j) acc[i][j] = Mma<TYPE>::run(fa[i], fb[j], acc[i][j]);
+            }
+        }
+        __syncthreads();
+        // The sums go through LDS, so that the epilogue reads and writes whole rows.
+        float* sums = reinterpret_cast<float*>(lds);
+        const int r = threadIdx.x & 15, g = (threadIdx.x & (kWave - 1)) >> 4;
+    #pragma unroll
+        for (int i = 0; i < kTm; ++i)
+    #pragma unroll
+            for (int j = 0; j < kTn; ++j)
+                *reinterpret_cast<f32x4*>(sums + ((wave_m * kTm + i) * 16 + r) * kOutLd + (wave_n * kTn + j) * 16 + 4 * g) = acc[i][j];
+        __syncthreads();
+        for (int u = threadIdx.x; u < BM * BN / 8; u += kThreads) {
+            const int row = u / (BN / 8), col = u % (BN / 8) * 8;
+            const int valid = p.n - n0 - col;
+            if (m0 + row >= m_end || valid <= 0) continue;
+            float v[8];
+    #pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = sums[row * kOutLd + col + e];
+            p.out(m0 + row, n0 + col, valid < 8 ? valid : 8, v, slice);
+        }
+        __syncthreads();
+    }
+}
+
+// Few rows: a workgroup has 16 rows of x and 16 of w, its waves share k between them and read both straight into the
+// operands of the MFMA, and the eight sums of every element meet in LDS.
+constexpr int kFewWaves = 8;
+template <int TYPE, class OUT>
+__global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(ProductArgs<OUT> p) {
+    constexpr int kBytes = type_bytes(TYPE), kPer = 16 / kBytes, kK = kStageBytes / kBytes;
+    __shared__ float sums[kFewWaves][16][20];
+    const int64_t count = p.rows.get(), m0 = static_cast<int64_t>(blockIdx.y) * 16;
+    const int32_t n0 = blockIdx.x * 16;
+    if (m0 >= count) return;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1), r = lane & 15, g = lane >> 4;
+    const bool in_a = m0 + r < count, in_b = n0 + r < p.n;
+    const char* a = p.a.data + (in_a ? m0 + r : m0) * p.a.ld;
+    const char* b = p.b.data + (in_b ? n0 + r : n0) * p.b.ld;
+    f32x4 acc = {0, 0, 0, 0};
+    for (int64_t k0 = wave * kK; k0 < p.k; k0 += kFewWaves * kK) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t k = k0 + (g + 4 * h) * kPer;
+            i32x4 fa = {0, 0, 0, 0}, fb = {0, 0, 0, 0};
+            if (k < p.k) {
+                fa = load_16_of<kBytes>(a + k * kBytes, p.k - k);
+                fb = load_16_of<kBytes>(b + k * kBytes, p.k - k);
+            }
+            acc = Mma<TYPE>::run(Mma<TYPE>::part(fa), Mma<TYPE>::part(fb), acc);
+        }
+    }
+    *reinterpret_cast<f32x4*>(&sums[wave][r][4 * g]) = acc;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const int row = threadIdx.x / 2, col = threadIdx.x % 2 * 8, valid = p.n - n0 - col;
+        if (m0 + row < count && valid > 0) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = 0;
+#pragma unroll
+                for (int w = 0; w < kFewWaves; ++w) v[e] += sums[w][row][col + e];
+            }
+            p.out(m0 + row, n0 + col, valid < 8 ? valid : 8, v, 0);
+        }
+    }
+}
+
+// ---- the gradient's other steps
+
+// dz = dy * act'(pre), rounded to the type the products work in, and the sums of dz's columns (from the values before
+// they are rounded) over the rows of a workgroup.
+constexpr int kSlopeCols = 16 * 8;                // columns of a workgroup: 16 lanes, 8 each; 16 rows at a time
+struct SlopeArgs {
+    Count rows;
+    int32_t n;
+    int act, type, z_type;
+    const void* dy;
+    int64_t dy_ld;
+    const void* pre;
+    int64_t pre_ld;
+    void* dz;                                     // nullable
+    int64_t dz_ld;
+    float* sums;                                  // [gridDim.y][n], nullable
+};
+__global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
+    __shared__ float s[16][kSlopeCols + 4];
+    const int64_t count = p.rows.get(), per = (count + gridDim.y - 1) / gridDim.y;
+    const int64_t row0 = blockIdx.y * per, row1 = row0 + per < count ? row0 + per : count;
+    const int lane = threadIdx.x % 16, sub = threadIdx.x / 16, col = blockIdx.x * kSlopeCols + lane * 8;
+    const int valid = p.n - col < 8 ? p.n - col : 8;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (valid > 0)
+        for (int64_t row = row0 + sub; row < row1; row += 16) {
+            float d[8];
+            load_8_of(p.type, p.dy, row * p.dy_ld + col, valid, d);
+            if (p.act != kActNone) {
+                float z[8];
+                load_8_of(p.type, p.pre, row * p.pre_ld + col, valid, z);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] *= act_slope(p.act, z[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += d[e];
+            if (p.dz) store_8_of(p.z_type, p.dz, row * p.dz_ld + col, valid, d);
+        }
+    if (!p.sums) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[sub][lane * 8 + e] = sum[e];
+    __syncthreads();
+    if (threadIdx.x < kSlopeCols && blockIdx.x * kSlopeCols + threadIdx.x < static_cast<uint32_t>(p.n)) {
+        float t = 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) t += s[k][threadIdx.x];
+        p.sums[static_cast<int64_t>(blockIdx.y) * p.n + blockIdx.x * kSlopeCols + threadIdx.x] = t;
+    }
+}
+
+// out[r][c] = the sum over s of part[s][r][c], in the order of s; the column sums of the slope kernel ride on the launch.
+struct JoinArgs {
+    const float* part;
+    int64_t cells;                                // of a slice, dense
+    int slices;
+    int32_t cols;
+    void* out;
+    int64_t out_ld;
+    int type;
+    uint32_t cell_blocks;                         // workgroups of this sum; the others have 16 columns each
+    const float* sums;
+    int32_t n;
+    int n_sums, sum_type;
+    void* sum_out;
+};
+__global__ __launch_bounds__(kBlock) void join_kernel(JoinArgs p) {
+    if (blockIdx.x >= p.cell_blocks) {
+        sum_columns(p.sums, p.n_sums, p.n, (blockIdx.x - p.cell_blocks) * kSumColumns, p.sum_out, p.sum_type);
+        return;
+    }
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x;
+    if (c >= p.cells) return;
+    float t = 0;
+    for (int s = 0; s < p.slices; ++s) t += p.part[s * p.cells + c];
+    store_1(p.type, p.out, c / p.cols * p.out_ld + c % p.cols, t);
+}
+
+Operand operand(const void* data, int64_t ld, int type, int64_t rows, int64_t cols) {
+    return Operand{static_cast<const char*>(data), ld * type_bytes(type), rows, cols};
+}
+
+uint32_t tiles_of(int64_t n, int tile) { return static_cast<uint32_t>((n + tile - 1) / tile); }
+
+// grid of tile_of: rows of tiles in eights, one for each XCD
+template <int TYPE, int BM, int BN, int WM, int WN, bool AS, bool BS, class OUT>
+hipError_t launch_tiles(hipStream_t stream, ProductArgs<OUT> p) {
+    p.tiles_n = tiles_of(p.n, BN);
+    const int64_t tiles = (tiles_of(p.m, BM) + 7ll) / 8 * 8 * p.tiles_n;
+    if (tiles >= 1ll << 32) return hipErrorInvalidValue;
+    p.tiles = static_cast<uint32_t>(tiles);
+    const dim3 grid(std::min(p.tiles, kMostBlocks), static_cast<unsigned>(p.slices));
+    hipLaunchKernelGGL((product_kernel<TYPE, BM, BN, WM, WN, AS, BS, OUT>), grid, dim3(WM * WN * kWave), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t forward(hipStream_t stream, const LinearJob& j) {
+    ProductArgs<ForwardOut> p{};
+    p.a = operand(j.x, j.x_ld, TYPE, j.rows.host, j.n_in);
+    p.b = operand(j.w, j.w_ld, TYPE, j.n_out, j.n_in);
+    p.m = j.rows.host;
+    p.n = j.n_out;
+    p.k = j.n_in;
+    p.rows = j.rows;
+    p.slices = 1;
+    p.out = ForwardOut{j.x_scale, j.w_scale, j.bias, j.residual, j.residual_ld, j.pre, j.pre_ld, j.y, j.y_ld, j.act, j.out_type};
+    if (p.m <= 16) {
+        const dim3 grid(tiles_of(p.n, 16), tiles_of(p.m, 16));
+        hipLaunchKernelGGL((product_few_kernel<TYPE, ForwardOut>), grid, dim3(kFewWaves * kWave), 0, stream, p);
+        return hipGetLastError();
+    }
+    if (static_cast<int64_t>(tiles_of(p.m, 128)) * tiles_of(p.n, 128) >= 256) return launch_tiles<TYPE, 128, 128, 2, 2, false, false>(stream, p);
+    return launch_tiles<TYPE, 64, 64, 2, 2, false, false>(stream, p);
+}
+
+struct GradPlan {                                 // of linear_grad: what lies where in the scratch, and how far k is cut up
+    bool needs_dz;
+    int64_t dz_ld;
+    int slices;                                   // of dw's k
+    unsigned slope_blocks;                        // workgroups along the rows of the slope kernel
+    size_t dz, part, sums, bytes;
+    explicit GradPlan(const LinearGradJob& j) {
+        const auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+        const int64_t n = j.rows.host;
+        needs_dz = (j.dx || j.dw) && (j.act != kActNone || j.out_type != j.x_type);
+        dz_ld = (j.n_out + 7) / 8 * 8;
+        const int64_t tiles = static_cast<int64_t>(tiles_of(j.n_out, 64)) * tiles_of(j.n_in, 64);
+        const int64_t steps = (n * type_bytes(j.x_type) + kStageBytes - 1) / kStageBytes;
+        slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({1024 / std::max<int64_t>(tiles, 1), steps / 4, 64})));
+        slope_blocks = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, 256)));
+        dz = 0;
+        part = dz + (needs_dz ? up(static_cast<size_t>(n * dz_ld) * type_bytes(j.x_type)) : 0);
+        sums = part + (j.dw ? up(static_cast<size_t>(slices) * j.n_out * j.n_in * sizeof(float)) : 0);
+        bytes = sums + (j.dbias ? up(static_cast<size_t>(slope_blocks) * j.n_out * sizeof(float)) : 0);
+    }
+};
+
+template <int TYPE>
+hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
+    const GradPlan plan(j);
+    const void* dz = plan.needs_dz ? scratch + plan.dz : j.dy;
+    const int64_t dz_ld = plan.needs_dz ? plan.dz_ld : j.dy_ld;
+    hipError_t e = hipSuccess;
+    if (plan.needs_dz || j.dbias) {
+        SlopeArgs s{j.rows, j.n_out, j.act, j.out_type, TYPE, j.dy, j.dy_ld, j.pre, j.pre_ld, plan.needs_dz ? scratch + plan.dz : nullptr, plan.dz_ld,
+                    j.dbias ? reinterpret_cast<float*>(scratch + plan.sums) : nullptr};
+        hipLaunchKernelGGL(slope_kernel, dim3(tiles_of(j.n_out, kSlopeCols), plan.slope_blocks), dim3(kBlock), 0, stream, s);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && j.dx && j.rows.host > 0) {
+        ProductArgs<PlainOut> p{};
+        p.a = operand(dz, dz_ld, TYPE, j.rows.host, j.n_out);
+        p.b = operand(j.w, j.w_ld, TYPE, j.n_out, j.n_in);
+        p.m = j.rows.host;
+        p.n = j.n_in;
+        p.k = j.n_out;
+        p.rows = j.rows;
+        p.slices = 1;
+        p.out = PlainOut{j.dx, j.dx_ld, 0, TYPE};
+        if (static_cast<int64_t>(tiles_of(p.m, 128)) * tiles_of(p.n, 128) >= 256) e = launch_tiles<TYPE, 128, 128, 2, 2, false, true>(stream, p);
+        else e = launch_tiles<TYPE, 64, 64, 2, 2, false, true>(stream, p);
+    }
+    if (e == hipSuccess && j.dw) {
+        ProductArgs<PlainOut> p{};
+        p.a = operand(dz, dz_ld, TYPE, j.rows.host, j.n_out);
+        p.b = operand(j.x, j.x_ld, TYPE, j.rows.host, j.n_in);
+        p.m = j.n_out;
+        p.n = j.n_in;
+        p.k = j.rows.host;
+        p.rows = j.rows;
+        p.slices = plan.slices;
+        p.out = PlainOut{scratch + plan.part, j.n_in, static_cast<int64_t>(j.n_out) * j.n_in, kF32};
+        e = launch_tiles<TYPE, 64, 64, 2, 2, true, true>(stream, p);
+    }
+    if (e == hipSuccess && (j.dw || j.dbias)) {
+        JoinArgs a{};
+        if (j.dw) {
+            a.part = reinterpret_cast<const float*>(scratch + plan.part);
+            a.cells = static_cast<int64_t>(j.n_out) * j.n_in;
+        }
+        a.slices = plan.slices;
+        a.cols = j.n_in;
+        a.out = j.dw;
+        a.out_ld = j.dw_ld;
+        a.type = TYPE;
+        a.cell_blocks = tiles_of(a.cells, kBlock);
+        a.sums = reinterpret_cast<const float*>(scratch + plan.sums);
+        a.n = j.n_out;
+        a.n_sums = static_cast<int>(plan.slope_blocks);
+        a.sum_type = j.out_type;
+        a.sum_out = j.dbias;
+        const uint32_t blocks = a.cell_blocks + (j.dbias ? tiles_of(j.n_out, kSumColumns) : 0);
+        hipLaunchKernelGGL(join_kernel, dim3(blocks), dim3(kBlock), 0, stream, a);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+}  // namespace
+
+hipError_t launch_linear(hipStream_t stream, const LinearJob& j) {
+    if (j.rows.host < 1) return hipSuccess;
+    switch (j.x_type) {
+        case kF32: return forward<kF32>(stream, j);
+        case kF16: return forward<kF16>(stream, j);
+        case kBF16: return forward<kBF16>(stream, j);
+        case kE4M3: return forward<kE4M3>(stream, j);
+    }
+    return hipErrorInvalidValue;
+}
+
+size_t linear_grad_scratch_bytes(const LinearGradJob& j) { return GradPlan(j).bytes; }
+
+hipError_t launch_linear_grad(hipStream_t stream, const LinearGradJob& j, void* scratch) {
+    char* at = static_cast<char*>(scratch);
+    switch (j.x_type) {
+        case kF32: return backward<kF32>(stream, j, at);
+        case kF16: return backward<kF16>(stream, j, at);
+        case kBF16: return backward<kBF16>(stream, j, at);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace helios

@@ -20,6 +20,9 @@ LIB_PATH = os.path.join(_HERE, "csrc", "libhelios.so")
 
 OK, EINVAL, ECAPACITY, EHIP, ESTATE, EDATA, EINTERNAL = 0, -1, -2, -3, -4, -5, -6
 MAX_HOPS, MAX_FANOUT = 8, 1024
+F32, F16, BF16, E4M3 = 0, 1, 2, 3
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+NORM_MAX_WIDTH = 32768
 DEDUP_NOALLOC_MAX_IDS = 262144
 PARAM_HBM_GATHER_BLOCKS, PARAM_HOST_GATHER_BLOCKS, PARAM_SPLIT_COPIES = 1, 2, 3
 PARAM_MISSQ_TIMEOUT_US, PARAM_MISSQ_WAVES, PARAM_SERVE_MISSES = 4, 5, 6
@@ -33,7 +36,9 @@ EXPORTS = ["helios_create", "helios_destroy", "helios_last_error", "helios_reser
            "helios_hotness_add", "helios_hotness_order", "helios_plan_create", "helios_plan_launch", "helios_plan_wait", "helios_plan_make_blocks", "helios_plan_destroy",
            "helios_gang_create", "helios_gang_launch", "helios_gang_wait", "helios_gang_make_blocks", "helios_gang_destroy", "helios_set_param", "helios_set_timing",
            "helios_gather_times", "helios_batch_ticks", "helios_missq_create", "helios_missq_submit", "helios_missq_complete",
-           "helios_missq_attach", "helios_missq_faulted", "helios_missq_counters", "helios_missq_destroy"]
+           "helios_missq_attach", "helios_missq_faulted", "helios_missq_counters", "helios_missq_destroy",
+           "helios_linear", "helios_linear_grad", "helios_rms_norm", "helios_rms_norm_grad", "helios_quantize_rows", "helios_block_mean",
+           "helios_block_transpose", "helios_block_mean_grad"]
 
 
 class HopOut(C.Structure):
@@ -52,6 +57,26 @@ class BatchBuffersC(C.Structure):
 
 
 MAX_GANG = 4
+
+
+def _args_struct(name: str, fields: str):
+    """A ctypes structure from "name:type" words (p pointer, l int64, i int32, f float), in the order of the header."""
+    kinds = {"p": C.c_void_p, "l": C.c_int64, "i": C.c_int32, "f": C.c_float}
+    return type(name, (C.Structure,), {"_fields_": [(w[:-2], kinds[w[-1]]) for w in fields.split()]})
+
+
+LinearArgs = _args_struct("LinearArgs", "n_rows:l n_rows_dev:p n_in:l n_out:l act:i x_type:i out_type:i reserved:i x:p x_ld:l x_scale:p w:p w_ld:l "
+                          "w_scale:p bias:p residual:p residual_ld:l pre:p pre_ld:l y:p y_ld:l")
+LinearGradArgs = _args_struct("LinearGradArgs", "n_rows:l n_rows_dev:p n_in:l n_out:l act:i x_type:i out_type:i reserved:i x:p x_ld:l w:p w_ld:l dy:p "
+                              "dy_ld:l pre:p pre_ld:l dx:p dx_ld:l dw:p dw_ld:l dbias:p")
+RmsNormArgs = _args_struct("RmsNormArgs", "n_rows:l n_rows_dev:p width:l x_type:i y_type:i eps:f reserved:i x:p x_ld:l residual:p residual_ld:l gain:p "
+                           "total:p total_ld:l y:p y_ld:l y_scale:p inv_rms:p")
+RmsNormGradArgs = _args_struct("RmsNormGradArgs", "n_rows:l n_rows_dev:p width:l x_type:i eps:f total:p total_ld:l gain:p inv_rms:p dy:p dy_ld:l "
+                               "dtotal:p dtotal_ld:l dx:p dx_ld:l dgain:p")
+BlockMeanArgs = _args_struct("BlockMeanArgs", "n_rows:l n_rows_dev:p width:l n_src:l n_col:l x_type:i reserved:i x:p x_ld:l indptr:p col:p row:p mean:p "
+                             "mean_ld:l own:p own_ld:l")
+BlockMeanGradArgs = _args_struct("BlockMeanGradArgs", "n_rows:l width:l n_src:l n_entries:l x_type:i reserved:i indptr:p src_indptr:p src_entry:p dmean:p "
+                                 "dmean_ld:l down:p down_ld:l dx:p dx_ld:l")
 
 
 class RoleTicks(C.Structure):
@@ -120,6 +145,14 @@ def load_library() -> C.CDLL:
     lib.helios_missq_faulted.argtypes = [vp]
     lib.helios_missq_counters.argtypes = [vp, C.POINTER(i64)]
     lib.helios_missq_destroy.argtypes = [vp]
+    lib.helios_linear.argtypes = [vp, C.POINTER(LinearArgs)]
+    lib.helios_linear_grad.argtypes = [vp, C.POINTER(LinearGradArgs)]
+    lib.helios_rms_norm.argtypes = [vp, C.POINTER(RmsNormArgs)]
+    lib.helios_rms_norm_grad.argtypes = [vp, C.POINTER(RmsNormGradArgs)]
+    lib.helios_quantize_rows.argtypes = [vp, i64, vp, i64, i32, vp, i64, vp, i64, vp]
+    lib.helios_block_mean.argtypes = [vp, C.POINTER(BlockMeanArgs)]
+    lib.helios_block_transpose.argtypes = [vp, i64, vp, vp, vp, i64, vp, i64, vp, vp]
+    lib.helios_block_mean_grad.argtypes = [vp, C.POINTER(BlockMeanGradArgs)]
     return lib
 
 
@@ -154,6 +187,37 @@ def _dev_accessible(t: torch.Tensor, dtype: torch.dtype, what: str) -> torch.Ten
     if t.dtype != dtype or not t.is_contiguous() or not (t.is_cuda or _is_pinned(t)):
         raise TypeError(f"{what}: expected a contiguous {dtype} tensor on the GPU or in pinned host memory")
     return t
+
+
+_TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+
+
+def _mat(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, what: str):
+    """(pointer, row stride) of a matrix on the GPU whose rows are contiguous; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.dtype != dtype or not t.is_cuda or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise TypeError(f"{what}: expected a {dtype} tensor of {rows} x {cols} on the GPU with contiguous rows")
+    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+
+
+def _vec(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_cuda or t.numel() != n or not t.is_contiguous():
+        raise TypeError(f"{what}: expected a contiguous {dtype} tensor of {n} on the GPU")
+    return t.data_ptr()
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    code = _TYPES.get(t.dtype)
+    if code is None or t.dim() != 2:
+        raise TypeError(f"{what}: expected a matrix of float32, float16, bfloat16 or float8_e4m3fn")
+    return code
+
+
+def _count(t: Optional[torch.Tensor], what: str) -> Optional[int]:
+    return None if t is None else _dev_accessible(t, torch.int64, what).data_ptr()
 
 
 class PinnedBuffer:
@@ -620,6 +684,118 @@ class Helios:
         _dev(counts, torch.int32, "counts"), _dev(order, torch.int32, "order")
         assert counts.numel() >= self.n_nodes and order.numel() >= self.n_nodes
         self._check(_lib.helios_hotness_order(self._h, _ptr(counts), _ptr(order)))
+
+    # ---- operators of a layer on the batch's rows (see the header for what each argument means)
+    def linear(self, x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
+               residual: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, x_scale: Optional[torch.Tensor] = None,
+               w_scale: Optional[torch.Tensor] = None, n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """y = act(x w^T + bias) + residual; pre (if given) receives x w^T + bias."""
+        x_type, out_type = _type(x, "x"), _type(y, "y")
+        n, k = x.shape
+        m = w.shape[0]
+        out = y.dtype
+        a = LinearArgs(n, _count(n_rows_dev, "n_rows_dev"), k, m, act, x_type, out_type, 0, *_mat(x, n, k, x.dtype, "x"),
+                       _vec(x_scale, n, torch.float32, "x_scale"), *_mat(w, m, k, x.dtype, "w"), _vec(w_scale, m, torch.float32, "w_scale"),
+                       _vec(bias, m, out, "bias"), *_mat(residual, n, m, out, "residual"), *_mat(pre, n, m, out, "pre"), *_mat(y, n, m, out, "y"))
+        rc = _lib.helios_linear(self._h, a)
+        if rc != OK:
+            self._check(rc)
+
+    def linear_grad(self, x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, act: int = ACT_NONE, pre: Optional[torch.Tensor] = None,
+                    dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                    n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """The gradients of linear that are given room for; the residual's is dy."""
+        x_type, out_type = _type(x, "x"), _type(dy, "dy")
+        n, k = x.shape
+        m = w.shape[0]
+        out = dy.dtype
+        a = LinearGradArgs(n, _count(n_rows_dev, "n_rows_dev"), k, m, act, x_type, out_type, 0, *_mat(x, n, k, x.dtype, "x"),
+                           *_mat(w, m, k, x.dtype, "w"), *_mat(dy, n, m, out, "dy"), *_mat(pre, n, m, out, "pre"), *_mat(dx, n, k, x.dtype, "dx"),
+                           *_mat(dw, m, k, x.dtype, "dw"), _vec(dbias, m, out, "dbias"))
+        rc = _lib.helios_linear_grad(self._h, a)
+        if rc != OK:
+            self._check(rc)
+
+    def rms_norm(self, x: torch.Tensor, y: torch.Tensor, eps: float, gain: Optional[torch.Tensor] = None,
+                 residual: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None, y_scale: Optional[torch.Tensor] = None,
+                 inv_rms: Optional[torch.Tensor] = None, n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """total = x + residual, y = its root-mean-square norm times gain, in 8 bits with y_scale if y is float8_e4m3fn."""
+        x_type, y_type = _type(x, "x"), _type(y, "y")
+        n, d = x.shape
+        dt = x.dtype
+        a = RmsNormArgs(n, _count(n_rows_dev, "n_rows_dev"), d, x_type, y_type, eps, 0, *_mat(x, n, d, dt, "x"), *_mat(residual, n, d, dt, "residual"),
+                        _vec(gain, d, dt, "gain"), *_mat(total, n, d, dt, "total"), *_mat(y, n, d, y.dtype, "y"),
+                        _vec(y_scale, n, torch.float32, "y_scale"), _vec(inv_rms, n, torch.float32, "inv_rms"))
+        rc = _lib.helios_rms_norm(self._h, a)
+        if rc != OK:
+            self._check(rc)
+
+    def rms_norm_grad(self, total: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor, eps: float, gain: Optional[torch.Tensor] = None,
+                      dtotal: Optional[torch.Tensor] = None, dgain: Optional[torch.Tensor] = None, inv_rms: Optional[torch.Tensor] = None,
+                      n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """The gradients of rms_norm: dx (the residual's too) and dgain; dtotal is what reaches total by other ways."""
+        x_type = _type(total, "total")
+        n, d = total.shape
+        dt = total.dtype
+        a = RmsNormGradArgs(n, _count(n_rows_dev, "n_rows_dev"), d, x_type, eps, *_mat(total, n, d, dt, "total"), _vec(gain, d, dt, "gain"),
+                            _vec(inv_rms, n, torch.float32, "inv_rms"), *_mat(dy, n, d, dt, "dy"), *_mat(dtotal, n, d, dt, "dtotal"),
+                            *_mat(dx, n, d, dt, "dx"), _vec(dgain, d, dt, "dgain"))
+        rc = _lib.helios_rms_norm_grad(self._h, a)
+        if rc != OK:
+            self._check(rc)
+
+    def quantize_rows(self, x: torch.Tensor, q: torch.Tensor, q_scale: torch.Tensor, n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """Rows in 8 bits with a scale each, as linear takes them."""
+        n, d = x.shape
+        rc = _lib.helios_quantize_rows(self._h, n, _count(n_rows_dev, "n_rows_dev"), d, _type(x, "x"), *_mat(x, n, d, x.dtype, "x"),
+                                       *_mat(q, n, d, torch.float8_e4m3fn, "q"), _vec(q_scale, n, torch.float32, "q_scale"))
+        if rc != OK:
+            self._check(rc)
+
+    def block_mean(self, x: torch.Tensor, indptr: torch.Tensor, col: torch.Tensor, mean: torch.Tensor, row: Optional[torch.Tensor] = None,
+                   own: Optional[torch.Tensor] = None, n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """mean[i] = the mean of x[col[e]] over row i's samples, own[i] = x[row[i]]; as many rows as mean has."""
+        x_type = _type(x, "x")
+        n_src, d = x.shape
+        n = mean.shape[0]
+        dt = x.dtype
+        _dev(indptr, torch.int64, "indptr"), _dev(col, torch.int32, "col")
+        assert indptr.numel() > n and (row is None or row.numel() >= n)
+        a = BlockMeanArgs(n, _count(n_rows_dev, "n_rows_dev"), d, n_src, col.numel(), x_type, 0, *_mat(x, n_src, d, dt, "x"), indptr.data_ptr(),
+                          col.data_ptr(), None if row is None else _dev_ptr(row, torch.int32, "row"), *_mat(mean, n, d, dt, "mean"),
+                          *_mat(own, n, d, dt, "own"))
+        rc = _lib.helios_block_mean(self._h, a)
+        if rc != OK:
+            self._check(rc)
+
+    def block_transpose(self, indptr: torch.Tensor, col: torch.Tensor, n_src: int, src_indptr: torch.Tensor, src_entry: torch.Tensor,
+                        row: Optional[torch.Tensor] = None, n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """The block's entries by source, for block_mean_grad; as many rows as indptr has."""
+        _dev(indptr, torch.int64, "indptr"), _dev(col, torch.int32, "col"), _dev(src_indptr, torch.int32, "src_indptr")
+        _dev(src_entry, torch.int32, "src_entry")
+        n = indptr.numel() - 1
+        assert n >= 0 and src_indptr.numel() > n_src and (row is None or row.numel() >= n)
+        assert src_entry.numel() >= col.numel() + (0 if row is None else n)
+        rc = _lib.helios_block_transpose(self._h, n, _count(n_rows_dev, "n_rows_dev"), indptr.data_ptr(), col.data_ptr(), col.numel(),
+                                         None if row is None else _dev_ptr(row, torch.int32, "row"), n_src, src_indptr.data_ptr(),
+                                         src_entry.data_ptr())
+        if rc != OK:
+            self._check(rc)
+
+    def block_mean_grad(self, indptr: torch.Tensor, src_indptr: torch.Tensor, src_entry: torch.Tensor, dmean: torch.Tensor, dx: torch.Tensor,
+                        down: Optional[torch.Tensor] = None) -> None:
+        """The gradient of block_mean, over as many sources as dx has rows."""
+        x_type = _type(dx, "dx")
+        n_src, d = dx.shape
+        n = dmean.shape[0]
+        dt = dx.dtype
+        _dev(indptr, torch.int64, "indptr"), _dev(src_indptr, torch.int32, "src_indptr"), _dev(src_entry, torch.int32, "src_entry")
+        assert indptr.numel() > n and src_indptr.numel() > n_src
+        a = BlockMeanGradArgs(n, d, n_src, src_entry.numel(), x_type, 0, indptr.data_ptr(), src_indptr.data_ptr(), src_entry.data_ptr(),
+                              *_mat(dmean, n, d, dt, "dmean"), *_mat(down, n, d, dt, "down"), *_mat(dx, n_src, d, dt, "dx"))
+        rc = _lib.helios_block_mean_grad(self._h, a)
+        if rc != OK:
+            self._check(rc)
 
     # ---- whole path
     def prepare_batch(self, seeds: torch.Tensor, fanouts: Sequence[int], rng_seed: int, hops: Sequence[HopBuffers],
