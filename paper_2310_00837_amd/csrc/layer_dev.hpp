@@ -128,6 +128,17 @@ __device__ __forceinline__ float act_of(int act, float z) {
     if (act == kActSilu) return z / (1.0f + __expf(-z));
     return z;
 }
+// the same for eight values (one branch for all of them)
+template <int ACT>
+__device__ __forceinline__ void act_each(float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = act_of(ACT, v[e]);
+}
+__device__ __forceinline__ void act_8(int act, float (&v)[8]) {
+    if (act == kActRelu) act_each<kActRelu>(v);
+    else if (act == kActGelu) act_each<kActGelu>(v);
+    else if (act == kActSilu) act_each<kActSilu>(v);
+}
 __device__ __forceinline__ float act_slope(int act, float z) {
     if (act == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
     if (act == kActGelu) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
@@ -136,6 +147,20 @@ __device__ __forceinline__ float act_slope(int act, float z) {
         return p * (1.0f + z * (1.0f - p));
     }
     return 1.0f;
+}
+
+// v *= the slopes at z
+__device__ __forceinline__ void scale_by_slope_8(int act, const float (&z)[8], float (&v)[8]) {
+    if (act == kActRelu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= act_slope(kActRelu, z[e]);
+    } else if (act == kActGelu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= act_slope(kActGelu, z[e]);
+    } else if (act == kActSilu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= act_slope(kActSilu, z[e]);
+    }
 }
 
 // Sum over the lanes of a group of G (a power of two, up to a wave), the same value in all of them.

@@ -66,25 +66,27 @@ template <> struct Mma<kE4M3> {
     }
 };
 
+__device__ const int32_t kZeroChunk[4] __attribute__((aligned(16))) = {0, 0, 0, 0};
+
 struct Operand {
     const char* data;
     int64_t ld;                                   // bytes from one row to the next
     int64_t rows, cols;                           // of the array in memory, in elements; what lies outside counts as zeros
 };
 
-// One operand's share of a stage: WIDTH rows of 128 bytes of k, or (STRIDED) the k-strided rows of WIDTH columns.
-template <int TYPE, int WIDTH, bool STRIDED, int THREADS>
+// One operand's share of a stage: WIDTH rows of ROW bytes of k, or (STRIDED) as many k-strided rows of WIDTH columns.
+template <int TYPE, int WIDTH, int ROW, bool STRIDED, int THREADS>
 struct Stage {
     static constexpr int kBytes = type_bytes(TYPE);
     static constexpr int kPer = 16 / kBytes;      // elements of a chunk
-    static constexpr int kK = kStageBytes / kBytes;
-    static constexpr int kChunks = WIDTH * (kStageBytes / 16);
+    static constexpr int kK = ROW / kBytes;
+    static constexpr int kChunks = WIDTH * (ROW / 16);
     static constexpr int kLoads = kChunks / THREADS;
-    static constexpr int kRowChunks = STRIDED ? WIDTH * kBytes / 16 : kStageBytes / 16;
+    static constexpr int kRowChunks = STRIDED ? WIDTH * kBytes / 16 : ROW / 16;
     static_assert(kChunks % THREADS == 0, "every thread stages as many chunks");
 
     static __device__ __forceinline__ uint32_t swizzle(uint32_t row) {
-        if (!STRIDED) return (row >> 1) & 7;
+        if (!STRIDED) return ROW == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
         if (kBytes == 4) return ((row >> 2) & 3) << 2;
         return ((row & 3) | (((row >> 3) & 1) << 2)) % (kRowChunks / 2) << 1;
     }
@@ -98,6 +100,41 @@ struct Stage {
             if (r < o.rows && c < o.cols) regs[l] = load_16_of<kBytes>(o.data + r * o.ld + c * kBytes, o.cols - c);
         }
     }
+    // The same straight into LDS, without a trip through registers: for rows of 16-byte multiples at 16-byte addresses.  Chunks of
+    // rows that do not exist are taken from the last that does (whatever they hold stays in rows and columns that are not
+    // written); chunks of k that do not exist are zeros.
+    struct Source {
+        const char* at[kLoads];
+    };
+    static __device__ __forceinline__ Source source(const Operand& o, int64_t first) {
+        Source s;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const uint32_t q = threadIdx.x + l * THREADS, row = q / kRowChunks, chunk = (q % kRowChunks) ^ swizzle(row);
+            if (STRIDED) {
+                const int64_t c = first + chunk * kPer, last = o.cols - kPer;
+                s.at[l] = o.data + row * o.ld + (c < last ? c : last) * kBytes;
+            } else {
+                const int64_t r = first + row, last = o.rows - 1;
+                s.at[l] = o.data + (r < last ? r : last) * o.ld + chunk * 16;
+            }
+        }
+        return s;
+    }
+    static __device__ __forceinline__ void load_lds(const Operand& o, const Source& s, int64_t k0, char* lds) {
+        const int64_t step = STRIDED ? k0 * o.ld : k0 * kBytes, left = (STRIDED ? o.rows : o.cols) - k0;
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const char* p = s.at[l] + step;
+            if (left < kK) {
+                const uint32_t q = threadIdx.x + l * THREADS, row = q / kRowChunks, chunk = (q % kRowChunks) ^ swizzle(row);
+                if (static_cast<int64_t>(STRIDED ? row : chunk * kPer) >= left) p = reinterpret_cast<const char*>(&kZeroChunk);
+            }
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                             (__attribute__((address_space(3))) void*)(lds + (wave * kWave + l * THREADS) * 16), 16, 0, 0);
+        }
+    }
     static __device__ __forceinline__ void put(char* lds, const i32x4 (&regs)[kLoads]) {
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) *reinterpret_cast<i32x4*>(lds + (threadIdx.x + l * THREADS) * 16) = regs[l];
@@ -108,7 +145,7 @@ struct Stage {
         const uint32_t lane = threadIdx.x & (kWave - 1), r = lane & 15, g = lane >> 4;
         if (!STRIDED) {
             const uint32_t row = at + r;
-            return *reinterpret_cast<const i32x4*>(lds + row * kStageBytes + (((g + 4 * half) ^ swizzle(row)) << 4));
+            return *reinterpret_cast<const i32x4*>(lds + row * ROW + (((g + 4 * half) ^ swizzle(row)) << 4));
         }
         if (kBytes == 4) {
             i32x4 v;
@@ -133,7 +170,12 @@ struct Stage {
     }
 };
 
-// The epilogues: eight neighbouring sums of a row.
+// The epilogues.  A thread has eight neighbouring columns, `valid` of them in the matrix, and goes through rows: at() takes what
+// belongs to the columns, row() finishes and writes the sums of one row.  The type written and whether the activation needs an
+// exponential are the kernel's: a round through a row is a chain that few waves have to bear, and with all types and activations
+// in it, it is longer (98 304 x 512 sums of 64 products in half precision: 33 us; branches for every row 44, for every
+// element 55).
+template <int OUT_TYPE, bool SMOOTH>
 struct ForwardOut {
     const float *x_scale, *w_scale;
     const void *bias, *residual;
@@ -142,40 +184,49 @@ struct ForwardOut {
     int64_t pre_ld;
     void* y;
     int64_t y_ld;
-    int act, type;
-    __device__ __forceinline__ void operator()(int64_t row, int col, int valid, float (&v)[8], int) const {
+    int act;
+    struct Columns {
+        int32_t col, valid;
+        float scale[8], bias[8], least;
+    };
+    __device__ __forceinline__ Columns at(int32_t col, int valid, int) const {
+        Columns c{col, valid, {1, 1, 1, 1, 1, 1, 1, 1}, {0, 0, 0, 0, 0, 0, 0, 0}, act == kActRelu ? 0.0f : -__builtin_inff()};
+        if (w_scale) load_8_of<kF32>(w_scale, col, valid, c.scale);
+        if (bias) load_8_of<OUT_TYPE>(bias, col, valid, c.bias);
+        return c;
+    }
+    __device__ __forceinline__ void row(const Columns& c, int64_t row, float (&v)[8]) const {
         if (x_scale) {
             const float s = x_scale[row];
-            float t[8];
-            load_8_of<kF32>(w_scale, col, valid, t);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= s * t[e];
+            for (int e = 0; e < 8; ++e) v[e] *= s * c.scale[e];
         }
-        if (bias) {
-            float b[8];
-            load_8_of(type, bias, col, valid, b);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += b[e];
-        }
-        if (pre) store_8_of(type, pre, row * pre_ld + col, valid, v);
+        for (int e = 0; e < 8; ++e) v[e] += c.bias[e];
+        if (pre) store_8_of<OUT_TYPE>(pre, row * pre_ld + c.col, c.valid, v);
+        if (SMOOTH) act_8(act, v);
+        else
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = act_of(act, v[e]);
+            for (int e = 0; e < 8; ++e) v[e] = v[e] < c.least ? c.least : v[e];        // NaN stays
         if (residual) {
             float r[8];
-            load_8_of(type, residual, row * residual_ld + col, valid, r);
+            load_8_of<OUT_TYPE>(residual, row * residual_ld + c.col, c.valid, r);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += r[e];
         }
-        store_8_of(type, y, row * y_ld + col, valid, v);
+        store_8_of<OUT_TYPE>(y, row * y_ld + c.col, c.valid, v);
     }
 };
+template <int OUT_TYPE>
 struct PlainOut {                                 // (slice: which part of k the sums are of)
     void* y;
     int64_t ld, slice_stride;
-    int type;
-    __device__ __forceinline__ void operator()(int64_t row, int col, int valid, float (&v)[8], int slice) const {
-        store_8_of(type, y, slice * slice_stride + row * ld + col, valid, v);
-    }
+    struct Columns {
+        int64_t at;
+        int32_t valid;
+    };
+    __device__ __forceinline__ Columns at(int32_t col, int valid, int slice) const { return Columns{slice * slice_stride + col, valid}; }
+    __device__ __forceinline__ void row(const Columns& c, int64_t row, float (&v)[8]) const { store_8_of<OUT_TYPE>(y, c.at + row * ld, c.valid, v); }
 };
 
 template <class OUT>
@@ -197,15 +248,32 @@ __device__ __forceinline__ void tile_of(uint32_t block, uint32_t tiles_n, uint32
     *tile_n = at % tiles_n;
 }
 
-template <int TYPE, int BM, int BN, int WAVES_M, int WAVES_N, bool A_STRIDED, bool B_STRIDED, class OUT>
-__global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void product_kernel(ProductArgs<OUT> p) {
-    constexpr int kThreads = WAVES_M * WAVES_N * kWave;
+// Waits until at most AHEAD of this wave's loads are in flight and its LDS reads are done, then for the other waves.
+template <int AHEAD>
+__device__ __forceinline__ void wait_and_meet() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(AHEAD) : "memory");
+}
+
+// Shape of a workgroup's tile: rows of A and B, the waves that share it, bytes of k to a stage, stages in LDS.
+template <int M, int N, int WAVES_M, int WAVES_N, int ROW, int STAGES>
+struct Tile {
+    static constexpr int kM = M, kN = N, kWavesM = WAVES_M, kWavesN = WAVES_N, kRow = ROW, kStages = STAGES;
+    static constexpr int kThreads = WAVES_M * WAVES_N * kWave;
+};
+
+template <int TYPE, class TILE, bool A_STRIDED, bool B_STRIDED, bool DIRECT, class OUT>
+__global__ __launch_bounds__(TILE::kThreads) void product_kernel(ProductArgs<OUT> p) {
+    constexpr int BM = TILE::kM, BN = TILE::kN, WAVES_M = TILE::kWavesM, WAVES_N = TILE::kWavesN, ROW = TILE::kRow, kThreads = TILE::kThreads;
+    constexpr int kStages = DIRECT ? TILE::kStages : 2;
     constexpr int kTm = BM / WAVES_M / 16, kTn = BN / WAVES_N / 16;      // 16 x 16 tiles of a wave
-    typedef Stage<TYPE, BM, A_STRIDED, kThreads> StageA;
-    typedef Stage<TYPE, BN, B_STRIDED, kThreads> StageB;
-    constexpr int kStage = (BM + BN) * kStageBytes;
+    typedef Stage<TYPE, BM, ROW, A_STRIDED, kThreads> StageA;
+    typedef Stage<TYPE, BN, ROW, B_STRIDED, kThreads> StageB;
+    constexpr int kStage = (BM + BN) * ROW;
     constexpr int kOutLd = BN + 4;
-    constexpr int kLds = 2 * kStage > BM * kOutLd * 4 ? 2 * kStage : BM * kOutLd * 4;
+    constexpr int kOutBytes = WAVES_M * 16 * kOutLd * 4;                 // of the sums of one row of tiles of every wave
+    constexpr int kOutTiles = kTm * kOutBytes <= kStages * kStage + 4096 ? kTm : kTm % 2 == 0 && kTm / 2 * kOutBytes <= kStages * kStage ? kTm / 2 : 1;
+    constexpr int kLds = kStages * kStage > kOutTiles * kOutBytes ? kStages * kStage : kOutTiles * kOutBytes;
+    static_assert(kOutTiles >= 1 && kTm % kOutTiles == 0, "the epilogue takes as many rows of tiles at a time");
     __shared__ __align__(16) char lds[kLds];
 
     const int64_t count = p.rows.get();
@@ -230,51 +298,88 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N* kWave) void product_kernel(Produc
     #pragma unroll
             for (int j = 0; j < kTn; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
-        i32x4 ra[StageA::kLoads], rb[StageB::kLoads];
-        if (step0 < step1) {
-            StageA::load(p.a, m0, step0 * StageA::kK, ra);
-            StageB::load(p.b, n0, step0 * StageA::kK, rb);
-        }
-        for (int64_t step = step0; step < step1; ++step) {
-            char* stage = lds + (step & 1) * kStage;
-            StageA::put(stage, ra);
-            StageB::put(stage + BM * kStageBytes, rb);
-            __syncthreads();                          // (the other stage's readers are done when its writers come round again)
-            if (step + 1 < step1) {
-                StageA::load(p.a, m0, (step + 1) * StageA::kK, ra);
-                StageB::load(p.b, n0, (step + 1) * StageA::kK, rb);
-            }
+        const auto multiply = [&](const char* stage) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
+            for (int half = 0; half < ROW / 64; ++half) {
                 typename Mma<TYPE>::Part fa[kTm], fb[kTn];
 #pragma unroll
                 for (int i = 0; i < kTm; ++i) fa[i] = Mma<TYPE>::part(StageA::fragment(stage, (wave_m * kTm + i) * 16, half));
 #pragma unroll
-                for (int j = 0; j < kTn; ++j) fb[j] = Mma<TYPE>::part(StageB::fragment(stage + BM * kStageBytes, (wave_n * kTn + j) * 16, half));
+                for (int j = 0; j < kTn; ++j) fb[j] = Mma<TYPE>::part(StageB::fragment(stage + BM * ROW, (wave_n * kTn + j) * 16, half));
 #pragma unroll
                 for (int i = 0; i < kTm; ++i)
 #pragma unroll
                     for (int j = 0; j < kTn; ++j) acc[i][j] = Mma<TYPE>::run(fa[i], fb[j], acc[i][j]);
             }
+        };
+        // One barrier a step: what it waits for is the step's loads (those of the stages ahead stay in flight) and every wave's reads of
+        // the stage before, which the next loads go to.
+        if constexpr (DIRECT) {
+            const typename StageA::Source sa = StageA::source(p.a, m0);
+            const typename StageB::Source sb = StageB::source(p.b, n0);
+            constexpr int kAhead = (kStages - 2) * (StageA::kLoads + StageB::kLoads);
+            const int steps = static_cast<int>(step1 - step0);
+            const auto load = [&](int step, int stage) {
+                char* to = lds + stage * kStage;
+                StageA::load_lds(p.a, sa, (step0 + step) * StageA::kK, to);
+                StageB::load_lds(p.b, sb, (step0 + step) * StageA::kK, to + BM * ROW);
+            };
+#pragma unroll
+            for (int s = 0; s < kStages - 1; ++s)
+                if (s < steps) load(s, s);
+            int stage = 0;
+            for (int step = 0; step < steps; ++step) {
+                if (step + kStages - 2 < steps) wait_and_meet<kAhead>();
+                else wait_and_meet<0>();
+                if (step + kStages - 1 < steps) load(step + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+                multiply(lds + stage * kStage);
+                stage = stage + 1 < kStages ? stage + 1 : 0;
+            }
+        } else {
+            i32x4 ra[StageA::kLoads], rb[StageB::kLoads];
+            if (step0 < step1) {
+                StageA::load(p.a, m0, step0 * StageA::kK, ra);
+                StageB::load(p.b, n0, step0 * StageA::kK, rb);
+            }
+            for (int64_t step = step0; step < step1; ++step) {
+                char* stage = lds + ((step - step0) & 1) * kStage;
+                StageA::put(stage, ra);
+                StageB::put(stage + BM * ROW, rb);
+                __syncthreads();
+                if (step + 1 < step1) {
+                    StageA::load(p.a, m0, (step + 1) * StageA::kK, ra);
+                    StageB::load(p.b, n0, (step + 1) * StageA::kK, rb);
+                }
+                multiply(stage);
+            }
         }
         __syncthreads();
-        // The sums go through LDS, so that the epilogue reads and writes whole rows.
+        // The sums go through LDS, so that the epilogue reads and writes whole rows; kOutTiles of every wave's rows of tiles at a time.
         float* sums = reinterpret_cast<float*>(lds);
         const int r = threadIdx.x & 15, g = (threadIdx.x & (kWave - 1)) >> 4;
-    #pragma unroll
-        for (int i = 0; i < kTm; ++i)
-    #pragma unroll
-            for (int j = 0; j < kTn; ++j)
-                *reinterpret_cast<f32x4*>(sums + ((wave_m * kTm + i) * 16 + r) * kOutLd + (wave_n * kTn + j) * 16 + 4 * g) = acc[i][j];
-        __syncthreads();
-        for (int u = threadIdx.x; u < BM * BN / 8; u += kThreads) {
-            const int row = u / (BN / 8), col = u % (BN / 8) * 8;
-            const int valid = p.n - n0 - col;
-            if (m0 + row >= m_end || valid <= 0) continue;
-            float v[8];
-    #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = sums[row * kOutLd + col + e];
-            p.out(m0 + row, n0 + col, valid < 8 ? valid : 8, v, slice);
+        static_assert(kThreads % (BN / 8) == 0, "a thread stays with its columns");
+        const int out_col = threadIdx.x % (BN / 8) * 8;
+        const typename OUT::Columns columns = p.out.at(n0 + out_col, p.n - n0 - out_col, slice);
+#pragma unroll
+        for (int i0 = 0; i0 < kTm; i0 += kOutTiles) {
+            if (i0 > 0) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kOutTiles; ++i)
+#pragma unroll
+                for (int j = 0; j < kTn; ++j)
+                    *reinterpret_cast<f32x4*>(sums + ((wave_m * kOutTiles + i) * 16 + r) * kOutLd + (wave_n * kTn + j) * 16 + 4 * g) = acc[i0 + i][j];
+            __syncthreads();
+            const int valid = p.n - n0 - out_col;
+            constexpr int kSlab = kOutTiles * 16;                        // the rows of one row of waves
+            if (valid > 0)
+                for (int at = threadIdx.x / (BN / 8); at < WAVES_M * kSlab; at += kThreads / (BN / 8)) {
+                    const int64_t row = m0 + at / kSlab * (kTm * 16) + i0 * 16 + at % kSlab;
+                    if (row >= m_end) continue;
+                    const f32x4* from = reinterpret_cast<const f32x4*>(sums + at * kOutLd + out_col);
+                    const f32x4 lo = from[0], hi = from[1];
+                    float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                    p.out.row(columns, row, v);
+                }
         }
         __syncthreads();
     }
@@ -319,7 +424,7 @@ __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(ProductAr
 #pragma unroll
                 for (int w = 0; w < kFewWaves; ++w) v[e] += sums[w][row][col + e];
             }
-            p.out(m0 + row, n0 + col, valid < 8 ? valid : 8, v, 0);
+            p.out.row(p.out.at(n0 + col, valid, 0), m0 + row, v);
         }
     }
 }
@@ -355,8 +460,7 @@ __global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
             if (p.act != kActNone) {
                 float z[8];
                 load_8_of(p.type, p.pre, row * p.pre_ld + col, valid, z);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] *= act_slope(p.act, z[e]);
+                scale_by_slope_8(p.act, z, d);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += d[e];
@@ -408,20 +512,31 @@ Operand operand(const void* data, int64_t ld, int type, int64_t rows, int64_t co
 uint32_t tiles_of(int64_t n, int tile) { return static_cast<uint32_t>((n + tile - 1) / tile); }
 
 // grid of tile_of: rows of tiles in eights, one for each XCD
-template <int TYPE, int BM, int BN, int WM, int WN, bool AS, bool BS, class OUT>
+// whether rows can go straight to LDS: 16-byte multiples at 16-byte addresses
+bool direct(const Operand& o, int bytes) {
+    return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % 16 == 0 && o.cols * bytes % 16 == 0;
+}
+
+template <int TYPE, class TILE, bool AS, bool BS, class OUT>
 hipError_t launch_tiles(hipStream_t stream, ProductArgs<OUT> p) {
-    p.tiles_n = tiles_of(p.n, BN);
-    const int64_t tiles = (tiles_of(p.m, BM) + 7ll) / 8 * 8 * p.tiles_n;
+    p.tiles_n = tiles_of(p.n, TILE::kN);
+    const int64_t tiles = (tiles_of(p.m, TILE::kM) + 7ll) / 8 * 8 * p.tiles_n;
     if (tiles >= 1ll << 32) return hipErrorInvalidValue;
     p.tiles = static_cast<uint32_t>(tiles);
     const dim3 grid(std::min(p.tiles, kMostBlocks), static_cast<unsigned>(p.slices));
-    hipLaunchKernelGGL((product_kernel<TYPE, BM, BN, WM, WN, AS, BS, OUT>), grid, dim3(WM * WN * kWave), 0, stream, p);
+    if (direct(p.a, type_bytes(TYPE)) && direct(p.b, type_bytes(TYPE)))
+        hipLaunchKernelGGL((product_kernel<TYPE, TILE, AS, BS, true, OUT>), grid, dim3(TILE::kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((product_kernel<TYPE, TILE, AS, BS, false, OUT>), grid, dim3(TILE::kThreads), 0, stream, p);
     return hipGetLastError();
 }
 
-template <int TYPE>
+typedef Tile<128, 128, 2, 4, 128, 2> Large;
+typedef Tile<64, 64, 2, 2, 128, 2> Small;
+
+template <int TYPE, int OUT_TYPE, bool SMOOTH>
 hipError_t forward(hipStream_t stream, const LinearJob& j) {
-    ProductArgs<ForwardOut> p{};
+    typedef ForwardOut<OUT_TYPE, SMOOTH> Out;
+    ProductArgs<Out> p{};
     p.a = operand(j.x, j.x_ld, TYPE, j.rows.host, j.n_in);
     p.b = operand(j.w, j.w_ld, TYPE, j.n_out, j.n_in);
     p.m = j.rows.host;
@@ -429,14 +544,18 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
     p.k = j.n_in;
     p.rows = j.rows;
     p.slices = 1;
-    p.out = ForwardOut{j.x_scale, j.w_scale, j.bias, j.residual, j.residual_ld, j.pre, j.pre_ld, j.y, j.y_ld, j.act, j.out_type};
+    p.out = Out{j.x_scale, j.w_scale, j.bias, j.residual, j.residual_ld, j.pre, j.pre_ld, j.y, j.y_ld, j.act};
     if (p.m <= 16) {
         const dim3 grid(tiles_of(p.n, 16), tiles_of(p.m, 16));
-        hipLaunchKernelGGL((product_few_kernel<TYPE, ForwardOut>), grid, dim3(kFewWaves * kWave), 0, stream, p);
+        hipLaunchKernelGGL((product_few_kernel<TYPE, Out>), grid, dim3(kFewWaves * kWave), 0, stream, p);
         return hipGetLastError();
     }
-    if (static_cast<int64_t>(tiles_of(p.m, 128)) * tiles_of(p.n, 128) >= 256) return launch_tiles<TYPE, 128, 128, 2, 2, false, false>(stream, p);
-    return launch_tiles<TYPE, 64, 64, 2, 2, false, false>(stream, p);
+    if (static_cast<int64_t>(tiles_of(p.m, 128)) * tiles_of(p.n, 128) >= 256) return launch_tiles<TYPE, Large, false, false>(stream, p);
+    return launch_tiles<TYPE, Small, false, false>(stream, p);
+}
+template <int TYPE, int OUT_TYPE>
+hipError_t forward(hipStream_t stream, const LinearJob& j) {
+    return j.act == kActGelu || j.act == kActSilu ? forward<TYPE, OUT_TYPE, true>(stream, j) : forward<TYPE, OUT_TYPE, false>(stream, j);
 }
 
 struct GradPlan {                                 // of linear_grad: what lies where in the scratch, and how far k is cut up
@@ -474,7 +593,7 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         e = hipGetLastError();
     }
     if (e == hipSuccess && j.dx && j.rows.host > 0) {
-        ProductArgs<PlainOut> p{};
+        ProductArgs<PlainOut<TYPE>> p{};
         p.a = operand(dz, dz_ld, TYPE, j.rows.host, j.n_out);
         p.b = operand(j.w, j.w_ld, TYPE, j.n_out, j.n_in);
         p.m = j.rows.host;
@@ -482,12 +601,12 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         p.k = j.n_out;
         p.rows = j.rows;
         p.slices = 1;
-        p.out = PlainOut{j.dx, j.dx_ld, 0, TYPE};
-        if (static_cast<int64_t>(tiles_of(p.m, 128)) * tiles_of(p.n, 128) >= 256) e = launch_tiles<TYPE, 128, 128, 2, 2, false, true>(stream, p);
-        else e = launch_tiles<TYPE, 64, 64, 2, 2, false, true>(stream, p);
+        p.out = PlainOut<TYPE>{j.dx, j.dx_ld, 0};
+        if (static_cast<int64_t>(tiles_of(p.m, 128)) * tiles_of(p.n, 128) >= 256) e = launch_tiles<TYPE, Large, false, true>(stream, p);
+        else e = launch_tiles<TYPE, Small, false, true>(stream, p);
     }
     if (e == hipSuccess && j.dw) {
-        ProductArgs<PlainOut> p{};
+        ProductArgs<PlainOut<kF32>> p{};
         p.a = operand(dz, dz_ld, TYPE, j.rows.host, j.n_out);
         p.b = operand(j.x, j.x_ld, TYPE, j.rows.host, j.n_in);
         p.m = j.n_out;
@@ -495,8 +614,8 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         p.k = j.rows.host;
         p.rows = j.rows;
         p.slices = plan.slices;
-        p.out = PlainOut{scratch + plan.part, j.n_in, static_cast<int64_t>(j.n_out) * j.n_in, kF32};
-        e = launch_tiles<TYPE, 64, 64, 2, 2, true, true>(stream, p);
+        p.out = PlainOut<kF32>{scratch + plan.part, j.n_in, static_cast<int64_t>(j.n_out) * j.n_in};
+        e = launch_tiles<TYPE, Small, true, true>(stream, p);
     }
     if (e == hipSuccess && (j.dw || j.dbias)) {
         JoinArgs a{};
@@ -527,10 +646,11 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
 hipError_t launch_linear(hipStream_t stream, const LinearJob& j) {
     if (j.rows.host < 1) return hipSuccess;
     switch (j.x_type) {
-        case kF32: return forward<kF32>(stream, j);
-        case kF16: return forward<kF16>(stream, j);
-        case kBF16: return forward<kBF16>(stream, j);
-        case kE4M3: return forward<kE4M3>(stream, j);
+        case kF32: return forward<kF32, kF32>(stream, j);
+        case kF16: return j.out_type == kF32 ? forward<kF16, kF32>(stream, j) : forward<kF16, kF16>(stream, j);
+        case kBF16: return j.out_type == kF32 ? forward<kBF16, kF32>(stream, j) : forward<kBF16, kBF16>(stream, j);
+        case kE4M3:
+            return j.out_type == kF32 ? forward<kE4M3, kF32>(stream, j) : j.out_type == kF16 ? forward<kE4M3, kF16>(stream, j) : forward<kE4M3, kBF16>(stream, j);
     }
     return hipErrorInvalidValue;
 }
