@@ -122,10 +122,22 @@ __device__ __forceinline__ void store_1(int type, void* base, int64_t at, float 
     else static_cast<__bf16*>(base)[at] = static_cast<__bf16>(v);
 }
 
+// The normal distribution's Phi(z) and density at z, by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: erfc(u) =
+// (a1 t + ... + a5 t^5) exp(-u^2), t = 1 / (1 + p u), off by at most 1.5e-7.  One exponential serves both (the library's erff
+// took three times as long: it is what the gradient's first step was bound by).
+__device__ __forceinline__ float normal_cdf(float z, float* density) {
+    const float u = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * u), e = __expf(-u * u);
+    const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    *density = 0.39894228040143268f * e;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
 __device__ __forceinline__ float act_of(int act, float z) {
     if (act == kActRelu) return z < 0.0f ? 0.0f : z;                                   // NaN stays NaN
-    if (act == kActGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    if (act == kActSilu) return z / (1.0f + __expf(-z));
+    if (act == kActGelu) {
+        float density;
+        return z * normal_cdf(z, &density);
+    }
+    if (act == kActSilu) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
     return z;
 }
 // the same for eight values (one branch for all of them)
@@ -141,9 +153,13 @@ __device__ __forceinline__ void act_8(int act, float (&v)[8]) {
 }
 __device__ __forceinline__ float act_slope(int act, float z) {
     if (act == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
-    if (act == kActGelu) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
+    if (act == kActGelu) {
+        float density;
+        const float phi = normal_cdf(z, &density);
+        return phi + z * density;
+    }
     if (act == kActSilu) {
-        const float p = 1.0f / (1.0f + __expf(-z));
+        const float p = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
         return p * (1.0f + z * (1.0f - p));
     }
     return 1.0f;
@@ -180,21 +196,28 @@ __device__ __forceinline__ float group_max(float v) {
     return v;
 }
 
-// out[c] = the sum over p of part[p][c], p < n_parts, for the 16 columns from `first` on, by a workgroup of kBlock threads: 16 of
-// them share a column, each with every 16th part, and the sixteen sums are added in order.
+// out[c] = the sum over p of part[p][c], p < n_parts, for the 16 columns from `first` on, by a workgroup of kBlock threads.  Four of
+// them share a part's columns and 64 go through the parts, so that few loads follow on one another; the order of the additions
+// is the same in every call.
 constexpr int kSumColumns = 16;
 __device__ __forceinline__ void sum_columns(const float* part, int n_parts, int32_t n, int32_t first, void* out, int type) {
-    __shared__ float s[kBlock / kSumColumns][kSumColumns + 1];
-    const int c = threadIdx.x % kSumColumns, sub = threadIdx.x / kSumColumns;
-    float t = 0;
-    if (first + c < n)
-        for (int p = sub; p < n_parts; p += kBlock / kSumColumns) t += part[static_cast<int64_t>(p) * n + first + c];
-    s[sub][c] = t;
-    __syncthreads();
-    if (sub == 0 && first + c < n) {
+    constexpr int kSubs = kBlock / 4;
+    __shared__ float s[kSubs][kSumColumns + 1], s2[16][kSumColumns + 1];
+    const int c = threadIdx.x % 4 * 4, sub = threadIdx.x / 4, valid = n - first - c;
+    f32x4 t = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int p = sub; p < n_parts; p += kSubs) t += __builtin_bit_cast(f32x4, load_16_of<4>(part + static_cast<int64_t>(p) * n + first + c, valid));
 #pragma unroll
-        for (int k = 1; k < kBlock / kSumColumns; ++k) t += s[k][c];
-        store_1(type, out, first + c, t);
+    for (int e = 0; e < 4; ++e) s[sub][c + e] = t[e];
+    __syncthreads();
+    const int col = threadIdx.x % 16, q = threadIdx.x / 16;
+    s2[q][col] = (s[4 * q][col] + s[4 * q + 1][col]) + (s[4 * q + 2][col] + s[4 * q + 3][col]);
+    __syncthreads();
+    if (q == 0 && first + col < n) {
+        float v = 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v += s2[k][col];
+        store_1(type, out, first + col, v);
     }
 }
 

@@ -235,17 +235,17 @@ struct ProductArgs {
     int64_t m, k;                                 // the most; `rows` limits m, or k where that runs over rows
     int32_t n;
     Count rows;
-    uint32_t tiles_n, tiles;
-    int slices;                                   // parts that k is cut into, each with sums of its own
+    uint32_t tiles_n, members, tiles;             // (members: of a group)
+    int slices;                                   // parts that k is cut into where it runs over rows, each with sums of its own
     OUT out;
 };
 
-// Tile of a workgroup.  Workgroups go round the eight XCDs, each of which has an L2 of its own: the tiles that share rows of A are
-// neighbours on one XCD.
-__device__ __forceinline__ void tile_of(uint32_t block, uint32_t tiles_n, uint32_t* tile_m, uint32_t* tile_n) {
+// Workgroups go round the eight XCDs, each of which has an L2 of its own.  The tiles that share what is long (rows of A; where k runs
+// over rows, a slice of it) are a group, and a group's tiles are neighbours on one XCD.
+__device__ __forceinline__ void tile_of(uint32_t block, uint32_t members, uint32_t* group, uint32_t* member) {
     const uint32_t xcd = block % 8, at = block / 8;
-    *tile_m = at / tiles_n * 8 + xcd;
-    *tile_n = at % tiles_n;
+    *group = at / members * 8 + xcd;
+    *member = at % members;
 }
 
 // Waits until at most AHEAD of this wave's loads are in flight and its LDS reads are done, then for the other waves.
@@ -281,17 +281,17 @@ __global__ __launch_bounds__(TILE::kThreads) void product_kernel(ProductArgs<OUT
     const int64_t m_end = rows_are_k ? p.m : count, k_end = rows_are_k ? count : p.k;
     if (rows_are_k) p.a.rows = p.b.rows = count;
     else p.a.rows = count;
-    const int slice = blockIdx.y;
     const int64_t steps_all = (k_end + StageA::kK - 1) / StageA::kK, per = (steps_all + p.slices - 1) / p.slices;
-    const int64_t step0 = slice * per, step1 = step0 + per < steps_all ? step0 + per : steps_all;
 
     const int wave = threadIdx.x / kWave, wave_m = wave / WAVES_N, wave_n = wave % WAVES_N;
     for (uint32_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {      // (once round, but for the longest lists)
-        uint32_t tile_m, tile_n;
-        tile_of(tile, p.tiles_n, &tile_m, &tile_n);
-        const int64_t m0 = static_cast<int64_t>(tile_m) * BM;
-        const int32_t n0 = static_cast<int32_t>(tile_n) * BN;
-        if (m0 >= m_end) continue;
+        uint32_t group, member;
+        tile_of(tile, p.members, &group, &member);
+        const int slice = rows_are_k ? static_cast<int>(group) : 0;
+        const int64_t m0 = static_cast<int64_t>(rows_are_k ? member / p.tiles_n : group) * BM;
+        const int32_t n0 = static_cast<int32_t>(rows_are_k ? member % p.tiles_n : member) * BN;
+        if (m0 >= m_end || slice >= p.slices) continue;
+        const int64_t step0 = slice * per, step1 = step0 + per < steps_all ? step0 + per : steps_all;
         f32x4 acc[kTm][kTn];
     #pragma unroll
         for (int i = 0; i < kTm; ++i)
@@ -433,11 +433,12 @@ __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(ProductAr
 
 // dz = dy * act'(pre), rounded to the type the products work in, and the sums of dz's columns (from the values before
 // they are rounded) over the rows of a workgroup.
-constexpr int kSlopeCols = 16 * 8;                // columns of a workgroup: 16 lanes, 8 each; 16 rows at a time
+constexpr int kSlopeCols = 16 * 8;                // columns of a workgroup: 16 lanes, 8 each
+constexpr int kSlopeRows = 2;                     // rows that a thread has in flight; 16 threads go through a workgroup's rows
 struct SlopeArgs {
     Count rows;
     int32_t n;
-    int act, type, z_type;
+    int act;
     const void* dy;
     int64_t dy_ld;
     const void* pre;
@@ -446,6 +447,7 @@ struct SlopeArgs {
     int64_t dz_ld;
     float* sums;                                  // [gridDim.y][n], nullable
 };
+template <int TYPE, int Z_TYPE, bool SLOPE>
 __global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
     __shared__ float s[16][kSlopeCols + 4];
     const int64_t count = p.rows.get(), per = (count + gridDim.y - 1) / gridDim.y;
@@ -454,17 +456,22 @@ __global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
     const int valid = p.n - col < 8 ? p.n - col : 8;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (valid > 0)
-        for (int64_t row = row0 + sub; row < row1; row += 16) {
-            float d[8];
-            load_8_of(p.type, p.dy, row * p.dy_ld + col, valid, d);
-            if (p.act != kActNone) {
-                float z[8];
-                load_8_of(p.type, p.pre, row * p.pre_ld + col, valid, z);
-                scale_by_slope_8(p.act, z, d);
+        for (int64_t row = row0 + sub; row < row1; row += 16 * kSlopeRows) {
+            float d[kSlopeRows][8], z[kSlopeRows][8];
+#pragma unroll
+            for (int k = 0; k < kSlopeRows; ++k) {
+                const int64_t r = row + 16 * k < row1 ? row + 16 * k : row;            // (a row that there is; its values are dropped below)
+                load_8_of<TYPE>(p.dy, r * p.dy_ld + col, valid, d[k]);
+                if (SLOPE) load_8_of<TYPE>(p.pre, r * p.pre_ld + col, valid, z[k]);
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += d[e];
-            if (p.dz) store_8_of(p.z_type, p.dz, row * p.dz_ld + col, valid, d);
+            for (int k = 0; k < kSlopeRows; ++k) {
+                if (row + 16 * k >= row1) continue;
+                if (SLOPE) scale_by_slope_8(p.act, z[k], d[k]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += d[k][e];
+                if (p.dz) store_8_of<Z_TYPE>(p.dz, (row + 16 * k) * p.dz_ld + col, valid, d[k]);
+            }
         }
     if (!p.sums) return;
 #pragma unroll
@@ -498,11 +505,20 @@ __global__ __launch_bounds__(kBlock) void join_kernel(JoinArgs p) {
         sum_columns(p.sums, p.n_sums, p.n, (blockIdx.x - p.cell_blocks) * kSumColumns, p.sum_out, p.sum_type);
         return;
     }
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 2;
     if (c >= p.cells) return;
-    float t = 0;
-    for (int s = 0; s < p.slices; ++s) t += p.part[s * p.cells + c];
-    store_1(p.type, p.out, c / p.cols * p.out_ld + c % p.cols, t);
+    typedef float f32x2 __attribute__((ext_vector_type(2), aligned(4)));
+    const bool pair = c + 1 < p.cells;
+    float a = 0, b = 0;
+#pragma unroll 8
+    for (int s = 0; s < p.slices; ++s) {
+        const float* from = p.part + s * p.cells + c;
+        const f32x2 v = pair ? *reinterpret_cast<const f32x2*>(from) : f32x2{*from, 0.0f};
+        a += v.x;
+        b += v.y;
+    }
+    store_1(p.type, p.out, c / p.cols * p.out_ld + c % p.cols, a);
+    if (pair) store_1(p.type, p.out, (c + 1) / p.cols * p.out_ld + (c + 1) % p.cols, b);
 }
 
 Operand operand(const void* data, int64_t ld, int type, int64_t rows, int64_t cols) {
@@ -520,10 +536,12 @@ bool direct(const Operand& o, int bytes) {
 template <int TYPE, class TILE, bool AS, bool BS, class OUT>
 hipError_t launch_tiles(hipStream_t stream, ProductArgs<OUT> p) {
     p.tiles_n = tiles_of(p.n, TILE::kN);
-    const int64_t tiles = (tiles_of(p.m, TILE::kM) + 7ll) / 8 * 8 * p.tiles_n;
+    const int64_t tiles_m = tiles_of(p.m, TILE::kM), members = AS ? tiles_m * p.tiles_n : p.tiles_n, groups = AS ? p.slices : tiles_m;
+    const int64_t tiles = (groups + 7) / 8 * 8 * members;
     if (tiles >= 1ll << 32) return hipErrorInvalidValue;
+    p.members = static_cast<uint32_t>(members);
     p.tiles = static_cast<uint32_t>(tiles);
-    const dim3 grid(std::min(p.tiles, kMostBlocks), static_cast<unsigned>(p.slices));
+    const dim3 grid(std::min(p.tiles, kMostBlocks));
     if (direct(p.a, type_bytes(TYPE)) && direct(p.b, type_bytes(TYPE)))
         hipLaunchKernelGGL((product_kernel<TYPE, TILE, AS, BS, true, OUT>), grid, dim3(TILE::kThreads), 0, stream, p);
     else hipLaunchKernelGGL((product_kernel<TYPE, TILE, AS, BS, false, OUT>), grid, dim3(TILE::kThreads), 0, stream, p);
@@ -559,7 +577,7 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
 }
 
 struct GradPlan {                                 // of linear_grad: what lies where in the scratch, and how far k is cut up
-    bool needs_dz;
+    bool needs_dz, large;                         // large: dw by large tiles
     int64_t dz_ld;
     int slices;                                   // of dw's k
     unsigned slope_blocks;                        // workgroups along the rows of the slope kernel
@@ -569,10 +587,15 @@ struct GradPlan {                                 // of linear_grad: what lies w
         const int64_t n = j.rows.host;
         needs_dz = (j.dx || j.dw) && (j.act != kActNone || j.out_type != j.x_type);
         dz_ld = (j.n_out + 7) / 8 * 8;
-        const int64_t tiles = static_cast<int64_t>(tiles_of(j.n_out, 64)) * tiles_of(j.n_in, 64);
-        const int64_t steps = (n * type_bytes(j.x_type) + kStageBytes - 1) / kStageBytes;
-        slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({1024 / std::max<int64_t>(tiles, 1), steps / 4, 64})));
-        slope_blocks = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, 256)));
+        // dw's k, the rows, is cut so that there are about 1024 small tiles or 512 large ones, in eights (one for each XCD) of at least
+        // four steps.  us, 26 624 x 512 x 256 in bfloat16: small tiles 16 slices 21.7, 32 17.4; large ones 32 20.5, 64 19.3;
+        // 50 000 x 2048 x 512: large ones 4 slices 223, 8 141, 16 150.
+        const auto tiles = [&](int64_t edge) { return (j.n_out + edge - 1) / edge * ((j.n_in + edge - 1) / edge); };
+        const int64_t steps = (n * type_bytes(j.x_type) + Large::kRow - 1) / Large::kRow;
+        large = tiles(128) >= 64;
+        const int64_t want = std::max<int64_t>(1, std::min((large ? 512 : 1024) / std::max<int64_t>(tiles(large ? 128 : 64), 1), steps / 4));
+        slices = static_cast<int>(want >= 8 ? want / 8 * 8 : want);
+        slope_blocks = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((n + 31) / 32, 512)));
         dz = 0;
         part = dz + (needs_dz ? up(static_cast<size_t>(n * dz_ld) * type_bytes(j.x_type)) : 0);
         sums = part + (j.dw ? up(static_cast<size_t>(slices) * j.n_out * j.n_in * sizeof(float)) : 0);
@@ -587,9 +610,14 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
     const int64_t dz_ld = plan.needs_dz ? plan.dz_ld : j.dy_ld;
     hipError_t e = hipSuccess;
     if (plan.needs_dz || j.dbias) {
-        SlopeArgs s{j.rows, j.n_out, j.act, j.out_type, TYPE, j.dy, j.dy_ld, j.pre, j.pre_ld, plan.needs_dz ? scratch + plan.dz : nullptr, plan.dz_ld,
+        SlopeArgs s{j.rows, j.n_out, j.act, j.dy, j.dy_ld, j.pre, j.pre_ld, plan.needs_dz ? scratch + plan.dz : nullptr, plan.dz_ld,
                     j.dbias ? reinterpret_cast<float*>(scratch + plan.sums) : nullptr};
-        hipLaunchKernelGGL(slope_kernel, dim3(tiles_of(j.n_out, kSlopeCols), plan.slope_blocks), dim3(kBlock), 0, stream, s);
+        const dim3 grid(tiles_of(j.n_out, kSlopeCols), plan.slope_blocks);
+        const bool slope = j.act != kActNone;
+        if (j.out_type == TYPE && slope) hipLaunchKernelGGL((slope_kernel<TYPE, TYPE, true>), grid, dim3(kBlock), 0, stream, s);
+        else if (j.out_type == TYPE) hipLaunchKernelGGL((slope_kernel<TYPE, TYPE, false>), grid, dim3(kBlock), 0, stream, s);
+        else if (slope) hipLaunchKernelGGL((slope_kernel<kF32, TYPE, true>), grid, dim3(kBlock), 0, stream, s);
+        else hipLaunchKernelGGL((slope_kernel<kF32, TYPE, false>), grid, dim3(kBlock), 0, stream, s);
         e = hipGetLastError();
     }
     if (e == hipSuccess && j.dx && j.rows.host > 0) {
@@ -615,7 +643,7 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         p.rows = j.rows;
         p.slices = plan.slices;
         p.out = PlainOut<kF32>{scratch + plan.part, j.n_in, static_cast<int64_t>(j.n_out) * j.n_in};
-        e = launch_tiles<TYPE, Small, true, true>(stream, p);
+        e = plan.large ? launch_tiles<TYPE, Large, true, true>(stream, p) : launch_tiles<TYPE, Small, true, true>(stream, p);
     }
     if (e == hipSuccess && (j.dw || j.dbias)) {
         JoinArgs a{};
@@ -628,7 +656,7 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         a.out = j.dw;
         a.out_ld = j.dw_ld;
         a.type = TYPE;
-        a.cell_blocks = tiles_of(a.cells, kBlock);
+        a.cell_blocks = tiles_of(a.cells, 2 * kBlock);
         a.sums = reinterpret_cast<const float*>(scratch + plan.sums);
         a.n = j.n_out;
         a.n_sums = static_cast<int>(plan.slope_blocks);
