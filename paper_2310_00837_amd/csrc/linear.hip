@@ -170,6 +170,106 @@ struct Stage {
     }
 };
 
+// Single precision goes through the 16-bit instructions, which are sixteen times as quick: a value is cut (not rounded) into three
+// of bfloat16, x = h + m + l exactly, and of the nine products the six that matter are added, the smallest first: l h', h l', m m',
+// m h', h m', h h' (those left out are below 2^-22 of the product).  Six instructions stand for eight of single precision that take twice as
+// long each.  A stage of 32 elements of k lies in LDS as three planes of 64-byte rows.  An infinity would meet zeros in this and
+// leave NaN, so the loads watch for values that are not finite, and a tile that has met one is done again by the instructions of
+// single precision.  Values below 2^-110 lose their last bits.
+struct SplitPart {
+    bf16x8 h, m, l;
+};
+template <int WIDTH, bool STRIDED, int THREADS>
+struct SplitStage {
+    typedef Stage<kF32, WIDTH, 128, STRIDED, THREADS> Whole;
+    typedef Stage<kBF16, WIDTH, 64, STRIDED, THREADS> Plane;
+    static constexpr int kLoads = Whole::kLoads, kPlane = WIDTH * 64;
+    static __device__ __forceinline__ void load(const Operand& o, int64_t first, int64_t k0, i32x4 (&regs)[kLoads]) {
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const uint32_t q = threadIdx.x + l * THREADS, row = q / Whole::kRowChunks, chunk = q % Whole::kRowChunks;
+            const int64_t r = (STRIDED ? k0 : first) + row, c = (STRIDED ? first : k0) + chunk * 4;
+            regs[l] = i32x4{0, 0, 0, 0};
+            if (r < o.rows && c < o.cols) regs[l] = load_16_of<4>(o.data + r * o.ld + c * 4, o.cols - c);
+        }
+    }
+    // the same for rows of whole chunks at 16-byte addresses (see Stage::source)
+    struct Source {
+        const char* at[kLoads];
+    };
+    static __device__ __forceinline__ Source source(const Operand& o, int64_t first) {
+        Source s;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const uint32_t q = threadIdx.x + l * THREADS, row = q / Whole::kRowChunks, chunk = q % Whole::kRowChunks;
+            if (STRIDED) {
+                const int64_t c = first + chunk * 4, last = o.cols - 4;
+                s.at[l] = o.data + row * o.ld + (c < last ? c : last) * 4;
+            } else {
+                const int64_t r = first + row, last = o.rows - 1;
+                s.at[l] = o.data + (r < last ? r : last) * o.ld + chunk * 16;
+            }
+        }
+        return s;
+    }
+    static __device__ __forceinline__ void load(const Operand& o, const Source& s, int64_t k0, i32x4 (&regs)[kLoads]) {
+        const int64_t step = STRIDED ? k0 * o.ld : k0 * 4, left = (STRIDED ? o.rows : o.cols) - k0;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const uint32_t q = threadIdx.x + l * THREADS, row = q / Whole::kRowChunks, chunk = q % Whole::kRowChunks;
+            const char* at = s.at[l] + step;
+            if (left < Whole::kK && static_cast<int64_t>(STRIDED ? row : chunk * 4) >= left) at = reinterpret_cast<const char*>(&kZeroChunk);
+            regs[l] = *reinterpret_cast<const i32x4*>(at);
+        }
+    }
+    // spoilt: 0, until a value is not finite
+    static __device__ __forceinline__ void put(char* lds, const i32x4 (&regs)[kLoads], float* spoilt) {
+        typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const uint32_t q = threadIdx.x + l * THREADS, row = q / Whole::kRowChunks, chunk = q % Whole::kRowChunks;
+            uint32_t part[3][4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t bits = static_cast<uint32_t>(regs[l][e]);
+                const float x = __builtin_bit_cast(float, bits);
+                *spoilt = __builtin_fmaf(x, 0.0f, *spoilt);
+                part[0][e] = bits & 0xffff0000u;
+                const float rest = x - __builtin_bit_cast(float, part[0][e]);
+                part[1][e] = __builtin_bit_cast(uint32_t, rest) & 0xffff0000u;
+                part[2][e] = __builtin_bit_cast(uint32_t, rest - __builtin_bit_cast(float, part[1][e]));
+            }
+            const uint32_t to = STRIDED ? row * (WIDTH * 2) + (((chunk >> 1) ^ Plane::swizzle(row)) << 4) + (chunk & 1) * 8
+                                        : row * 64 + (((chunk >> 1) ^ Plane::swizzle(row)) << 4) + (chunk & 1) * 8;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                i32x2 v;
+                v.x = static_cast<int32_t>(__builtin_amdgcn_perm(part[k][1], part[k][0], 0x07060302));
+                v.y = static_cast<int32_t>(__builtin_amdgcn_perm(part[k][3], part[k][2], 0x07060302));
+                *reinterpret_cast<i32x2*>(lds + k * kPlane + to) = v;
+            }
+        }
+    }
+    typedef SplitPart Part;
+    static __device__ __forceinline__ Part fragment(const char* lds, int at) {
+        return Part{__builtin_bit_cast(bf16x8, Plane::fragment(lds, at, 0)), __builtin_bit_cast(bf16x8, Plane::fragment(lds + kPlane, at, 0)),
+                    __builtin_bit_cast(bf16x8, Plane::fragment(lds + 2 * kPlane, at, 0))};
+    }
+};
+// (the six products one after the other for all tiles of a wave, so that an instruction seldom waits for the one before it)
+template <int TM, int TN>
+__device__ __forceinline__ void split_mma(const SplitPart (&a)[TM], const SplitPart (&b)[TN], f32x4 (&c)[TM][TN]) {
+#pragma unroll
+    for (int k = 0; k < 6; ++k)
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const bf16x8 x = k == 0 ? a[i].l : k == 2 || k == 3 ? a[i].m : a[i].h, y = k == 1 ? b[j].l : k == 2 || k == 4 ? b[j].m : b[j].h;
+                c[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x, c[i][j], 0, 0, 0);
+            }
+}
+
 // The epilogues.  A thread has eight neighbouring columns, `valid` of them in the matrix, and goes through rows: at() takes what
 // belongs to the columns, row() finishes and writes the sums of one row.  The type written and whether the activation needs an
 // exponential are the kernel's: a round through a row is a chain that few waves have to bear, and with all types and activations
@@ -264,11 +364,12 @@ struct Tile {
 template <int TYPE, class TILE, bool A_STRIDED, bool B_STRIDED, bool DIRECT, class OUT>
 __global__ __launch_bounds__(TILE::kThreads) void product_kernel(ProductArgs<OUT> p) {
     constexpr int BM = TILE::kM, BN = TILE::kN, WAVES_M = TILE::kWavesM, WAVES_N = TILE::kWavesN, ROW = TILE::kRow, kThreads = TILE::kThreads;
-    constexpr int kStages = DIRECT ? TILE::kStages : 2;
+    constexpr int kStages = DIRECT && TYPE != kF32 ? TILE::kStages : 2;
     constexpr int kTm = BM / WAVES_M / 16, kTn = BN / WAVES_N / 16;      // 16 x 16 tiles of a wave
     typedef Stage<TYPE, BM, ROW, A_STRIDED, kThreads> StageA;
     typedef Stage<TYPE, BN, ROW, B_STRIDED, kThreads> StageB;
-    constexpr int kStage = (BM + BN) * ROW;
+    constexpr bool kSplit = TYPE == kF32;
+    constexpr int kStage = (BM + BN) * (kSplit ? 192 : ROW);
     constexpr int kOutLd = BN + 4;
     constexpr int kOutBytes = WAVES_M * 16 * kOutLd * 4;                 // of the sums of one row of tiles of every wave
     constexpr int kOutTiles = kTm * kOutBytes <= kStages * kStage + 4096 ? kTm : kTm % 2 == 0 && kTm / 2 * kOutBytes <= kStages * kStage ? kTm / 2 : 1;
@@ -293,11 +394,13 @@ __global__ __launch_bounds__(TILE::kThreads) void product_kernel(ProductArgs<OUT
         if (m0 >= m_end || slice >= p.slices) continue;
         const int64_t step0 = slice * per, step1 = step0 + per < steps_all ? step0 + per : steps_all;
         f32x4 acc[kTm][kTn];
-    #pragma unroll
-        for (int i = 0; i < kTm; ++i)
-    #pragma unroll
-            for (int j = 0; j < kTn; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-
+        const auto clear = [&] {
+#pragma unroll
+            for (int i = 0; i < kTm; ++i)
+#pragma unroll
+                for (int j = 0; j < kTn; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+        };
+        clear();
         const auto multiply = [&](const char* stage) {
 #pragma unroll
             for (int half = 0; half < ROW / 64; ++half) {
@@ -314,7 +417,7 @@ __global__ __launch_bounds__(TILE::kThreads) void product_kernel(ProductArgs<OUT
         };
         // One barrier a step: what it waits for is the step's loads (those of the stages ahead stay in flight) and every wave's reads of
         // the stage before, which the next loads go to.
-        if constexpr (DIRECT) {
+        if constexpr (DIRECT && !kSplit) {
             const typename StageA::Source sa = StageA::source(p.a, m0);
             const typename StageB::Source sb = StageB::source(p.b, n0);
             constexpr int kAhead = (kStages - 2) * (StageA::kLoads + StageB::kLoads);
@@ -336,22 +439,65 @@ __global__ __launch_bounds__(TILE::kThreads) void product_kernel(ProductArgs<OUT
                 stage = stage + 1 < kStages ? stage + 1 : 0;
             }
         } else {
-            i32x4 ra[StageA::kLoads], rb[StageB::kLoads];
-            if (step0 < step1) {
-                StageA::load(p.a, m0, step0 * StageA::kK, ra);
-                StageB::load(p.b, n0, step0 * StageA::kK, rb);
-            }
-            for (int64_t step = step0; step < step1; ++step) {
-                char* stage = lds + ((step - step0) & 1) * kStage;
-                StageA::put(stage, ra);
-                StageB::put(stage + BM * ROW, rb);
-                __syncthreads();
-                if (step + 1 < step1) {
-                    StageA::load(p.a, m0, (step + 1) * StageA::kK, ra);
-                    StageB::load(p.b, n0, (step + 1) * StageA::kK, rb);
+            const auto by_registers = [&] {
+                i32x4 ra[StageA::kLoads], rb[StageB::kLoads];
+                if (step0 < step1) {
+                    StageA::load(p.a, m0, step0 * StageA::kK, ra);
+                    StageB::load(p.b, n0, step0 * StageA::kK, rb);
                 }
-                multiply(stage);
-            }
+                for (int64_t step = step0; step < step1; ++step) {
+                    char* stage = lds + ((step - step0) & 1) * kStage;
+                    StageA::put(stage, ra);
+                    StageB::put(stage + BM * ROW, rb);
+                    __syncthreads();
+                    if (step + 1 < step1) {
+                        StageA::load(p.a, m0, (step + 1) * StageA::kK, ra);
+                        StageB::load(p.b, n0, (step + 1) * StageA::kK, rb);
+                    }
+                    multiply(stage);
+                }
+            };
+            if constexpr (kSplit) {
+                typedef SplitStage<BM, A_STRIDED, kThreads> SplitA;
+                typedef SplitStage<BN, B_STRIDED, kThreads> SplitB;
+                typename SplitA::Source sa;
+                typename SplitB::Source sb;
+                if constexpr (DIRECT) sa = SplitA::source(p.a, m0), sb = SplitB::source(p.b, n0);
+                i32x4 ra[SplitA::kLoads], rb[SplitB::kLoads];
+                float spoilt = 0.0f;
+                const auto load = [&](int64_t step) {
+                    if constexpr (DIRECT) {
+                        SplitA::load(p.a, sa, step * StageA::kK, ra);
+                        SplitB::load(p.b, sb, step * StageA::kK, rb);
+                    } else {
+                        SplitA::load(p.a, m0, step * StageA::kK, ra);
+                        SplitB::load(p.b, n0, step * StageA::kK, rb);
+                    }
+                };
+                const auto put = [&](int64_t step) {
+                    char* stage = lds + ((step - step0) & 1) * kStage;
+                    SplitA::put(stage, ra, &spoilt);
+                    SplitB::put(stage + 3 * SplitA::kPlane, rb, &spoilt);
+                };
+                if (step0 < step1) load(step0), put(step0);
+                if (step0 + 1 < step1) load(step0 + 1);
+                for (int64_t step = step0; step < step1; ++step) {
+                    const char* stage = lds + ((step - step0) & 1) * kStage;
+                    __syncthreads();
+                    SplitPart fa[kTm], fb[kTn];
+#pragma unroll
+                    for (int i = 0; i < kTm; ++i) fa[i] = SplitA::fragment(stage, (wave_m * kTm + i) * 16);
+#pragma unroll
+                    for (int j = 0; j < kTn; ++j) fb[j] = SplitB::fragment(stage + 3 * SplitA::kPlane, (wave_n * kTn + j) * 16);
+                    split_mma(fa, fb, acc);
+                    if (step + 1 < step1) put(step + 1);             // (beside the products: into the stage that was read a step ago)
+                    if (step + 2 < step1) load(step + 2);
+                }
+                if (__syncthreads_or(spoilt != 0.0f)) {
+                    clear();
+                    by_registers();
+                }
+            } else by_registers();
         }
         __syncthreads();
         // The sums go through LDS, so that the epilogue reads and writes whole rows; kOutTiles of every wave's rows of tiles at a time.
