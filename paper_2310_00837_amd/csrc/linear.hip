@@ -361,21 +361,28 @@ struct Tile {
     static constexpr int kThreads = WAVES_M * WAVES_N * kWave;
 };
 
+// LDS of a product: the stages, and after them the sums on their way out.
+template <int TYPE, class TILE, bool DIRECT>
+struct ProductLds {
+    static constexpr int kTm = TILE::kM / TILE::kWavesM / 16, kTn = TILE::kN / TILE::kWavesN / 16;      // 16 x 16 tiles of a wave
+    static constexpr int kStages = DIRECT && TYPE != kF32 ? TILE::kStages : 2;
+    static constexpr int kStage = (TILE::kM + TILE::kN) * (TYPE == kF32 ? 192 : TILE::kRow);
+    static constexpr int kOutLd = TILE::kN + 4;
+    static constexpr int kOutBytes = TILE::kWavesM * 16 * kOutLd * 4;    // of the sums of one row of tiles of every wave
+    static constexpr int kOutTiles = kTm * kOutBytes <= kStages * kStage + 4096 ? kTm : kTm % 2 == 0 && kTm / 2 * kOutBytes <= kStages * kStage ? kTm / 2 : 1;
+    static constexpr int kBytes = kStages * kStage > kOutTiles * kOutBytes ? kStages * kStage : kOutTiles * kOutBytes;
+    static_assert(kTm % kOutTiles == 0, "the epilogue takes as many rows of tiles at a time");
+};
+
+// The tiles block, block + blocks, ... of a product.
 template <int TYPE, class TILE, bool A_STRIDED, bool B_STRIDED, bool DIRECT, class OUT>
-__global__ __launch_bounds__(TILE::kThreads) void product_kernel(ProductArgs<OUT> p) {
+__device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint32_t blocks, char* lds) {
     constexpr int BM = TILE::kM, BN = TILE::kN, WAVES_M = TILE::kWavesM, WAVES_N = TILE::kWavesN, ROW = TILE::kRow, kThreads = TILE::kThreads;
-    constexpr int kStages = DIRECT && TYPE != kF32 ? TILE::kStages : 2;
-    constexpr int kTm = BM / WAVES_M / 16, kTn = BN / WAVES_N / 16;      // 16 x 16 tiles of a wave
+    typedef ProductLds<TYPE, TILE, DIRECT> Lds;
+    constexpr int kTm = Lds::kTm, kTn = Lds::kTn, kStages = Lds::kStages, kStage = Lds::kStage, kOutLd = Lds::kOutLd, kOutTiles = Lds::kOutTiles;
+    constexpr bool kSplit = TYPE == kF32;
     typedef Stage<TYPE, BM, ROW, A_STRIDED, kThreads> StageA;
     typedef Stage<TYPE, BN, ROW, B_STRIDED, kThreads> StageB;
-    constexpr bool kSplit = TYPE == kF32;
-    constexpr int kStage = (BM + BN) * (kSplit ? 192 : ROW);
-    constexpr int kOutLd = BN + 4;
-    constexpr int kOutBytes = WAVES_M * 16 * kOutLd * 4;                 // of the sums of one row of tiles of every wave
-    constexpr int kOutTiles = kTm * kOutBytes <= kStages * kStage + 4096 ? kTm : kTm % 2 == 0 && kTm / 2 * kOutBytes <= kStages * kStage ? kTm / 2 : 1;
-    constexpr int kLds = kStages * kStage > kOutTiles * kOutBytes ? kStages * kStage : kOutTiles * kOutBytes;
-    static_assert(kOutTiles >= 1 && kTm % kOutTiles == 0, "the epilogue takes as many rows of tiles at a time");
-    __shared__ __align__(16) char lds[kLds];
 
     const int64_t count = p.rows.get();
     const bool rows_are_k = A_STRIDED;
@@ -385,7 +392,7 @@ __global__ __launch_bounds__(TILE::kThreads) void product_kernel(ProductArgs<OUT
     const int64_t steps_all = (k_end + StageA::kK - 1) / StageA::kK, per = (steps_all + p.slices - 1) / p.slices;
 
     const int wave = threadIdx.x / kWave, wave_m = wave / WAVES_N, wave_n = wave % WAVES_N;
-    for (uint32_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {      // (once round, but for the longest lists)
+    for (uint32_t tile = block; tile < p.tiles; tile += blocks) {      // (once round, but for the longest lists)
         uint32_t group, member;
         tile_of(tile, p.members, &group, &member);
         const int slice = rows_are_k ? static_cast<int>(group) : 0;
@@ -531,6 +538,20 @@ __global__ __launch_bounds__(TILE::kThreads) void product_kernel(ProductArgs<OUT
     }
 }
 
+template <int TYPE, class TILE, bool DIRECT, class OUT>
+__global__ __launch_bounds__(TILE::kThreads) void forward_kernel(ProductArgs<OUT> p) {
+    __shared__ __align__(16) char lds[ProductLds<TYPE, TILE, DIRECT>::kBytes];
+    product<TYPE, TILE, false, false, DIRECT>(p, blockIdx.x, gridDim.x, lds);
+}
+
+// Both products of the gradient in one launch, each with workgroups of its own: dw's tiles come first, since each takes longest.
+template <int TYPE, class TILE, bool DIRECT>
+__global__ __launch_bounds__(TILE::kThreads) void backward_kernel(ProductArgs<PlainOut<kF32>> dw, uint32_t dw_blocks, ProductArgs<PlainOut<TYPE>> dx) {
+    __shared__ __align__(16) char lds[ProductLds<TYPE, TILE, DIRECT>::kBytes];
+    if (blockIdx.x < dw_blocks) product<TYPE, TILE, true, true, DIRECT>(dw, blockIdx.x, dw_blocks, lds);
+    else product<TYPE, TILE, false, true, DIRECT>(dx, blockIdx.x - dw_blocks, gridDim.x - dw_blocks, lds);
+}
+
 // Few rows: a workgroup has 16 rows of x and 16 of w, its waves share k between them and read both straight into the
 // operands of the MFMA, and the eight sums of every element meet in LDS.
 constexpr int kFewWaves = 8;
@@ -579,8 +600,7 @@ __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(ProductAr
 
 // dz = dy * act'(pre), rounded to the type the products work in, and the sums of dz's columns (from the values before
 // they are rounded) over the rows of a workgroup.
-constexpr int kSlopeCols = 16 * 8;                // columns of a workgroup: 16 lanes, 8 each
-constexpr int kSlopeRows = 2;                     // rows that a thread has in flight; 16 threads go through a workgroup's rows
+constexpr int kSlopeRows = 2;                     // rows that a thread has in flight
 struct SlopeArgs {
     Count rows;
     int32_t n;
@@ -593,41 +613,43 @@ struct SlopeArgs {
     int64_t dz_ld;
     float* sums;                                  // [gridDim.y][n], nullable
 };
-template <int TYPE, int Z_TYPE, bool SLOPE>
+// (LANES threads share a row of the workgroup's columns, eight each; the others go through the rows)
+template <int TYPE, int Z_TYPE, bool SLOPE, int LANES>
 __global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
-    __shared__ float s[16][kSlopeCols + 4];
+    constexpr int kSubs = kBlock / LANES, kCols = LANES * 8;
+    __shared__ float s[kSubs][kCols + 4];
     const int64_t count = p.rows.get(), per = (count + gridDim.y - 1) / gridDim.y;
     const int64_t row0 = blockIdx.y * per, row1 = row0 + per < count ? row0 + per : count;
-    const int lane = threadIdx.x % 16, sub = threadIdx.x / 16, col = blockIdx.x * kSlopeCols + lane * 8;
+    const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES, col = blockIdx.x * kCols + lane * 8;
     const int valid = p.n - col < 8 ? p.n - col : 8;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (valid > 0)
-        for (int64_t row = row0 + sub; row < row1; row += 16 * kSlopeRows) {
+        for (int64_t row = row0 + sub; row < row1; row += kSubs * kSlopeRows) {
             float d[kSlopeRows][8], z[kSlopeRows][8];
 #pragma unroll
             for (int k = 0; k < kSlopeRows; ++k) {
-                const int64_t r = row + 16 * k < row1 ? row + 16 * k : row;            // (a row that there is; its values are dropped below)
+                const int64_t r = row + kSubs * k < row1 ? row + kSubs * k : row;            // (a row that there is; its values are dropped below)
                 load_8_of<TYPE>(p.dy, r * p.dy_ld + col, valid, d[k]);
                 if (SLOPE) load_8_of<TYPE>(p.pre, r * p.pre_ld + col, valid, z[k]);
             }
 #pragma unroll
             for (int k = 0; k < kSlopeRows; ++k) {
-                if (row + 16 * k >= row1) continue;
+                if (row + kSubs * k >= row1) continue;
                 if (SLOPE) scale_by_slope_8(p.act, z[k], d[k]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += d[k][e];
-                if (p.dz) store_8_of<Z_TYPE>(p.dz, (row + 16 * k) * p.dz_ld + col, valid, d[k]);
+                if (p.dz) store_8_of<Z_TYPE>(p.dz, (row + kSubs * k) * p.dz_ld + col, valid, d[k]);
             }
         }
     if (!p.sums) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[sub][lane * 8 + e] = sum[e];
     __syncthreads();
-    if (threadIdx.x < kSlopeCols && blockIdx.x * kSlopeCols + threadIdx.x < static_cast<uint32_t>(p.n)) {
+    if (threadIdx.x < kCols && blockIdx.x * kCols + threadIdx.x < static_cast<uint32_t>(p.n)) {
         float t = 0;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) t += s[k][threadIdx.x];
-        p.sums[static_cast<int64_t>(blockIdx.y) * p.n + blockIdx.x * kSlopeCols + threadIdx.x] = t;
+#pragma unroll 16
+        for (int k = 0; k < kSubs; ++k) t += s[k][threadIdx.x];
+        p.sums[static_cast<int64_t>(blockIdx.y) * p.n + blockIdx.x * kCols + threadIdx.x] = t;
     }
 }
 
@@ -640,6 +662,7 @@ struct JoinArgs {
     void* out;
     int64_t out_ld;
     int type;
+    int subs;                                     // threads that share four cells, each with every subs-th slice
     uint32_t cell_blocks;                         // workgroups of this sum; the others have 16 columns each
     const float* sums;
     int32_t n;
@@ -651,20 +674,21 @@ __global__ __launch_bounds__(kBlock) void join_kernel(JoinArgs p) {
         sum_columns(p.sums, p.n_sums, p.n, (blockIdx.x - p.cell_blocks) * kSumColumns, p.sum_out, p.sum_type);
         return;
     }
-    const int64_t c = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * 2;
-    if (c >= p.cells) return;
-    typedef float f32x2 __attribute__((ext_vector_type(2), aligned(4)));
-    const bool pair = c + 1 < p.cells;
-    float a = 0, b = 0;
+    __shared__ f32x4 s_sum[kBlock];
+    const int lanes = kBlock / p.subs, lane = threadIdx.x % lanes, sub = threadIdx.x / lanes;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x) * lanes + lane) * 4;
+    f32x4 t = {0, 0, 0, 0};
+    if (c < p.cells) {
 #pragma unroll 8
-    for (int s = 0; s < p.slices; ++s) {
-        const float* from = p.part + s * p.cells + c;
-        const f32x2 v = pair ? *reinterpret_cast<const f32x2*>(from) : f32x2{*from, 0.0f};
-        a += v.x;
-        b += v.y;
+        for (int s = sub; s < p.slices; s += p.subs) t += __builtin_bit_cast(f32x4, load_16_of<4>(p.part + s * p.cells + c, p.cells - c));
     }
-    store_1(p.type, p.out, c / p.cols * p.out_ld + c % p.cols, a);
-    if (pair) store_1(p.type, p.out, (c + 1) / p.cols * p.out_ld + (c + 1) % p.cols, b);
+    s_sum[threadIdx.x] = t;
+    __syncthreads();
+    if (sub > 0) return;
+    for (int k = 1; k < p.subs; ++k) t += s_sum[k * lanes + lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < p.cells) store_1(p.type, p.out, (c + e) / p.cols * p.out_ld + (c + e) % p.cols, t[e]);
 }
 
 Operand operand(const void* data, int64_t ld, int type, int64_t rows, int64_t cols) {
@@ -679,18 +703,48 @@ bool direct(const Operand& o, int bytes) {
     return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % 16 == 0 && o.cols * bytes % 16 == 0;
 }
 
-template <int TYPE, class TILE, bool AS, bool BS, class OUT>
-hipError_t launch_tiles(hipStream_t stream, ProductArgs<OUT> p) {
-    p.tiles_n = tiles_of(p.n, TILE::kN);
-    const int64_t tiles_m = tiles_of(p.m, TILE::kM), members = AS ? tiles_m * p.tiles_n : p.tiles_n, groups = AS ? p.slices : tiles_m;
+// The tiles of a product (by_slices: k runs over rows and is cut up) and the workgroups for them; false if there are too many.
+template <class TILE, class OUT>
+bool lay_out(ProductArgs<OUT>* p, bool by_slices, uint32_t* blocks) {
+    p->tiles_n = tiles_of(p->n, TILE::kN);
+    const int64_t tiles_m = tiles_of(p->m, TILE::kM), members = by_slices ? tiles_m * p->tiles_n : p->tiles_n, groups = by_slices ? p->slices : tiles_m;
     const int64_t tiles = (groups + 7) / 8 * 8 * members;
-    if (tiles >= 1ll << 32) return hipErrorInvalidValue;
-    p.members = static_cast<uint32_t>(members);
-    p.tiles = static_cast<uint32_t>(tiles);
-    const dim3 grid(std::min(p.tiles, kMostBlocks));
+    p->members = static_cast<uint32_t>(members);
+    p->tiles = static_cast<uint32_t>(tiles);
+    *blocks = static_cast<uint32_t>(std::min<int64_t>(tiles, kMostBlocks));
+    return tiles < 1ll << 32;
+}
+
+template <int TYPE, class TILE, class OUT>
+hipError_t launch_forward(hipStream_t stream, ProductArgs<OUT> p) {
+    uint32_t blocks = 0;
+    if (!lay_out<TILE>(&p, false, &blocks)) return hipErrorInvalidValue;
     if (direct(p.a, type_bytes(TYPE)) && direct(p.b, type_bytes(TYPE)))
-        hipLaunchKernelGGL((product_kernel<TYPE, TILE, AS, BS, true, OUT>), grid, dim3(TILE::kThreads), 0, stream, p);
-    else hipLaunchKernelGGL((product_kernel<TYPE, TILE, AS, BS, false, OUT>), grid, dim3(TILE::kThreads), 0, stream, p);
+        hipLaunchKernelGGL((forward_kernel<TYPE, TILE, true, OUT>), dim3(blocks), dim3(TILE::kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((forward_kernel<TYPE, TILE, false, OUT>), dim3(blocks), dim3(TILE::kThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+// dw and dx: nullptr if not asked for
+template <int TYPE, class TILE>
+hipError_t launch_backward(hipStream_t stream, ProductArgs<PlainOut<kF32>>* dw, ProductArgs<PlainOut<TYPE>>* dx) {
+    ProductArgs<PlainOut<kF32>> w{};
+    ProductArgs<PlainOut<TYPE>> x{};
+    uint32_t dw_blocks = 0, dx_blocks = 0;
+    bool straight = true;
+    if (dw) {
+        if (!lay_out<TILE>(dw, true, &dw_blocks)) return hipErrorInvalidValue;
+        straight = straight && direct(dw->a, type_bytes(TYPE)) && direct(dw->b, type_bytes(TYPE));
+        w = *dw;
+    }
+    if (dx) {
+        if (!lay_out<TILE>(dx, false, &dx_blocks)) return hipErrorInvalidValue;
+        straight = straight && direct(dx->a, type_bytes(TYPE)) && direct(dx->b, type_bytes(TYPE));
+        x = *dx;
+    }
+    const dim3 grid(dw_blocks + dx_blocks);
+    if (straight) hipLaunchKernelGGL((backward_kernel<TYPE, TILE, true>), grid, dim3(TILE::kThreads), 0, stream, w, dw_blocks, x);
+    else hipLaunchKernelGGL((backward_kernel<TYPE, TILE, false>), grid, dim3(TILE::kThreads), 0, stream, w, dw_blocks, x);
     return hipGetLastError();
 }
 
@@ -714,8 +768,8 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
         hipLaunchKernelGGL((product_few_kernel<TYPE, Out>), grid, dim3(kFewWaves * kWave), 0, stream, p);
         return hipGetLastError();
     }
-    if (static_cast<int64_t>(tiles_of(p.m, 128)) * tiles_of(p.n, 128) >= 256) return launch_tiles<TYPE, Large, false, false>(stream, p);
-    return launch_tiles<TYPE, Small, false, false>(stream, p);
+    if (static_cast<int64_t>(tiles_of(p.m, 128)) * tiles_of(p.n, 128) >= 256) return launch_forward<TYPE, Large>(stream, p);
+    return launch_forward<TYPE, Small>(stream, p);
 }
 template <int TYPE, int OUT_TYPE>
 hipError_t forward(hipStream_t stream, const LinearJob& j) {
@@ -723,7 +777,7 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
 }
 
 struct GradPlan {                                 // of linear_grad: what lies where in the scratch, and how far k is cut up
-    bool needs_dz, large;                         // large: dw by large tiles
+    bool needs_dz, large;                         // large: by large tiles
     int64_t dz_ld;
     int slices;                                   // of dw's k
     unsigned slope_blocks;                        // workgroups along the rows of the slope kernel
@@ -733,14 +787,20 @@ struct GradPlan {                                 // of linear_grad: what lies w
         const int64_t n = j.rows.host;
         needs_dz = (j.dx || j.dw) && (j.act != kActNone || j.out_type != j.x_type);
         dz_ld = (j.n_out + 7) / 8 * 8;
-        // dw's k, the rows, is cut so that there are about 1024 small tiles or 512 large ones, in eights (one for each XCD) of at least
-        // four steps.  us, 26 624 x 512 x 256 in bfloat16: small tiles 16 slices 21.7, 32 17.4; large ones 32 20.5, 64 19.3;
-        // 50 000 x 2048 x 512: large ones 4 slices 223, 8 141, 16 150.
-        const auto tiles = [&](int64_t edge) { return (j.n_out + edge - 1) / edge * ((j.n_in + edge - 1) / edge); };
+        // dw's k, the rows, is cut so that there are about 1024 small tiles or 256 large ones, in eights (one for each XCD) of at least
+        // four steps.  us, dw of 26 624 x 512 x 256 in bfloat16: small tiles 16 slices 21.7, 32 17.4; large ones 32 20.5, 64 19.3;
+        // 50 000 x 2048 x 512: large ones 4 slices 223, 8 141, 16 150.  Large tiles where there are enough of them for the CUs (in single
+        // precision, where a tile takes longest, for half of them), us by small / large: 5000 x 256 x 256 in bfloat16 16.4 / 18.9, in
+        // single precision 32.2 / 29.5; 26 624 x 512 x 256 50.1 / 44.9; 50 000 x 2048 x 512 598 / 333.
+        const auto tiles = [](int64_t m, int64_t n, int64_t edge) { return (m + edge - 1) / edge * ((n + edge - 1) / edge); };
         const int64_t steps = (n * type_bytes(j.x_type) + Large::kRow - 1) / Large::kRow;
-        large = tiles(128) >= 64;
-        const int64_t want = std::max<int64_t>(1, std::min((large ? 512 : 1024) / std::max<int64_t>(tiles(large ? 128 : 64), 1), steps / 4));
-        slices = static_cast<int>(want >= 8 ? want / 8 * 8 : want);
+        const auto cut = [&](int64_t edge, int64_t most) {
+            const int64_t want = std::max<int64_t>(1, std::min(std::max<int64_t>(most / tiles(j.n_out, j.n_in, edge), 8), steps / 4));
+            return static_cast<int>(want >= 8 ? want / 8 * 8 : want);
+        };
+        slices = cut(128, 256);
+        large = (j.dx ? tiles(n, j.n_in, 128) : 0) + (j.dw ? tiles(j.n_out, j.n_in, 128) * slices : 0) >= (j.x_type == kF32 ? 128 : 256);
+        if (!large) slices = cut(64, 1024);
         slope_blocks = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((n + 31) / 32, 512)));
         dz = 0;
         part = dz + (needs_dz ? up(static_cast<size_t>(n * dz_ld) * type_bytes(j.x_type)) : 0);
@@ -748,6 +808,17 @@ struct GradPlan {                                 // of linear_grad: what lies w
         bytes = sums + (j.dbias ? up(static_cast<size_t>(slope_blocks) * j.n_out * sizeof(float)) : 0);
     }
 };
+
+template <int TYPE, int LANES>
+hipError_t launch_slope(hipStream_t stream, const SlopeArgs& s, const LinearGradJob& j, unsigned blocks) {
+    const dim3 grid(tiles_of(j.n_out, LANES * 8), blocks), block(kBlock);
+    const bool slope = j.act != kActNone;
+    if (j.out_type == TYPE && slope) hipLaunchKernelGGL((slope_kernel<TYPE, TYPE, true, LANES>), grid, block, 0, stream, s);
+    else if (j.out_type == TYPE) hipLaunchKernelGGL((slope_kernel<TYPE, TYPE, false, LANES>), grid, block, 0, stream, s);
+    else if (slope) hipLaunchKernelGGL((slope_kernel<kF32, TYPE, true, LANES>), grid, block, 0, stream, s);
+    else hipLaunchKernelGGL((slope_kernel<kF32, TYPE, false, LANES>), grid, block, 0, stream, s);
+    return hipGetLastError();
+}
 
 template <int TYPE>
 hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
@@ -758,38 +829,30 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
     if (plan.needs_dz || j.dbias) {
         SlopeArgs s{j.rows, j.n_out, j.act, j.dy, j.dy_ld, j.pre, j.pre_ld, plan.needs_dz ? scratch + plan.dz : nullptr, plan.dz_ld,
                     j.dbias ? reinterpret_cast<float*>(scratch + plan.sums) : nullptr};
-        const dim3 grid(tiles_of(j.n_out, kSlopeCols), plan.slope_blocks);
-        const bool slope = j.act != kActNone;
-        if (j.out_type == TYPE && slope) hipLaunchKernelGGL((slope_kernel<TYPE, TYPE, true>), grid, dim3(kBlock), 0, stream, s);
-        else if (j.out_type == TYPE) hipLaunchKernelGGL((slope_kernel<TYPE, TYPE, false>), grid, dim3(kBlock), 0, stream, s);
-        else if (slope) hipLaunchKernelGGL((slope_kernel<kF32, TYPE, true>), grid, dim3(kBlock), 0, stream, s);
-        else hipLaunchKernelGGL((slope_kernel<kF32, TYPE, false>), grid, dim3(kBlock), 0, stream, s);
-        e = hipGetLastError();
+        e = j.n_out <= 32 ? launch_slope<TYPE, 4>(stream, s, j, plan.slope_blocks) : launch_slope<TYPE, 16>(stream, s, j, plan.slope_blocks);
     }
-    if (e == hipSuccess && j.dx && j.rows.host > 0) {
-        ProductArgs<PlainOut<TYPE>> p{};
-        p.a = operand(dz, dz_ld, TYPE, j.rows.host, j.n_out);
-        p.b = operand(j.w, j.w_ld, TYPE, j.n_out, j.n_in);
-        p.m = j.rows.host;
-        p.n = j.n_in;
-        p.k = j.n_out;
-        p.rows = j.rows;
-        p.slices = 1;
-        p.out = PlainOut<TYPE>{j.dx, j.dx_ld, 0};
-        if (static_cast<int64_t>(tiles_of(p.m, 128)) * tiles_of(p.n, 128) >= 256) e = launch_tiles<TYPE, Large, false, true>(stream, p);
-        else e = launch_tiles<TYPE, Small, false, true>(stream, p);
-    }
-    if (e == hipSuccess && j.dw) {
-        ProductArgs<PlainOut<kF32>> p{};
-        p.a = operand(dz, dz_ld, TYPE, j.rows.host, j.n_out);
-        p.b = operand(j.x, j.x_ld, TYPE, j.rows.host, j.n_in);
-        p.m = j.n_out;
-        p.n = j.n_in;
-        p.k = j.rows.host;
-        p.rows = j.rows;
-        p.slices = plan.slices;
-        p.out = PlainOut<kF32>{scratch + plan.part, j.n_in, static_cast<int64_t>(j.n_out) * j.n_in};
-        e = plan.large ? launch_tiles<TYPE, Large, true, true>(stream, p) : launch_tiles<TYPE, Small, true, true>(stream, p);
+    const bool has_dx = j.dx && j.rows.host > 0;
+    if (e == hipSuccess && (has_dx || j.dw)) {
+        ProductArgs<PlainOut<TYPE>> x{};
+        x.a = operand(dz, dz_ld, TYPE, j.rows.host, j.n_out);
+        x.b = operand(j.w, j.w_ld, TYPE, j.n_out, j.n_in);
+        x.m = j.rows.host;
+        x.n = j.n_in;
+        x.k = j.n_out;
+        x.rows = j.rows;
+        x.slices = 1;
+        x.out = PlainOut<TYPE>{j.dx, j.dx_ld, 0};
+        ProductArgs<PlainOut<kF32>> w{};
+        w.a = x.a;
+        w.b = operand(j.x, j.x_ld, TYPE, j.rows.host, j.n_in);
+        w.m = j.n_out;
+        w.n = j.n_in;
+        w.k = j.rows.host;
+        w.rows = j.rows;
+        w.slices = plan.slices;
+        w.out = PlainOut<kF32>{scratch + plan.part, j.n_in, static_cast<int64_t>(j.n_out) * j.n_in};
+        e = plan.large ? launch_backward<TYPE, Large>(stream, j.dw ? &w : nullptr, has_dx ? &x : nullptr)
+                       : launch_backward<TYPE, Small>(stream, j.dw ? &w : nullptr, has_dx ? &x : nullptr);
     }
     if (e == hipSuccess && (j.dw || j.dbias)) {
         JoinArgs a{};
@@ -802,7 +865,8 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         a.out = j.dw;
         a.out_ld = j.dw_ld;
         a.type = TYPE;
-        a.cell_blocks = tiles_of(a.cells, 2 * kBlock);
+        for (a.subs = 1; a.subs < 16 && a.slices / (2 * a.subs) >= 8;) a.subs *= 2;
+        a.cell_blocks = tiles_of(a.cells, 4 * kBlock / a.subs);
         a.sums = reinterpret_cast<const float*>(scratch + plan.sums);
         a.n = j.n_out;
         a.n_sums = static_cast<int>(plan.slope_blocks);

@@ -41,6 +41,18 @@ __device__ __forceinline__ void copy_8_of(const void* from, int64_t at, void* to
     }
 }
 
+// Eight columns of a row that may be asked for in vain: zeros then.  (One branch, so that a group whose list is shorter than what is
+// asked for together does not go through the elements one by one.)
+template <int TYPE>
+__device__ __forceinline__ void load_row_8(const void* base, int64_t at, bool wanted, int valid, float (&v)[8]) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] = 0;
+    if (wanted) {
+        if (valid >= 8) load_8<TYPE>(base, at, v);
+        else load_8_of<TYPE>(base, at, valid, v);
+    }
+}
+
 template <int TYPE, int LANES>
 __global__ __launch_bounds__(kBlock) void block_mean_kernel(MeanJob p) {
     const int64_t count = p.rows.get();
@@ -59,17 +71,17 @@ __global__ __launch_bounds__(kBlock) void block_mean_kernel(MeanJob p) {
         for (int64_t e = list.lo; e < end; e += kAhead) {
             int32_t src[kAhead];
             float v[kAhead][8];
-    #pragma unroll
-            for (int k = 0; k < kAhead; ++k) src[k] = e + k < end ? p.col[e + k] : -1;
-    #pragma unroll
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) src[k] = p.col[e + k < end ? e + k : e];
+#pragma unroll
             for (int k = 0; k < kAhead; ++k) {
-                const bool good = src[k] >= 0 && src[k] < p.n_src;
-                if (!good && e + k < end) raise(p.err, kErrData);
-                load_8_of<TYPE>(p.x, good ? static_cast<int64_t>(src[k]) * p.x_ld + col : 0, good ? valid : 0, v[k]);
+                const bool good = static_cast<uint32_t>(src[k]) < static_cast<uint64_t>(p.n_src);
+                if (!good) raise(p.err, kErrData);
+                load_row_8<TYPE>(p.x, static_cast<int64_t>(src[k]) * p.x_ld + col, e + k < end && good, valid, v[k]);
             }
-    #pragma unroll
+#pragma unroll
             for (int k = 0; k < kAhead; ++k)
-    #pragma unroll
+#pragma unroll
                 for (int c = 0; c < 8; ++c) sum[c] += v[k][c];
         }
         const float n = end > list.lo ? static_cast<float>(end - list.lo) : 1.0f;
@@ -165,19 +177,19 @@ __global__ __launch_bounds__(kBlock) void block_mean_grad_kernel(MeanGradJob p) 
             int32_t entry[kAhead];
             float v[kAhead][8], weight[kAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) entry[k] = k0 + k < hi ? p.src_entry[k0 + k] : 0;
+            for (int k = 0; k < kAhead; ++k) entry[k] = p.src_entry[k0 + k < hi ? k0 + k : k0];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 const bool own = entry[k] < 0;
                 const int64_t row = own ? ~entry[k] : entry[k];
-                const bool here = k0 + k < hi, good = here && row < p.n_rows && (!own || p.down);
-                if (here && !good) raise(p.err, kErrData);
+                const bool good = row < p.n_rows && (!own || p.down), wanted = k0 + k < hi && good;
+                if (!good) raise(p.err, kErrData);
                 weight[k] = 1.0f;
-                if (good && !own) {
+                if (wanted && !own) {
                     const RowBounds list = row_bounds(p.indptr, static_cast<uint32_t>(row));
                     weight[k] = static_cast<float>(list.hi - list.lo);
                 }
-                load_8_of<TYPE>(own ? p.down : p.dmean, good ? row * (own ? p.down_ld : p.dmean_ld) + col : 0, good ? valid : 0, v[k]);
+                load_row_8<TYPE>(own ? p.down : p.dmean, row * (own ? p.down_ld : p.dmean_ld) + col, wanted, valid, v[k]);
             }
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
