@@ -90,6 +90,7 @@ size_t norm_grad_scratch_bytes(const NormGradJob& job);
 hipError_t launch_norm_grad(hipStream_t stream, const NormGradJob& job, void* scratch);
 
 // ---- neighbours.hip
+constexpr uint32_t kLayerCounters = 512;
 struct MeanJob {
     Count rows;
     int32_t width, type;
@@ -134,6 +135,8 @@ struct MeanGradJob {
     int64_t dx_ld;
     int32_t* err;
 };
-hipError_t launch_block_mean_grad(hipStream_t stream, const MeanGradJob& job);
+// counters: uint32[kLayerCounters], zero, and left so
+size_t block_mean_grad_scratch_bytes(const MeanGradJob& job);
+hipError_t launch_block_mean_grad(hipStream_t stream, const MeanGradJob& job, uint32_t* counters, void* scratch);
 
 }  // namespace helios

@@ -65,7 +65,11 @@ int check_width(helios_ctx* c, const char* call, const char* what, int64_t width
 }
 constexpr int64_t kMaxWidth = 1 << 24;            // of a product's rows
 
-int scratch(helios_ctx* c, size_t bytes) {
+// Scratch of at least `bytes` bytes (*at), behind a line of counters that are zero between calls.
+constexpr size_t kCounterBytes = sizeof(uint32_t) * kLayerCounters;
+int scratch(helios_ctx* c, size_t bytes, char** at) {
+    bytes += kCounterBytes;
+    *at = static_cast<char*>(c->layer_scratch) + kCounterBytes;
     if (bytes <= c->layer_scratch_bytes) return HELIOS_OK;
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     HIP_TRY(c, hipStreamIsCapturing(c->stream, &capture));
@@ -74,9 +78,15 @@ int scratch(helios_ctx* c, size_t bytes) {
     void* p = nullptr;
     if (c->n_layer_outgrown >= 64) return fail(c, HELIOS_EINVAL, "scratch of %zu bytes", bytes);
     HIP_TRY(c, hipMalloc(&p, bytes));
+    const hipError_t e = hipMemsetAsync(p, 0, kCounterBytes, c->stream);
+    if (e != hipSuccess) {
+        (void)hipFree(p);
+        return fail(c, HELIOS_EHIP, "hipMemsetAsync: %s", hipGetErrorString(e));
+    }
     if (c->layer_scratch) c->layer_outgrown[c->n_layer_outgrown++] = c->layer_scratch;
     c->layer_scratch = p;
     c->layer_scratch_bytes = bytes;
+    *at = static_cast<char*>(p) + kCounterBytes;
     return HELIOS_OK;
 }
 
@@ -150,8 +160,9 @@ int helios_linear_grad(helios_ctx* c, const helios_linear_grad_args* a) {
     DeviceGuard guard(c->device);
     const LinearGradJob job{Count{a->n_rows_dev, a->n_rows}, static_cast<int32_t>(a->n_in), static_cast<int32_t>(a->n_out), a->act, a->x_type, a->out_type,
                             a->x, a->x_ld, a->w, a->w_ld, a->dy, a->dy_ld, a->pre, a->pre_ld, a->dx, a->dx_ld, a->dw, a->dw_ld, a->dbias};
-    TRY(scratch(c, linear_grad_scratch_bytes(job)));
-    HIP_TRY(c, launch_linear_grad(c->stream, job, c->layer_scratch));
+    char* at = nullptr;
+    TRY(scratch(c, linear_grad_scratch_bytes(job), &at));
+    HIP_TRY(c, launch_linear_grad(c->stream, job, at));
     return HELIOS_OK;
 }
 
@@ -206,8 +217,9 @@ int helios_rms_norm_grad(helios_ctx* c, const helios_rms_norm_grad_args* a) {
     DeviceGuard guard(c->device);
     const NormGradJob job{Count{a->n_rows_dev, a->n_rows}, static_cast<int32_t>(a->width), a->x_type, a->eps, a->total, a->total_ld, a->gain, a->inv_rms,
                           a->dy, a->dy_ld, a->dtotal, a->dtotal_ld, a->dx, a->dx_ld, a->dgain};
-    TRY(scratch(c, norm_grad_scratch_bytes(job)));
-    HIP_TRY(c, launch_norm_grad(c->stream, job, c->layer_scratch));
+    char* at = nullptr;
+    TRY(scratch(c, norm_grad_scratch_bytes(job), &at));
+    HIP_TRY(c, launch_norm_grad(c->stream, job, at));
     return HELIOS_OK;
 }
 
@@ -271,8 +283,9 @@ int helios_block_transpose(helios_ctx* c, int64_t n_rows, const int64_t* n_rows_
     TRY(check(c, m, 5, twins));
     DeviceGuard guard(c->device);
     const TransposeJob job{Count{n_rows_dev, n_rows}, indptr, col, n_col, row, n_src, src_indptr, src_entry, c->err};
-    TRY(scratch(c, block_transpose_scratch_bytes(job)));
-    HIP_TRY(c, launch_block_transpose(c->stream, job, c->layer_scratch));
+    char* at = nullptr;
+    TRY(scratch(c, block_transpose_scratch_bytes(job), &at));
+    HIP_TRY(c, launch_block_transpose(c->stream, job, at));
     return HELIOS_OK;
 }
 
@@ -299,7 +312,9 @@ int helios_block_mean_grad(helios_ctx* c, const helios_block_mean_grad_args* a) 
     DeviceGuard guard(c->device);
     const MeanGradJob job{a->n_rows, a->n_src, a->n_entries, static_cast<int32_t>(a->width), a->x_type, a->indptr, a->src_indptr, a->src_entry, a->dmean,
                           a->dmean_ld, a->down, a->down_ld, a->dx, a->dx_ld, c->err};
-    HIP_TRY(c, launch_block_mean_grad(c->stream, job));
+    char* at = nullptr;
+    TRY(scratch(c, block_mean_grad_scratch_bytes(job), &at));
+    HIP_TRY(c, launch_block_mean_grad(c->stream, job, reinterpret_cast<uint32_t*>(at - kCounterBytes), at));
     return HELIOS_OK;
 }
 

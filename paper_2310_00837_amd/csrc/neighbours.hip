@@ -22,8 +22,13 @@ hipError_t launch_hotness_order(hipStream_t stream, const int32_t* counts, int64
 
 namespace {
 
-constexpr int kAhead = 4;                         // entries of a list whose rows are asked for together
-constexpr int kLongList = 64;                     // entries from which a source is shared by a workgroup
+constexpr int kMeanAhead = 8;                     // entries of a list whose rows are asked for together
+constexpr int kAhead = 4;                         // ... in the gradient, where a list begins (most have few)
+constexpr int kPiece = 256;                       // entries of a long list that a workgroup adds up
+constexpr int kLongBlock = 256;                   // ... and its threads
+constexpr uint32_t kLines = 8, kLineWords = 32;   // of the counters
+static_assert((1 + kLines) * kLineWords <= kLayerCounters, "a context has room for as many counters");
+constexpr int kLongList = 32;                     // entries of a source that a group adds up by itself
 
 template <int TYPE>
 __device__ __forceinline__ void copy_8_of(const void* from, int64_t at, void* to, int64_t to_at, int valid) {
@@ -68,25 +73,25 @@ __global__ __launch_bounds__(kBlock) void block_mean_kernel(MeanJob p) {
         if (!fits) raise(p.err, kErrData);
         float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         const int64_t end = fits ? list.hi : list.lo;
-        for (int64_t e = list.lo; e < end; e += kAhead) {
-            int32_t src[kAhead];
-            float v[kAhead][8];
+        for (int64_t e = list.lo; e < end; e += kMeanAhead) {
+            int32_t src[kMeanAhead];
+            float v[kMeanAhead][8];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) src[k] = p.col[e + k < end ? e + k : e];
+            for (int k = 0; k < kMeanAhead; ++k) src[k] = p.col[e + k < end ? e + k : e];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
+            for (int k = 0; k < kMeanAhead; ++k) {
                 const bool good = static_cast<uint32_t>(src[k]) < static_cast<uint64_t>(p.n_src);
                 if (!good) raise(p.err, kErrData);
                 load_row_8<TYPE>(p.x, static_cast<int64_t>(src[k]) * p.x_ld + col, e + k < end && good, valid, v[k]);
             }
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k)
+            for (int k = 0; k < kMeanAhead; ++k)
 #pragma unroll
                 for (int c = 0; c < 8; ++c) sum[c] += v[k][c];
         }
-        const float n = end > list.lo ? static_cast<float>(end - list.lo) : 1.0f;
+        const float weight = 1.0f / (end > list.lo ? static_cast<float>(end - list.lo) : 1.0f);
     #pragma unroll
-        for (int c = 0; c < 8; ++c) sum[c] /= n;
+        for (int c = 0; c < 8; ++c) sum[c] *= weight;
         store_8_of<TYPE>(p.mean, row * p.mean_ld + col, valid, sum);
     }
 }
@@ -133,20 +138,24 @@ __global__ __launch_bounds__(kBlock) void transpose_keys_kernel(TransposeArgs a)
 __global__ __launch_bounds__(kBlock) void transpose_finish_kernel(TransposeArgs a) {
     const TransposeJob& p = a.job;
     const int64_t stride = static_cast<int64_t>(gridDim.x) * kBlock;
-    const auto source = [&](int64_t j) {
+    const auto source = [&](int64_t j, int32_t* place) {
         const int32_t e = a.order[j];
         const int32_t key = e >= 0 && e < a.n ? a.keys[e] : 0;
+        if (place) *place = e;
         return key > 0 && key <= p.n_src ? p.n_src - key : p.n_src;
     };
     // (whole waves go round, so that a wave can fill its lanes' gaps together)
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x - lane_id(); base <= a.n; base += stride) {
         const int64_t j = base + lane_id();
         int64_t from = 0, to = 0;                 // sources whose entries begin at j: [from, to)
+        int32_t e = -1;
+        const int64_t src = j < a.n ? source(j, &e) : p.n_src;
+        int64_t before = __shfl_up(src, 1);
+        if (lane_id() == 0) before = j > 0 ? source(j - 1, nullptr) : -1;
         if (j <= a.n) {
-            from = j > 0 ? source(j - 1) + 1 : 0;
-            const int64_t src = j < a.n ? source(j) : p.n_src;
+            from = before + 1;
             to = src + 1;
-            if (j < a.n && src < p.n_src) p.src_entry[j] = a.entry[a.order[j]];
+            if (src < p.n_src) p.src_entry[j] = a.entry[e];
         }
         for (uint64_t look = __ballot(from < to); look != 0; look &= look - 1) {
             const int lane = __ffsll(static_cast<long long>(look)) - 1;
@@ -156,82 +165,318 @@ __global__ __launch_bounds__(kBlock) void transpose_finish_kernel(TransposeArgs 
     }
 }
 
+// The same in one launch, for lists that are short enough for every workgroup to look through all of them: a workgroup has a range of
+// sources, counts what belongs to sources before it, and gathers what belongs to its own in LDS, where it is sorted by source
+// and place.  Lists that hold more for a range than LDS does are gone through again, in windows of as many places.
+constexpr int kRangeBlock = 1024, kRangeMost = 1024, kRangeHeld = 8192, kRangeSteps = 1024;
+struct RangeLds {
+    unsigned long long held[kRangeHeld];          // (source in the range, place)
+    uint32_t count[kRangeMost];                   // of a source; then where its next entry goes
+    uint32_t taken[kRangeMost], placed[kRangeBlock];
+    int32_t step[kRangeSteps + 1];                // indptr at every stride-th row
+    uint32_t wave[kRangeBlock / kWave];
+    uint32_t n_held, below;
+};
+
+// held[0, n) in ascending order, n <= 2^bits; the words from n on are the largest there is.
+__device__ void sort_held(unsigned long long* held, uint32_t size) {
+    for (uint32_t k = 2; k <= size; k <<= 1)
+        for (uint32_t j = k >> 1; j > 0; j >>= 1) {
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < size / 2; i += kRangeBlock) {
+                const uint32_t lo = 2 * i - (i & (j - 1)), hi = lo + j;
+                const unsigned long long a = held[lo], b = held[hi];
+                if ((a > b) == ((lo & k) == 0)) held[lo] = b, held[hi] = a;
+            }
+        }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(kRangeBlock) void transpose_range_kernel(TransposeArgs a, uint32_t range) {
+    __shared__ RangeLds s;
+    const TransposeJob& p = a.job;
+    const int64_t count = p.rows.get();
+    const uint32_t first = blockIdx.x * range, t = threadIdx.x;
+    const uint32_t sources = first >= p.n_src ? 0u : static_cast<uint32_t>(p.n_src - first < range ? p.n_src - first : range);
+    if (sources == 0) return;
+    int64_t used = count > 0 ? p.indptr[count] : 0;
+    if (used < 0 || used > p.n_col) {
+        raise(p.err, kErrData);
+        used = 0;
+    }
+    const uint32_t n_col = static_cast<uint32_t>(used), n = n_col + (p.row ? static_cast<uint32_t>(count) : 0u);     // places in use: samples, then rows
+    // where rows begin, roughly: the row of a place is looked up there first
+    const uint32_t stride = static_cast<uint32_t>((count + kRangeSteps - 1) / kRangeSteps) > 0 ? static_cast<uint32_t>((count + kRangeSteps - 1) / kRangeSteps) : 1u;
+    const uint32_t steps = static_cast<uint32_t>((count + stride - 1) / stride);
+    for (uint32_t i = t; i < steps; i += kRangeBlock) s.step[i] = static_cast<int32_t>(p.indptr[static_cast<int64_t>(i) * stride]);
+    for (uint32_t i = t; i < sources; i += kRangeBlock) s.count[i] = s.taken[i] = 0;
+    if (t == 0) s.n_held = 0, s.below = 0;
+    __syncthreads();
+
+    const auto source = [&](uint32_t place) { return place < n_col ? p.col[place] : p.row[place - n_col]; };
+    const auto hold = [&](uint32_t local, uint32_t place) {
+        const uint32_t at = atomicAdd(&s.n_held, 1u);
+        if (at < kRangeHeld) s.held[at] = static_cast<unsigned long long>(local) << 32 | place;
+    };
+    uint32_t below = 0;
+    const auto look = [&](int32_t src, uint32_t place) {
+        const uint32_t u = static_cast<uint32_t>(src);
+        if (u >= p.n_src) raise(p.err, kErrData);
+        else if (u < first) ++below;
+        else if (u - first < sources) {
+            atomicAdd(&s.count[u - first], 1u);
+            hold(u - first, place);
+        }
+    };
+    // (sixteen places to a thread are asked for together: a round is a trip to memory)
+    const auto look_through = [&](const int32_t* list, uint32_t len, uint32_t base_place) {
+        constexpr uint32_t kWords = 4, kRound = kRangeBlock * 4 * kWords;
+        for (uint32_t base = 0; base < len; base += kRound) {
+            i32x4 v[kWords];
+#pragma unroll
+            for (uint32_t k = 0; k < kWords; ++k) {
+                const uint32_t at = base + (k * kRangeBlock + t) * 4;
+                v[k] = at < len ? load_16_of<4>(list + at, len - at) : i32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < kWords; ++k) {
+                const uint32_t at = base + (k * kRangeBlock + t) * 4;
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+                    if (at + e < len) look(v[k][e], base_place + at + e);
+            }
+        }
+    };
+    look_through(p.col, n_col, 0);
+    if (p.row) look_through(p.row, n - n_col, n_col);
+    below = dpp_sum(below);
+    if (lane_id() == 0) atomicAdd(&s.below, below);
+    __syncthreads();
+    // counts -> where a source's entries begin (a thread to a source)
+    const uint32_t mine = t < sources ? s.count[t] : 0, upto = dpp_inclusive_scan(mine);
+    if (lane_id() == kWave - 1) s.wave[wave_id()] = upto;
+    __syncthreads();
+    uint32_t begin = s.below + upto - mine;
+    for (int w = 0; w < wave_id(); ++w) begin += s.wave[w];
+    if (t < sources) {
+        s.count[t] = begin;
+        p.src_indptr[first + t] = static_cast<int32_t>(begin);
+        if (first + t + 1 == p.n_src) p.src_indptr[p.n_src] = static_cast<int32_t>(begin + mine);
+    }
+    const uint32_t found = s.n_held;
+    __syncthreads();
+
+    const auto row_of = [&](uint32_t place) {                // the last row that begins at or before the place
+        uint32_t lo = 0, hi = steps;
+        while (hi - lo > 1) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (s.step[mid] <= static_cast<int32_t>(place)) lo = mid;
+            else hi = mid;
+        }
+        int64_t r0 = static_cast<int64_t>(lo) * stride, r1 = r0 + stride < count ? r0 + stride : count;
+        while (r1 - r0 > 1) {
+            const int64_t mid = (r0 + r1) / 2;
+            if (p.indptr[mid] <= place) r0 = mid;
+            else r1 = mid;
+        }
+        return static_cast<int32_t>(r0);
+    };
+    // sorts what is held and writes it behind what its sources have got so far
+    const auto place_held = [&](uint32_t held) {
+        uint32_t size = 2;
+        while (size < held) size <<= 1;
+        for (uint32_t i = held + t; i < size; i += kRangeBlock) s.held[i] = ~0ull;
+        sort_held(s.held, size);
+        for (uint32_t i = t; i < held; i += kRangeBlock) {
+            const uint32_t local = static_cast<uint32_t>(s.held[i] >> 32), place = static_cast<uint32_t>(s.held[i]);
+            uint32_t lo = 0, hi = i;                         // the source's first entry among those held
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (s.held[mid] >> 32 < local) lo = mid + 1;
+                else hi = mid;
+            }
+            const uint32_t to = s.count[local] + (i - lo);
+            if (to < a.n) p.src_entry[to] = place < n_col ? row_of(place) : ~static_cast<int32_t>(place - n_col);
+        }
+        __syncthreads();
+    };
+    if (found <= kRangeBlock) {                   // few: they are put together by source, and an entry counts those of its source before it
+        uint32_t local = 0, place = 0, at = 0;
+        if (t < found) {
+            local = static_cast<uint32_t>(s.held[t] >> 32);
+            place = static_cast<uint32_t>(s.held[t]);
+            at = s.count[local] - s.below;
+            s.placed[at + atomicAdd(&s.taken[local], 1u)] = place;
+        }
+        __syncthreads();
+        if (t < found) {
+            uint32_t before = 0;
+            const uint32_t end = at + s.taken[local];
+#pragma unroll 4
+            for (uint32_t i = at; i < end; ++i) before += s.placed[i] < place;
+            if (s.count[local] + before < a.n) p.src_entry[s.count[local] + before] = place < n_col ? row_of(place) : ~static_cast<int32_t>(place - n_col);
+        }
+        return;
+    }
+    if (found <= kRangeHeld) {
+        place_held(found);
+        return;
+    }
+    for (uint32_t base = 0; base < n; base += kRangeHeld) {
+        if (t == 0) s.n_held = 0;
+        __syncthreads();
+        for (uint32_t k = t; k < kRangeHeld; k += kRangeBlock)
+            if (base + k < n && static_cast<uint32_t>(source(base + k)) - first < sources) hold(static_cast<uint32_t>(source(base + k)) - first, base + k);
+        __syncthreads();
+        const uint32_t held = s.n_held;
+        place_held(held);
+        for (uint32_t i = t; i < held; i += kRangeBlock) {   // (the last of a source among those held moves it on)
+            const uint32_t local = static_cast<uint32_t>(s.held[i] >> 32);
+            if (i + 1 < held && s.held[i + 1] >> 32 == local) continue;
+            uint32_t lo = 0, hi = i;
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (s.held[mid] >> 32 < local) lo = mid + 1;
+                else hi = mid;
+            }
+            s.count[local] += i - lo + 1;
+        }
+        __syncthreads();
+    }
+}
+
+// Sources with long lists wait for the second kernel, cut into pieces; the pieces of one source are neighbours.
+struct LongPiece {
+    int32_t src, piece, pieces;
+    int32_t left;                                 // (of the first piece) workgroups that have not added up theirs
+    uint32_t slot;                                // where the piece's sums go, if there are several
+};
+struct GradScratch {
+    uint32_t* counters;                           // pieces waiting, slots taken, eighths that are done; from kLineWords on the eighths' counts.  Zero between calls
+    LongPiece* piece;                             // [most]
+    float* part;                                  // [slots][width]: sums of pieces
+    uint32_t most, slots;
+};
+
+// An entry's share of the gradient: a row of dmean and 1 / its samples, or of down and 1; nothing and an error if there is no such row.
+template <int TYPE>
+__device__ __forceinline__ void share_of(const MeanGradJob& p, int32_t entry, bool wanted, int col, int valid, float (&v)[8], float* weight) {
+    const bool own = entry < 0;
+    const int64_t row = own ? ~entry : entry;
+    const bool good = row < p.n_rows && (!own || p.down);
+    if (wanted && !good) raise(p.err, kErrData);
+    *weight = 1.0f;
+    if (wanted && good && !own) {
+        const RowBounds list = row_bounds(p.indptr, static_cast<uint32_t>(row));
+        *weight = 1.0f / static_cast<float>(list.hi - list.lo);
+    }
+    load_row_8<TYPE>(own ? p.down : p.dmean, row * (own ? p.down_ld : p.dmean_ld) + col, wanted && good, valid, v);
+}
+// sum += the shares of the entries [lo, hi), AHEAD at a time, in order
+template <int TYPE, int AHEAD>
+__device__ __forceinline__ void add_shares(const MeanGradJob& p, int32_t lo, int32_t hi, int col, int valid, float (&sum)[8]) {
+    for (int32_t k0 = lo; k0 < hi; k0 += AHEAD) {
+        int32_t entry[AHEAD];
+        float v[AHEAD][8], weight[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) entry[k] = p.src_entry[k0 + k < hi ? k0 + k : k0];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) share_of<TYPE>(p, entry[k], k0 + k < hi, col, valid, v[k], &weight[k]);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sum[c] += v[k][c] * weight[k];
+    }
+}
+
+// A group of lanes has a source.  (Two to a group, with the loads of both together, took half as long again: 20.6 and 12.0 us for
+// 24 000 sources of 26 600 entries and 256 columns in bfloat16, as fewer waves fit.)
 template <int TYPE, int LANES>
-__global__ __launch_bounds__(kBlock) void block_mean_grad_kernel(MeanGradJob p) {
-    constexpr int kGroups = kBlock / LANES, kCols = LANES * 8;
-    __shared__ float s_part[kGroups][kCols];
-    __shared__ int s_long[kGroups], s_n_long;
-    const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, col = (blockIdx.y * LANES + lane) * 8, valid = p.width - col;
-    const auto bounds = [&](int64_t src, int64_t* lo, int64_t* hi) {
-        *lo = p.src_indptr[src];
-        *hi = p.src_indptr[src + 1];
-        if (*lo < 0 || *lo > *hi || *hi > p.n_entries) {
+__global__ __launch_bounds__(kBlock) void block_mean_grad_kernel(MeanGradJob p, GradScratch s) {
+    constexpr int kGroups = kBlock / LANES;
+    const int lane = threadIdx.x % LANES, col = (blockIdx.y * LANES + lane) * 8, valid = p.width - col;
+    for (int64_t src = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / LANES; src < p.n_src; src += static_cast<int64_t>(gridDim.x) * kGroups) {
+        int32_t lo = p.src_indptr[src], hi = p.src_indptr[src + 1];
+        if (lo < 0 || lo > hi || hi > p.n_entries) {
             raise(p.err, kErrData);
-            *lo = *hi = 0;
+            lo = hi = 0;
         }
-    };
-    const auto add_up = [&](int64_t lo, int64_t hi, float (&sum)[8]) {
+        if (hi - lo > kLongList) {
+            if (lane == 0 && blockIdx.y == 0) {
+                const uint32_t pieces = (hi - lo + kPiece - 1) / kPiece, at = atomicAdd(s.counters, pieces);
+                const uint32_t slot = pieces > 1 ? atomicAdd(s.counters + 1, pieces) : 0u;
+                const bool room = at + pieces <= s.most && (pieces == 1 || slot + pieces <= s.slots);
+                if (!room) raise(p.err, kErrData);          // (only if lists overlap)
+                for (uint32_t k = 0; k < pieces && at + k < s.most; ++k)
+                    s.piece[at + k] = LongPiece{static_cast<int32_t>(src), static_cast<int32_t>(k), room ? static_cast<int32_t>(pieces) : 0,
+                                                static_cast<int32_t>(pieces * gridDim.y), slot + k};
+            }
+            continue;
+        }
+        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        add_shares<TYPE, kAhead>(p, lo, hi < lo + kAhead ? hi : lo + kAhead, col, valid, sum);
+        add_shares<TYPE, 8>(p, lo + kAhead, hi, col, valid, sum);
+        store_8_of<TYPE>(p.dx, src * p.dx_ld + col, valid, sum);
+    }
+}
+
+// The pieces of long lists, a workgroup to each at a time: its groups share the entries, and their sums are added in order.  Who
+// finishes the last piece of a source adds the pieces up, in order.
+template <int TYPE, int LANES>
+__global__ __launch_bounds__(kLongBlock) void block_mean_grad_long_kernel(MeanGradJob p, GradScratch s) {
+    constexpr int kGroups = kLongBlock / LANES, kCols = LANES * 8;
+    __shared__ float s_part[kGroups][kCols];
+    __shared__ int s_last;
+    const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, col = (blockIdx.y * LANES + lane) * 8, valid = p.width - col;
+    const uint32_t waiting = s.counters[0], n = waiting < s.most ? waiting : s.most;
+    for (uint32_t at = blockIdx.x; at < n; at += gridDim.x) {
+        const LongPiece it = s.piece[at];
+        if (it.pieces == 0) continue;
+        const int32_t lo = p.src_indptr[it.src] + it.piece * kPiece, end = p.src_indptr[it.src + 1], hi = lo + kPiece < end ? lo + kPiece : end;
+        const int32_t per = (hi - lo + kGroups - 1) / kGroups, lo_mine = lo + group * per, hi_mine = lo_mine + per < hi ? lo_mine + per : hi;
+        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        add_shares<TYPE, 8>(p, lo_mine, hi_mine, col, valid, sum);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) sum[c] = 0;
-        for (int64_t k0 = lo; k0 < hi; k0 += kAhead) {
-            int32_t entry[kAhead];
-            float v[kAhead][8], weight[kAhead];
+        for (int c = 0; c < 8; ++c) s_part[group][lane * 8 + c] = sum[c];
+        __syncthreads();
+        if (group == 0) {
+            for (int q = 1; q < kGroups; ++q)
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) entry[k] = p.src_entry[k0 + k < hi ? k0 + k : k0];
+                for (int c = 0; c < 8; ++c) sum[c] += s_part[q][lane * 8 + c];
+            if (it.pieces == 1) store_8_of<TYPE>(p.dx, it.src * p.dx_ld + col, valid, sum);
+            else store_8_of<kF32>(s.part, static_cast<int64_t>(it.slot) * p.width + col, valid, sum);
+        }
+        if (it.pieces > 1) {
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) s_last = atomicSub(&s.piece[at - it.piece].left, 1) == 1;
+            __syncthreads();
+            if (s_last) {                          // (of all columns: the workgroups of the other columns have left their sums, too)
+                __threadfence();
+                for (int c0 = threadIdx.x * 8; c0 < p.width; c0 += kLongBlock * 8) {
+                    float total[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 8
+                    for (int k = 0; k < it.pieces; ++k) {
+                        float v[8];
+                        load_8_of<kF32>(s.part, static_cast<int64_t>(it.slot - it.piece + k) * p.width + c0, p.width - c0, v);
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const bool own = entry[k] < 0;
-                const int64_t row = own ? ~entry[k] : entry[k];
-                const bool good = row < p.n_rows && (!own || p.down), wanted = k0 + k < hi && good;
-                if (!good) raise(p.err, kErrData);
-                weight[k] = 1.0f;
-                if (wanted && !own) {
-                    const RowBounds list = row_bounds(p.indptr, static_cast<uint32_t>(row));
-                    weight[k] = static_cast<float>(list.hi - list.lo);
+                        for (int c = 0; c < 8; ++c) total[c] += v[c];
+                    }
+                    store_8_of<TYPE>(p.dx, it.src * p.dx_ld + c0, p.width - c0, total);
                 }
-                load_row_8<TYPE>(own ? p.down : p.dmean, row * (own ? p.down_ld : p.dmean_ld) + col, wanted, valid, v[k]);
             }
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) sum[c] += v[k][c] / weight[k];
-        }
-    };
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups; first < p.n_src; first += static_cast<int64_t>(gridDim.x) * kGroups) {
-        if (threadIdx.x == 0) s_n_long = 0;
-        __syncthreads();
-        const int64_t src = first + group;
-        if (src < p.n_src) {
-            int64_t lo, hi;
-            bounds(src, &lo, &hi);
-            if (hi - lo <= kLongList) {
-                float sum[8];
-                add_up(lo, hi, sum);
-                store_8_of<TYPE>(p.dx, src * p.dx_ld + col, valid, sum);
-            } else if (lane == 0) s_long[atomicAdd(&s_n_long, 1)] = group;
         }
         __syncthreads();
-        // Sources with long lists: every group takes a part of the list, and the parts are added in order.
-        const int n_long = s_n_long;
-        for (int k = 0; k < n_long; ++k) {
-            const int64_t it = first + s_long[k];
-            int64_t lo, hi;
-            bounds(it, &lo, &hi);
-            const int64_t per = (hi - lo + kGroups - 1) / kGroups, lo_mine = lo + group * per, hi_mine = lo_mine + per < hi ? lo_mine + per : hi;
-            float sum[8];
-            add_up(lo_mine, hi_mine, sum);
-    #pragma unroll
-            for (int c = 0; c < 8; ++c) s_part[group][lane * 8 + c] = sum[c];
-            __syncthreads();
-            if (group == 0) {
-                for (int q = 1; q < kGroups; ++q)
-    #pragma unroll
-                    for (int c = 0; c < 8; ++c) sum[c] += s_part[q][lane * 8 + c];
-                store_8_of<TYPE>(p.dx, it * p.dx_ld + col, valid, sum);
-            }
-            __syncthreads();
+    }
+    // The last workgroup leaves the counters as it found them.  (A word that hundreds add to costs 60 ns for each of them, so they
+    // count by eighths first.)
+    if (threadIdx.x == 0) {
+        const uint32_t all = gridDim.x * gridDim.y, me = blockIdx.y * gridDim.x + blockIdx.x, line = me % kLines, lines = all < kLines ? all : kLines;
+        uint32_t* count = s.counters + (1 + line) * kLineWords;
+        if (atomicAdd(count, 1u) + 1 == (all - line + kLines - 1) / kLines) {
+            *count = 0;
+            if (atomicAdd(s.counters + 2, 1u) + 1 == lines) s.counters[0] = s.counters[1] = s.counters[2] = 0;
         }
-        __syncthreads();
     }
 }
 
@@ -262,22 +507,38 @@ struct RunMean {
         return hipGetLastError();
     }
 };
+// Most pieces that lists of n entries in all can be cut into (one of kLongList + 1 entries is one piece), and most of them that belong to
+// lists of several (kPiece + 1 entries are two).
+int64_t most_pieces(int64_t n) { return n / kLongList + 1; }
+int64_t most_slots(int64_t n) { return 2 * n / kPiece + 2; }
 struct RunMeanGrad {
     hipStream_t stream;
     MeanGradJob job;
+    GradScratch s;
     template <int TYPE, int LANES>
     hipError_t go() const {
-        hipLaunchKernelGGL((block_mean_grad_kernel<TYPE, LANES>), grid_of(job.n_src, job.width, LANES), dim3(kBlock), 0, stream, job);
-        return hipGetLastError();
+        const dim3 grid = grid_of(job.n_src, job.width, LANES);
+        hipLaunchKernelGGL((block_mean_grad_kernel<TYPE, LANES>), grid, dim3(kBlock), 0, stream, job, s);
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess && job.n_entries > kLongList) {
+            const unsigned most = static_cast<unsigned>(std::min<int64_t>(most_pieces(job.n_entries), 256));
+            hipLaunchKernelGGL((block_mean_grad_long_kernel<TYPE, LANES>), dim3(most, grid.y), dim3(kLongBlock), 0, stream, job, s);
+            e = hipGetLastError();
+        }
+        return e;
     }
 };
 
+constexpr int64_t kRangePlaces = 1 << 16;
 struct TransposePlan {
-    int64_t n;
+    int64_t n, ranges;                            // (ranges: 0 by a sort)
     size_t keys, entry, order, sort, bytes;
     explicit TransposePlan(const TransposeJob& j) {
         const auto up = [](size_t b) { return (b + 255) / 256 * 256; };
         n = j.n_col + (j.row ? j.rows.host : 0);
+        // By ranges where looking through all places takes less than the sort's five launches
+        ranges = n > kRangePlaces || j.n_src < 1 ? 0 : std::max<int64_t>(std::min<int64_t>(256, (j.n_src + 31) / 32), (j.n_src + kRangeMost - 1) / kRangeMost);
+        if (ranges > 4096) ranges = 0;
         const size_t ints = up(sizeof(int32_t) * static_cast<size_t>(std::max<int64_t>(n, 1)));
         keys = 0;
         entry = ints;
@@ -300,6 +561,11 @@ hipError_t launch_block_transpose(hipStream_t stream, const TransposeJob& job, v
     const TransposePlan plan(job);
     char* at = static_cast<char*>(scratch);
     TransposeArgs a{job, plan.n, reinterpret_cast<int32_t*>(at + plan.keys), reinterpret_cast<int32_t*>(at + plan.entry), reinterpret_cast<int32_t*>(at + plan.order)};
+    if (plan.ranges > 0) {
+        const uint32_t range = static_cast<uint32_t>((std::max<int64_t>(job.n_src, 1) + plan.ranges - 1) / plan.ranges);
+        hipLaunchKernelGGL(transpose_range_kernel, dim3(static_cast<unsigned>(plan.ranges)), dim3(kRangeBlock), 0, stream, a, range);
+        return hipGetLastError();
+    }
     hipError_t e = hipSuccess;
     const auto blocks = [](int64_t n) { return dim3(static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((n + kBlock - 1) / kBlock, 4096)))); };
     if (a.n > 0) {
@@ -314,9 +580,24 @@ hipError_t launch_block_transpose(hipStream_t stream, const TransposeJob& job, v
     return e;
 }
 
-hipError_t launch_block_mean_grad(hipStream_t stream, const MeanGradJob& job) {
+namespace {
+struct GradPlan {
+    size_t part, bytes;
+    explicit GradPlan(const MeanGradJob& j) {
+        part = (sizeof(LongPiece) * static_cast<size_t>(most_pieces(j.n_entries)) + 255) / 256 * 256;
+        bytes = part + sizeof(float) * static_cast<size_t>(most_slots(j.n_entries)) * static_cast<size_t>(j.width);
+    }
+};
+}  // namespace
+
+size_t block_mean_grad_scratch_bytes(const MeanGradJob& job) { return GradPlan(job).bytes; }
+
+hipError_t launch_block_mean_grad(hipStream_t stream, const MeanGradJob& job, uint32_t* counters, void* scratch) {
     if (job.n_src < 1) return hipSuccess;
-    return by_type(job.type, job.width, RunMeanGrad{stream, job});
+    char* at = static_cast<char*>(scratch);
+    const GradScratch s{counters, reinterpret_cast<LongPiece*>(at), reinterpret_cast<float*>(at + GradPlan(job).part),
+                        static_cast<uint32_t>(most_pieces(job.n_entries)), static_cast<uint32_t>(most_slots(job.n_entries))};
+    return by_type(job.type, job.width, RunMeanGrad{stream, job, s});
 }
 
 }  // namespace helios
