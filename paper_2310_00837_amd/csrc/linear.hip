@@ -552,7 +552,7 @@ __global__ __launch_bounds__(TILE::kThreads) void backward_kernel(ProductArgs<Pl
     else product<TYPE, TILE, false, true, DIRECT>(dx, blockIdx.x - dw_blocks, gridDim.x - dw_blocks, lds);
 }
 
-// Few rows: a workgroup has 16 rows of x and 16 of w, its waves share k between them and read both straight into the
+// Few tiles: a workgroup has 16 rows of x and 16 of w, its waves share k between them and read both straight into the
 // operands of the MFMA, and the eight sums of every element meet in LDS.
 constexpr int kFewWaves = 8;
 template <int TYPE, class OUT>
@@ -763,7 +763,13 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
     p.rows = j.rows;
     p.slices = 1;
     p.out = Out{j.x_scale, j.w_scale, j.bias, j.residual, j.residual_ld, j.pre, j.pre_ld, j.y, j.y_ld, j.act};
-    if (p.m <= 16) {
+    // Few tiles: 16 x 16 with k shared by eight waves, 3 us + (2 + 0.45 steps) ns a tile, against 3 us + a step's latency (0.33 us with
+    // elements of 16 bits, 0.27 with 8, 0.9 with 32) a step, a step being 128 bytes of k.  us, few / small tiles, half precision: 16 x 1024 x 256
+    // 4.4 / 8.3, 256 x 1024 x 256 4.7 / 8.8, 777 x 1024 x 256 10.5 / 9.0; single: 777 x 200 x 48 3.4 / 9.5, 1536 x 1024 x 256
+    // 27 / 29, 3000 x 256 x 256 17.5 / 11.2.  Large tiles from where they fill the CUs: 3000 x 2048 x 1024 in half precision small 23.6, large 27.5
+    // (192 large tiles), 6000 48.0 and 36.0 (376).
+    const int64_t steps = (p.k * type_bytes(TYPE) + kStageBytes - 1) / kStageBytes, latency = TYPE == kF32 ? 900 : TYPE == kE4M3 ? 270 : 330;
+    if (static_cast<int64_t>(tiles_of(p.m, 16)) * tiles_of(p.n, 16) * (200 + 45 * steps) <= 100 * latency * steps && tiles_of(p.m, 16) <= 65535) {
         const dim3 grid(tiles_of(p.n, 16), tiles_of(p.m, 16));
         hipLaunchKernelGGL((product_few_kernel<TYPE, Out>), grid, dim3(kFewWaves * kWave), 0, stream, p);
         return hipGetLastError();

@@ -192,19 +192,22 @@ def _dev_accessible(t: torch.Tensor, dtype: torch.dtype, what: str) -> torch.Ten
 _TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
 
 
-def _mat(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, what: str):
+def _mat(t: Optional[torch.Tensor], shape, dtype: torch.dtype, what: str):
     """(pointer, row stride) of a matrix on the GPU whose rows are contiguous; (None, 0) for None."""
     if t is None:
         return None, 0
-    if t.dtype != dtype or not t.is_cuda or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
-        raise TypeError(f"{what}: expected a {dtype} tensor of {rows} x {cols} on the GPU with contiguous rows")
-    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+    if t.dtype is dtype and t.shape == shape and t.is_cuda:
+        step, one = t.stride()
+        rows, cols = shape
+        if one == 1 or cols <= 1:
+            return t.data_ptr(), step if rows > 1 else cols
+    raise TypeError(f"{what}: expected a {dtype} tensor of {shape[0]} x {shape[1]} on the GPU with contiguous rows")
 
 
 def _vec(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype != dtype or not t.is_cuda or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_cuda or t.numel() != n or not t.is_contiguous():
         raise TypeError(f"{what}: expected a contiguous {dtype} tensor of {n} on the GPU")
     return t.data_ptr()
 
@@ -693,10 +696,10 @@ class Helios:
         x_type, out_type = _type(x, "x"), _type(y, "y")
         n, k = x.shape
         m = w.shape[0]
-        out = y.dtype
-        a = LinearArgs(n, _count(n_rows_dev, "n_rows_dev"), k, m, act, x_type, out_type, 0, *_mat(x, n, k, x.dtype, "x"),
-                       _vec(x_scale, n, torch.float32, "x_scale"), *_mat(w, m, k, x.dtype, "w"), _vec(w_scale, m, torch.float32, "w_scale"),
-                       _vec(bias, m, out, "bias"), *_mat(residual, n, m, out, "residual"), *_mat(pre, n, m, out, "pre"), *_mat(y, n, m, out, "y"))
+        out, shape = y.dtype, (n, m)
+        a = LinearArgs(n, _count(n_rows_dev, "n_rows_dev"), k, m, act, x_type, out_type, 0, *_mat(x, x.shape, x.dtype, "x"),
+                       _vec(x_scale, n, torch.float32, "x_scale"), *_mat(w, (m, k), x.dtype, "w"), _vec(w_scale, m, torch.float32, "w_scale"),
+                       _vec(bias, m, out, "bias"), *_mat(residual, shape, out, "residual"), *_mat(pre, shape, out, "pre"), *_mat(y, shape, out, "y"))
         rc = _lib.helios_linear(self._h, a)
         if rc != OK:
             self._check(rc)
@@ -709,9 +712,9 @@ class Helios:
         n, k = x.shape
         m = w.shape[0]
         out = dy.dtype
-        a = LinearGradArgs(n, _count(n_rows_dev, "n_rows_dev"), k, m, act, x_type, out_type, 0, *_mat(x, n, k, x.dtype, "x"),
-                           *_mat(w, m, k, x.dtype, "w"), *_mat(dy, n, m, out, "dy"), *_mat(pre, n, m, out, "pre"), *_mat(dx, n, k, x.dtype, "dx"),
-                           *_mat(dw, m, k, x.dtype, "dw"), _vec(dbias, m, out, "dbias"))
+        a = LinearGradArgs(n, _count(n_rows_dev, "n_rows_dev"), k, m, act, x_type, out_type, 0, *_mat(x, x.shape, x.dtype, "x"),
+                           *_mat(w, (m, k), x.dtype, "w"), *_mat(dy, (n, m), out, "dy"), *_mat(pre, (n, m), out, "pre"), *_mat(dx, (n, k), x.dtype, "dx"),
+                           *_mat(dw, (m, k), x.dtype, "dw"), _vec(dbias, m, out, "dbias"))
         rc = _lib.helios_linear_grad(self._h, a)
         if rc != OK:
             self._check(rc)
@@ -723,8 +726,9 @@ class Helios:
         x_type, y_type = _type(x, "x"), _type(y, "y")
         n, d = x.shape
         dt = x.dtype
-        a = RmsNormArgs(n, _count(n_rows_dev, "n_rows_dev"), d, x_type, y_type, eps, 0, *_mat(x, n, d, dt, "x"), *_mat(residual, n, d, dt, "residual"),
-                        _vec(gain, d, dt, "gain"), *_mat(total, n, d, dt, "total"), *_mat(y, n, d, y.dtype, "y"),
+        shape = x.shape
+        a = RmsNormArgs(n, _count(n_rows_dev, "n_rows_dev"), d, x_type, y_type, eps, 0, *_mat(x, shape, dt, "x"), *_mat(residual, shape, dt, "residual"),
+                        _vec(gain, d, dt, "gain"), *_mat(total, shape, dt, "total"), *_mat(y, shape, y.dtype, "y"),
                         _vec(y_scale, n, torch.float32, "y_scale"), _vec(inv_rms, n, torch.float32, "inv_rms"))
         rc = _lib.helios_rms_norm(self._h, a)
         if rc != OK:
@@ -737,9 +741,10 @@ class Helios:
         x_type = _type(total, "total")
         n, d = total.shape
         dt = total.dtype
-        a = RmsNormGradArgs(n, _count(n_rows_dev, "n_rows_dev"), d, x_type, eps, *_mat(total, n, d, dt, "total"), _vec(gain, d, dt, "gain"),
-                            _vec(inv_rms, n, torch.float32, "inv_rms"), *_mat(dy, n, d, dt, "dy"), *_mat(dtotal, n, d, dt, "dtotal"),
-                            *_mat(dx, n, d, dt, "dx"), _vec(dgain, d, dt, "dgain"))
+        shape = total.shape
+        a = RmsNormGradArgs(n, _count(n_rows_dev, "n_rows_dev"), d, x_type, eps, *_mat(total, shape, dt, "total"), _vec(gain, d, dt, "gain"),
+                            _vec(inv_rms, n, torch.float32, "inv_rms"), *_mat(dy, shape, dt, "dy"), *_mat(dtotal, shape, dt, "dtotal"),
+                            *_mat(dx, shape, dt, "dx"), _vec(dgain, d, dt, "dgain"))
         rc = _lib.helios_rms_norm_grad(self._h, a)
         if rc != OK:
             self._check(rc)
@@ -747,8 +752,8 @@ class Helios:
     def quantize_rows(self, x: torch.Tensor, q: torch.Tensor, q_scale: torch.Tensor, n_rows_dev: Optional[torch.Tensor] = None) -> None:
         """Rows in 8 bits with a scale each, as linear takes them."""
         n, d = x.shape
-        rc = _lib.helios_quantize_rows(self._h, n, _count(n_rows_dev, "n_rows_dev"), d, _type(x, "x"), *_mat(x, n, d, x.dtype, "x"),
-                                       *_mat(q, n, d, torch.float8_e4m3fn, "q"), _vec(q_scale, n, torch.float32, "q_scale"))
+        rc = _lib.helios_quantize_rows(self._h, n, _count(n_rows_dev, "n_rows_dev"), d, _type(x, "x"), *_mat(x, (n, d), x.dtype, "x"),
+                                       *_mat(q, (n, d), torch.float8_e4m3fn, "q"), _vec(q_scale, n, torch.float32, "q_scale"))
         if rc != OK:
             self._check(rc)
 
@@ -761,9 +766,9 @@ class Helios:
         dt = x.dtype
         _dev(indptr, torch.int64, "indptr"), _dev(col, torch.int32, "col")
         assert indptr.numel() > n and (row is None or row.numel() >= n)
-        a = BlockMeanArgs(n, _count(n_rows_dev, "n_rows_dev"), d, n_src, col.numel(), x_type, 0, *_mat(x, n_src, d, dt, "x"), indptr.data_ptr(),
-                          col.data_ptr(), None if row is None else _dev_ptr(row, torch.int32, "row"), *_mat(mean, n, d, dt, "mean"),
-                          *_mat(own, n, d, dt, "own"))
+        a = BlockMeanArgs(n, _count(n_rows_dev, "n_rows_dev"), d, n_src, col.numel(), x_type, 0, *_mat(x, (n_src, d), dt, "x"), indptr.data_ptr(),
+                          col.data_ptr(), None if row is None else _dev_ptr(row, torch.int32, "row"), *_mat(mean, (n, d), dt, "mean"),
+                          *_mat(own, (n, d), dt, "own"))
         rc = _lib.helios_block_mean(self._h, a)
         if rc != OK:
             self._check(rc)
@@ -792,7 +797,7 @@ class Helios:
         _dev(indptr, torch.int64, "indptr"), _dev(src_indptr, torch.int32, "src_indptr"), _dev(src_entry, torch.int32, "src_entry")
         assert indptr.numel() > n and src_indptr.numel() > n_src
         a = BlockMeanGradArgs(n, d, n_src, src_entry.numel(), x_type, 0, indptr.data_ptr(), src_indptr.data_ptr(), src_entry.data_ptr(),
-                              *_mat(dmean, n, d, dt, "dmean"), *_mat(down, n, d, dt, "down"), *_mat(dx, n_src, d, dt, "dx"))
+                              *_mat(dmean, (n, d), dt, "dmean"), *_mat(down, (n, d), dt, "down"), *_mat(dx, (n_src, d), dt, "dx"))
         rc = _lib.helios_block_mean_grad(self._h, a)
         if rc != OK:
             self._check(rc)
