@@ -47,26 +47,34 @@ __device__ __forceinline__ i32x4 load_16_of(const void* p, int64_t valid) {
     return i32x4{static_cast<int32_t>(w[0]), static_cast<int32_t>(w[1]), static_cast<int32_t>(w[2]), static_cast<int32_t>(w[3])};
 }
 
-// Eight neighbouring elements, widened to 32 bits (TYPE: one of the floating types of 16 or 32 bits).
+// Eight neighbouring elements, widened to 32 bits (TYPE: one of the floating types of 16 or 32 bits): from their 16 or 32 bytes ...
 template <int TYPE>
-__device__ __forceinline__ void load_8(const void* base, int64_t at, float (&v)[8]) {
+__device__ __forceinline__ void widen_8(const i32x4 (&raw)[type_bytes(TYPE) / 2], float (&v)[8]) {
     if constexpr (TYPE == kF32) {
-        const float* p = static_cast<const float*>(base) + at;
-        const f32x4 a = __builtin_bit_cast(f32x4, load_16(p)), b = __builtin_bit_cast(f32x4, load_16(p + 4));
+        const f32x4 a = __builtin_bit_cast(f32x4, raw[0]), b = __builtin_bit_cast(f32x4, raw[1]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
     } else if constexpr (TYPE == kF16) {
-        const f16x8 a = __builtin_bit_cast(f16x8, load_16(static_cast<const _Float16*>(base) + at));
+        const f16x8 a = __builtin_bit_cast(f16x8, raw[0]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(a[e]);
     } else {
-        const i32x4 a = load_16(static_cast<const uint16_t*>(base) + at);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            v[2 * e] = __builtin_bit_cast(float, a[e] << 16);
-            v[2 * e + 1] = __builtin_bit_cast(float, a[e] & static_cast<int32_t>(0xffff0000));
+            const int32_t two = raw[0][e];
+            v[2 * e] = __builtin_bit_cast(float, two << 16);
+            v[2 * e + 1] = __builtin_bit_cast(float, two & static_cast<int32_t>(0xffff0000));
         }
     }
+}
+// ... or from memory
+template <int TYPE>
+__device__ __forceinline__ void load_8(const void* base, int64_t at, float (&v)[8]) {
+    const char* p = static_cast<const char*>(base) + at * type_bytes(TYPE);
+    i32x4 raw[type_bytes(TYPE) / 2];
+    raw[0] = load_16(p);
+    if constexpr (TYPE == kF32) raw[1] = load_16(p + 16);
+    widen_8<TYPE>(raw, v);
 }
 template <int TYPE>
 __device__ __forceinline__ float load_1(const void* base, int64_t at) {

@@ -295,12 +295,27 @@ struct ForwardOut {
         if (bias) load_8_of<OUT_TYPE>(bias, col, valid, c.bias);
         return c;
     }
-    __device__ __forceinline__ void row(const Columns& c, int64_t row, float (&v)[8]) const {
-        if (x_scale) {
-            const float s = x_scale[row];
+    // what a row needs from memory, asked for before its sums are there
+    struct Ahead {
+        i32x4 residual[type_bytes(OUT_TYPE) / 2];
+        float scale;
+    };
+    __device__ __forceinline__ Ahead ahead(const Columns& c, int64_t row) const {
+        Ahead a{};
+        if (residual) {
+            constexpr int kBytes = type_bytes(OUT_TYPE), kPer = 16 / kBytes;
+            const char* p = static_cast<const char*>(residual) + (row * residual_ld + c.col) * kBytes;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= s * c.scale[e];
+            for (int k = 0; k < 8 / kPer; ++k)
+                if (c.valid > k * kPer) a.residual[k] = load_16_of<kBytes>(p + 16 * k, c.valid - k * kPer);
         }
+        if (x_scale) a.scale = x_scale[row];
+        return a;
+    }
+    __device__ __forceinline__ void row(const Columns& c, const Ahead& a, int64_t row, float (&v)[8]) const {
+        if (x_scale)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= a.scale * c.scale[e];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += c.bias[e];
         if (pre) store_8_of<OUT_TYPE>(pre, row * pre_ld + c.col, c.valid, v);
@@ -310,7 +325,7 @@ struct ForwardOut {
             for (int e = 0; e < 8; ++e) v[e] = v[e] < c.least ? c.least : v[e];        // NaN stays
         if (residual) {
             float r[8];
-            load_8_of<OUT_TYPE>(residual, row * residual_ld + c.col, c.valid, r);
+            widen_8<OUT_TYPE>(a.residual, r);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += r[e];
         }
@@ -326,7 +341,9 @@ struct PlainOut {                                 // (slice: which part of k the
         int32_t valid;
     };
     __device__ __forceinline__ Columns at(int32_t col, int valid, int slice) const { return Columns{slice * slice_stride + col, valid}; }
-    __device__ __forceinline__ void row(const Columns& c, int64_t row, float (&v)[8]) const { store_8_of<OUT_TYPE>(y, c.at + row * ld, c.valid, v); }
+    struct Ahead {};
+    __device__ __forceinline__ Ahead ahead(const Columns&, int64_t) const { return Ahead{}; }
+    __device__ __forceinline__ void row(const Columns& c, const Ahead&, int64_t row, float (&v)[8]) const { store_8_of<OUT_TYPE>(y, c.at + row * ld, c.valid, v); }
 };
 
 template <class OUT>
@@ -513,8 +530,19 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
         static_assert(kThreads % (BN / 8) == 0, "a thread stays with its columns");
         const int out_col = threadIdx.x % (BN / 8) * 8;
         const typename OUT::Columns columns = p.out.at(n0 + out_col, p.n - n0 - out_col, slice);
+        constexpr int kSlab = kOutTiles * 16, kStep = kThreads / (BN / 8), kOutRows = WAVES_M * kSlab / kStep;      // (a slab: the rows of one row of waves)
+        static_assert(WAVES_M * kSlab % kStep == 0, "every thread has as many rows");
+        const int valid = p.n - n0 - out_col;
 #pragma unroll
         for (int i0 = 0; i0 < kTm; i0 += kOutTiles) {
+            const auto row_at = [&](int q) {
+                const int at = threadIdx.x / (BN / 8) + q * kStep;
+                return m0 + at / kSlab * (kTm * 16) + i0 * 16 + at % kSlab;
+            };
+            typename OUT::Ahead ahead[kOutRows];
+#pragma unroll
+            for (int q = 0; q < kOutRows; ++q)
+                if (valid > 0 && row_at(q) < m_end) ahead[q] = p.out.ahead(columns, row_at(q));
             if (i0 > 0) __syncthreads();
 #pragma unroll
             for (int i = 0; i < kOutTiles; ++i)
@@ -522,17 +550,14 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
                 for (int j = 0; j < kTn; ++j)
                     *reinterpret_cast<f32x4*>(sums + ((wave_m * kOutTiles + i) * 16 + r) * kOutLd + (wave_n * kTn + j) * 16 + 4 * g) = acc[i0 + i][j];
             __syncthreads();
-            const int valid = p.n - n0 - out_col;
-            constexpr int kSlab = kOutTiles * 16;                        // the rows of one row of waves
-            if (valid > 0)
-                for (int at = threadIdx.x / (BN / 8); at < WAVES_M * kSlab; at += kThreads / (BN / 8)) {
-                    const int64_t row = m0 + at / kSlab * (kTm * 16) + i0 * 16 + at % kSlab;
-                    if (row >= m_end) continue;
-                    const f32x4* from = reinterpret_cast<const f32x4*>(sums + at * kOutLd + out_col);
-                    const f32x4 lo = from[0], hi = from[1];
-                    float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                    p.out.row(columns, row, v);
-                }
+#pragma unroll
+            for (int q = 0; q < kOutRows; ++q) {
+                if (valid <= 0 || row_at(q) >= m_end) continue;
+                const f32x4* from = reinterpret_cast<const f32x4*>(sums + (threadIdx.x / (BN / 8) + q * kStep) * kOutLd + out_col);
+                const f32x4 lo = from[0], hi = from[1];
+                float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                p.out.row(columns, ahead[q], row_at(q), v);
+            }
         }
         __syncthreads();
     }
@@ -591,7 +616,8 @@ __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(ProductAr
 #pragma unroll
                 for (int w = 0; w < kFewWaves; ++w) v[e] += sums[w][row][col + e];
             }
-            p.out.row(p.out.at(n0 + col, valid, 0), m0 + row, v);
+            const typename OUT::Columns columns = p.out.at(n0 + col, valid, 0);
+            p.out.row(columns, p.out.ahead(columns, m0 + row), m0 + row, v);
         }
     }
 }
