@@ -187,21 +187,50 @@ __device__ __forceinline__ void scale_by_slope_8(int act, const float (&z)[8], f
     }
 }
 
-// Sum over the lanes of a group of G (a power of two, up to a wave), the same value in all of them.
-template <int G>
-__device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-    for (int d = G / 2; d >= 1; d >>= 1) v += __shfl_xor(v, d, kWave);
+// The value of another lane, by moves that need no trip through LDS: STEP 0 and 1 the lane 1 and 2 away (within four), 2 and 3 the
+// mirrored one of eight and of sixteen lanes.
+template <int STEP>
+__device__ __forceinline__ float moved(float v) {
+    constexpr int kControl = STEP == 0 ? 0xb1 : STEP == 1 ? 0x4e : STEP == 2 ? 0x141 : 0x140;
+    const int bits = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(bits, bits, kControl, 0xf, 0xf, false));
+}
+// {the value of the row of 16 (32) lanes that comes first of two, that of the second}
+struct TwoFloats {
+    float a, b;
+};
+template <int ROW>
+__device__ __forceinline__ TwoFloats both_rows(float v) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    const u32x2 r = ROW == 16 ? __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(bits, bits, false, false))
+                              : __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(bits, bits, false, false));
+    const uint32_t lo = r.x, hi = r.y;
+    return TwoFloats{__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi)};
+}
+// A sum, or a maximum that keeps NaN, over the lanes of a group of G (16 or 64), the same bits in all of them.
+template <int G, class OP>
+__device__ __forceinline__ float group_reduce(float v, OP op) {
+    static_assert(G == 16 || G == 64, "a row of lanes, or a wave");
+    v = op(v, moved<0>(v));
+    v = op(v, moved<1>(v));
+    v = op(v, moved<2>(v));
+    v = op(v, moved<3>(v));
+    if (G == 64) {
+        TwoFloats t = both_rows<16>(v);
+        v = op(t.a, t.b);
+        t = both_rows<32>(v);
+        v = op(t.a, t.b);
+    }
     return v;
 }
 template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+    return group_reduce<G>(v, [](float a, float b) { return a + b; });
+}
+template <int G>
 __device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-    for (int d = G / 2; d >= 1; d >>= 1) {
-        const float o = __shfl_xor(v, d, kWave);
-        v = o > v || o != o ? o : v;                                                   // NaN stays
-    }
-    return v;
+    return group_reduce<G>(v, [](float a, float b) { return a > b || a != a ? a : b; });
 }
 
 // out[c] = the sum over p of part[p][c], p < n_parts, for the 16 columns from `first` on, by a workgroup of kBlock threads.  Four of

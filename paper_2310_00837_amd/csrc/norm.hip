@@ -148,29 +148,78 @@ __global__ __launch_bounds__(RowShape<LANES>::kThreads) void norm_kernel(NormJob
         norm_row<TYPE, LANES, CHUNKS>(p, row, lane, s);
 }
 
-// Every workgroup goes through rows blockIdx.x * kRows + ..., and keeps its lanes' sums for dgain until the end.
+// A workgroup of the gradient: with one chunk to a lane, as many rows at a time as fit 1024 threads, so that there are few sums of
+// dgain to be added up.
+template <int LANES, int CHUNKS>
+struct GradShape {
+    static constexpr int kThreads = LANES <= kWave && CHUNKS == 1 ? 1024 : RowShape<LANES>::kThreads, kRows = kThreads / LANES;
+    static constexpr int kMostBlocks = kThreads == 1024 ? 256 : 1024;
+};
+// eight elements as they are in memory; zeros where there are none
+template <int TYPE>
+struct Raw8 {
+    i32x4 v[type_bytes(TYPE) / 2];
+    __device__ __forceinline__ void load(const void* base, int64_t at, int valid) {
+        constexpr int kBytes = type_bytes(TYPE), kPer = 16 / kBytes;
+        const char* p = static_cast<const char*>(base) + at * kBytes;
+#pragma unroll
+        for (int k = 0; k < 8 / kPer; ++k) {
+            v[k] = i32x4{0, 0, 0, 0};
+            if (valid > k * kPer) v[k] = load_16_of<kBytes>(p + 16 * k, valid - k * kPer);
+        }
+    }
+};
+
+// Every workgroup goes through rows blockIdx.x * kRows + ..., asks for a row while the one before it is worked on (rows of up to
+// eight elements a lane: more would not fit the registers), and keeps its lanes' sums for dgain until the end.
 template <int TYPE, int LANES, int CHUNKS>
-__global__ __launch_bounds__(RowShape<LANES>::kThreads) void norm_grad_kernel(NormGradJob p, float* part) {
-    constexpr int kThreads = RowShape<LANES>::kThreads, kRows = RowShape<LANES>::kRows, kWidth = LANES * CHUNKS * 8;
+__global__ __launch_bounds__((GradShape<LANES, CHUNKS>::kThreads)) void norm_grad_kernel(NormGradJob p, float* part) {
+    constexpr int kThreads = GradShape<LANES, CHUNKS>::kThreads, kRows = GradShape<LANES, CHUNKS>::kRows, kWidth = LANES * CHUNKS * 8;
+    constexpr bool kPipeline = CHUNKS == 1;
     __shared__ float s[kThreads / kWave];
     __shared__ float s_gain[kRows > 1 ? kRows : 1][kRows > 1 ? kWidth : 1];
-    const int64_t count = p.rows.get();
+    const int64_t count = p.rows.get(), stride = static_cast<int64_t>(gridDim.x) * kRows;
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
     float dg[CHUNKS][8];
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int e = 0; e < 8; ++e) dg[c][e] = 0;
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + sub; row < count; row += static_cast<int64_t>(gridDim.x) * kRows) {
-        float t[CHUNKS][8], d[CHUNKS][8];
-        float square = 0, dot = 0;
+    Raw8<TYPE> t_raw[CHUNKS], d_raw[CHUNKS], r_raw[CHUNKS];
+    const auto load = [&](int64_t row) {
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             const int col = (c * LANES + lane) * 8, valid = p.width - col;
-            load_8_of<TYPE>(p.total, row * p.total_ld + col, valid, t[c]);
-            load_8_of<TYPE>(p.dy, row * p.dy_ld + col, valid, d[c]);
-            float g[8] = {1, 1, 1, 1, 1, 1, 1, 1};
-            if (p.gain) load_8_of<TYPE>(p.gain, col, valid, g);
+            t_raw[c].load(p.total, row * p.total_ld + col, valid);
+            d_raw[c].load(p.dy, row * p.dy_ld + col, valid);
+            if (kPipeline && p.dtotal) r_raw[c].load(p.dtotal, row * p.dtotal_ld + col, valid);
+        }
+    };
+    float gain[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+    if (kPipeline && p.gain) load_8_of<TYPE>(p.gain, lane * 8, p.width - lane * 8, gain);
+    const auto gain_of = [&](int c, float (&g)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] = gain[e];
+        if (!kPipeline && p.gain) load_8_of<TYPE>(p.gain, (c * LANES + lane) * 8, p.width - (c * LANES + lane) * 8, g);
+    };
+    // (where a row takes the whole workgroup the rows in turn are the same for all of its threads)
+    int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + sub;
+    if (kPipeline && row < count) load(row);
+    for (; row < count; row += stride) {
+        float t[CHUNKS][8], d[CHUNKS][8], r[8];
+        if (!kPipeline) load(row);
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            widen_8<TYPE>(t_raw[c].v, t[c]);
+            widen_8<TYPE>(d_raw[c].v, d[c]);
+            if (kPipeline && p.dtotal) widen_8<TYPE>(r_raw[c].v, r);
+        }
+        if (kPipeline && row + stride < count) load(row + stride);
+        float square = 0, dot = 0;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            float g[8];
+            gain_of(c, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) square += t[c][e] * t[c][e], dot += t[c][e] * d[c][e] * g[e];
         }
@@ -180,16 +229,15 @@ __global__ __launch_bounds__(RowShape<LANES>::kThreads) void norm_grad_kernel(No
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             const int col = (c * LANES + lane) * 8, valid = p.width - col;
-            float g[8] = {1, 1, 1, 1, 1, 1, 1, 1}, out[8];
-            if (p.gain) load_8_of<TYPE>(p.gain, col, valid, g);
+            float g[8], out[8];
+            gain_of(c, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 dg[c][e] += d[c][e] * t[c][e] * q;
                 out[e] = q * (d[c][e] * g[e] - t[c][e] * f);
             }
             if (p.dtotal) {
-                float r[8];
-                load_8_of<TYPE>(p.dtotal, row * p.dtotal_ld + col, valid, r);
+                if (!kPipeline) load_8_of<TYPE>(p.dtotal, row * p.dtotal_ld + col, valid, r);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) out[e] += r[e];
             }
@@ -224,7 +272,7 @@ __global__ __launch_bounds__(kBlock) void gain_sum_kernel(const float* part, int
 
 // The lanes and chunks for a row of `width` elements
 template <int TYPE, class RUN>
-hipError_t by_width(int32_t width, RUN run) {
+auto by_width(int32_t width, RUN run) {
     if (width <= 128) return run.template go<TYPE, 16, 1>();
     if (width <= 512) return run.template go<TYPE, 64, 1>();
     if (width <= 1024) return run.template go<TYPE, 64, 2>();
@@ -239,12 +287,6 @@ hipError_t by_type(int type, int32_t width, RUN run) {
     return by_width<kBF16>(width, run);
 }
 
-int rows_per_workgroup(int32_t width) { return width <= 128 ? kBlock / 16 : width <= 1024 ? kBlock / kWave : 1; }
-unsigned grad_blocks(const NormGradJob& j) {
-    const int64_t groups = (j.rows.host + rows_per_workgroup(j.width) - 1) / rows_per_workgroup(j.width);
-    return static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((groups + 1) / 2, 1024)));
-}
-
 struct RunNorm {
     hipStream_t stream;
     NormJob job;
@@ -256,13 +298,22 @@ struct RunNorm {
         return hipGetLastError();
     }
 };
+struct GradBlocks {                               // workgroups of the gradient
+    int64_t rows;
+    template <int TYPE, int LANES, int CHUNKS>
+    unsigned go() const {
+        typedef GradShape<LANES, CHUNKS> Shape;
+        return static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((rows + Shape::kRows - 1) / Shape::kRows, Shape::kMostBlocks)));
+    }
+};
 struct RunGrad {
     hipStream_t stream;
     NormGradJob job;
     float* part;
     template <int TYPE, int LANES, int CHUNKS>
     hipError_t go() const {
-        hipLaunchKernelGGL((norm_grad_kernel<TYPE, LANES, CHUNKS>), dim3(grad_blocks(job)), dim3(RowShape<LANES>::kThreads), 0, stream, job, part);
+        const unsigned blocks = GradBlocks{job.rows.host}.go<TYPE, LANES, CHUNKS>();
+        hipLaunchKernelGGL((norm_grad_kernel<TYPE, LANES, CHUNKS>), dim3(blocks), dim3(GradShape<LANES, CHUNKS>::kThreads), 0, stream, job, part);
         return hipGetLastError();
     }
 };
@@ -275,7 +326,7 @@ hipError_t launch_norm(hipStream_t stream, const NormJob& job) {
 }
 
 size_t norm_grad_scratch_bytes(const NormGradJob& job) {
-    return job.dgain ? sizeof(float) * grad_blocks(job) * static_cast<size_t>(job.width) : 0;
+    return job.dgain ? sizeof(float) * by_width<kF32>(job.width, GradBlocks{job.rows.host}) * static_cast<size_t>(job.width) : 0;
 }
 
 hipError_t launch_norm_grad(hipStream_t stream, const NormGradJob& job, void* scratch) {
@@ -283,7 +334,7 @@ hipError_t launch_norm_grad(hipStream_t stream, const NormGradJob& job, void* sc
     hipError_t e = by_type(job.type, job.width, RunGrad{stream, job, part});
     if (e == hipSuccess && job.dgain) {
         const unsigned blocks = static_cast<unsigned>((job.width + kSumColumns - 1) / kSumColumns);
-        hipLaunchKernelGGL(gain_sum_kernel, dim3(blocks), dim3(kBlock), 0, stream, part, static_cast<int>(grad_blocks(job)), job.width, job.dgain, job.type);
+        hipLaunchKernelGGL(gain_sum_kernel, dim3(blocks), dim3(kBlock), 0, stream, part, static_cast<int>(by_width<kF32>(job.width, GradBlocks{job.rows.host})), job.width, job.dgain, job.type);
         e = hipGetLastError();
     }
     return e;
