@@ -113,17 +113,7 @@ __device__ __forceinline__ void store_8_of(void* base, int64_t at, int valid, co
     for (int e = 0; e < 8; ++e)
         if (e < valid) p[e] = static_cast<T>(v[e]);
 }
-// the same for a type that is an argument of the kernel (the branches are the same for all lanes)
-__device__ __forceinline__ void load_8_of(int type, const void* base, int64_t at, int valid, float (&v)[8]) {
-    if (type == kF32) load_8_of<kF32>(base, at, valid, v);
-    else if (type == kF16) load_8_of<kF16>(base, at, valid, v);
-    else load_8_of<kBF16>(base, at, valid, v);
-}
-__device__ __forceinline__ void store_8_of(int type, void* base, int64_t at, int valid, const float (&v)[8]) {
-    if (type == kF32) store_8_of<kF32>(base, at, valid, v);
-    else if (type == kF16) store_8_of<kF16>(base, at, valid, v);
-    else store_8_of<kBF16>(base, at, valid, v);
-}
+// (the type is an argument of the kernel: the branches are the same for all lanes)
 __device__ __forceinline__ void store_1(int type, void* base, int64_t at, float v) {
     if (type == kF32) static_cast<float*>(base)[at] = v;
     else if (type == kF16) static_cast<_Float16*>(base)[at] = static_cast<_Float16>(v);

@@ -315,7 +315,7 @@ struct ForwardOut {
     __device__ __forceinline__ void row(const Columns& c, const Ahead& a, int64_t row, float (&v)[8]) const {
         if (x_scale)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= a.scale * c.scale[e];
+            for (int e = 0; e < 8; ++e) v[e] = v[e] * a.scale * c.scale[e];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += c.bias[e];
         if (pre) store_8_of<OUT_TYPE>(pre, row * pre_ld + c.col, c.valid, v);
@@ -365,41 +365,37 @@ __device__ __forceinline__ void tile_of(uint32_t block, uint32_t members, uint32
     *member = at % members;
 }
 
-// Waits until at most AHEAD of this wave's loads are in flight and its LDS reads are done, then for the other waves.
-template <int AHEAD>
-__device__ __forceinline__ void wait_and_meet() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(AHEAD) : "memory");
-}
+// Waits until this wave's loads into LDS and its LDS reads are done, then for the other waves.
+__device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Shape of a workgroup's tile: rows of A and B, the waves that share it, bytes of k to a stage, stages in LDS.
-template <int M, int N, int WAVES_M, int WAVES_N, int ROW, int STAGES>
+// Shape of a workgroup's tile: rows of A and B, and the waves that share it.
+template <int M, int N, int WAVES_M, int WAVES_N>
 struct Tile {
-    static constexpr int kM = M, kN = N, kWavesM = WAVES_M, kWavesN = WAVES_N, kRow = ROW, kStages = STAGES;
+    static constexpr int kM = M, kN = N, kWavesM = WAVES_M, kWavesN = WAVES_N;
     static constexpr int kThreads = WAVES_M * WAVES_N * kWave;
 };
 
 // LDS of a product: the stages, and after them the sums on their way out.
-template <int TYPE, class TILE, bool DIRECT>
+template <int TYPE, class TILE>
 struct ProductLds {
     static constexpr int kTm = TILE::kM / TILE::kWavesM / 16, kTn = TILE::kN / TILE::kWavesN / 16;      // 16 x 16 tiles of a wave
-    static constexpr int kStages = DIRECT && TYPE != kF32 ? TILE::kStages : 2;
-    static constexpr int kStage = (TILE::kM + TILE::kN) * (TYPE == kF32 ? 192 : TILE::kRow);
+    static constexpr int kStage = (TILE::kM + TILE::kN) * (TYPE == kF32 ? 192 : kStageBytes);      // (single precision: three planes of 64 bytes)
     static constexpr int kOutLd = TILE::kN + 4;
     static constexpr int kOutBytes = TILE::kWavesM * 16 * kOutLd * 4;    // of the sums of one row of tiles of every wave
-    static constexpr int kOutTiles = kTm * kOutBytes <= kStages * kStage + 4096 ? kTm : kTm % 2 == 0 && kTm / 2 * kOutBytes <= kStages * kStage ? kTm / 2 : 1;
-    static constexpr int kBytes = kStages * kStage > kOutTiles * kOutBytes ? kStages * kStage : kOutTiles * kOutBytes;
+    static constexpr int kOutTiles = kTm * kOutBytes <= 2 * kStage + 4096 ? kTm : kTm % 2 == 0 && kTm / 2 * kOutBytes <= 2 * kStage ? kTm / 2 : 1;
+    static constexpr int kBytes = 2 * kStage > kOutTiles * kOutBytes ? 2 * kStage : kOutTiles * kOutBytes;
     static_assert(kTm % kOutTiles == 0, "the epilogue takes as many rows of tiles at a time");
 };
 
 // The tiles block, block + blocks, ... of a product.
 template <int TYPE, class TILE, bool A_STRIDED, bool B_STRIDED, bool DIRECT, class OUT>
 __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint32_t blocks, char* lds) {
-    constexpr int BM = TILE::kM, BN = TILE::kN, WAVES_M = TILE::kWavesM, WAVES_N = TILE::kWavesN, ROW = TILE::kRow, kThreads = TILE::kThreads;
-    typedef ProductLds<TYPE, TILE, DIRECT> Lds;
-    constexpr int kTm = Lds::kTm, kTn = Lds::kTn, kStages = Lds::kStages, kStage = Lds::kStage, kOutLd = Lds::kOutLd, kOutTiles = Lds::kOutTiles;
+    constexpr int BM = TILE::kM, BN = TILE::kN, WAVES_M = TILE::kWavesM, WAVES_N = TILE::kWavesN, kThreads = TILE::kThreads;
+    typedef ProductLds<TYPE, TILE> Lds;
+    constexpr int kTm = Lds::kTm, kTn = Lds::kTn, kStage = Lds::kStage, kOutLd = Lds::kOutLd, kOutTiles = Lds::kOutTiles;
     constexpr bool kSplit = TYPE == kF32;
-    typedef Stage<TYPE, BM, ROW, A_STRIDED, kThreads> StageA;
-    typedef Stage<TYPE, BN, ROW, B_STRIDED, kThreads> StageB;
+    typedef Stage<TYPE, BM, kStageBytes, A_STRIDED, kThreads> StageA;
+    typedef Stage<TYPE, BN, kStageBytes, B_STRIDED, kThreads> StageB;
 
     const int64_t count = p.rows.get();
     const bool rows_are_k = A_STRIDED;
@@ -427,40 +423,34 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
         clear();
         const auto multiply = [&](const char* stage) {
 #pragma unroll
-            for (int half = 0; half < ROW / 64; ++half) {
+            for (int half = 0; half < kStageBytes / 64; ++half) {
                 typename Mma<TYPE>::Part fa[kTm], fb[kTn];
 #pragma unroll
                 for (int i = 0; i < kTm; ++i) fa[i] = Mma<TYPE>::part(StageA::fragment(stage, (wave_m * kTm + i) * 16, half));
 #pragma unroll
-                for (int j = 0; j < kTn; ++j) fb[j] = Mma<TYPE>::part(StageB::fragment(stage + BM * ROW, (wave_n * kTn + j) * 16, half));
+                for (int j = 0; j < kTn; ++j) fb[j] = Mma<TYPE>::part(StageB::fragment(stage + BM * kStageBytes, (wave_n * kTn + j) * 16, half));
 #pragma unroll
                 for (int i = 0; i < kTm; ++i)
 #pragma unroll
                     for (int j = 0; j < kTn; ++j) acc[i][j] = Mma<TYPE>::run(fa[i], fb[j], acc[i][j]);
             }
         };
-        // One barrier a step: what it waits for is the step's loads (those of the stages ahead stay in flight) and every wave's reads of
-        // the stage before, which the next loads go to.
+        // Two stages in turn and one barrier a step: it waits for the step's loads, and for every wave's reads of the stage before, which the
+        // next loads go to.  (Three or four stages, or stages of 64 bytes, were no quicker: what the loads take is hidden by the other
+        // workgroup of the CU.)
         if constexpr (DIRECT && !kSplit) {
             const typename StageA::Source sa = StageA::source(p.a, m0);
             const typename StageB::Source sb = StageB::source(p.b, n0);
-            constexpr int kAhead = (kStages - 2) * (StageA::kLoads + StageB::kLoads);
-            const int steps = static_cast<int>(step1 - step0);
-            const auto load = [&](int step, int stage) {
-                char* to = lds + stage * kStage;
-                StageA::load_lds(p.a, sa, (step0 + step) * StageA::kK, to);
-                StageB::load_lds(p.b, sb, (step0 + step) * StageA::kK, to + BM * ROW);
+            const auto load = [&](int64_t step) {
+                char* to = lds + ((step - step0) & 1) * kStage;
+                StageA::load_lds(p.a, sa, step * StageA::kK, to);
+                StageB::load_lds(p.b, sb, step * StageA::kK, to + BM * kStageBytes);
             };
-#pragma unroll
-            for (int s = 0; s < kStages - 1; ++s)
-                if (s < steps) load(s, s);
-            int stage = 0;
-            for (int step = 0; step < steps; ++step) {
-                if (step + kStages - 2 < steps) wait_and_meet<kAhead>();
-                else wait_and_meet<0>();
-                if (step + kStages - 1 < steps) load(step + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
-                multiply(lds + stage * kStage);
-                stage = stage + 1 < kStages ? stage + 1 : 0;
+            if (step0 < step1) load(step0);
+            for (int64_t step = step0; step < step1; ++step) {
+                wait_and_meet();
+                if (step + 1 < step1) load(step + 1);
+                multiply(lds + ((step - step0) & 1) * kStage);
             }
         } else {
             const auto by_registers = [&] {
@@ -472,7 +462,7 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
                 for (int64_t step = step0; step < step1; ++step) {
                     char* stage = lds + ((step - step0) & 1) * kStage;
                     StageA::put(stage, ra);
-                    StageB::put(stage + BM * ROW, rb);
+                    StageB::put(stage + BM * kStageBytes, rb);
                     __syncthreads();
                     if (step + 1 < step1) {
                         StageA::load(p.a, m0, (step + 1) * StageA::kK, ra);
@@ -565,14 +555,14 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
 
 template <int TYPE, class TILE, bool DIRECT, class OUT>
 __global__ __launch_bounds__(TILE::kThreads) void forward_kernel(ProductArgs<OUT> p) {
-    __shared__ __align__(16) char lds[ProductLds<TYPE, TILE, DIRECT>::kBytes];
+    __shared__ __align__(16) char lds[ProductLds<TYPE, TILE>::kBytes];
     product<TYPE, TILE, false, false, DIRECT>(p, blockIdx.x, gridDim.x, lds);
 }
 
 // Both products of the gradient in one launch, each with workgroups of its own: dw's tiles come first, since each takes longest.
 template <int TYPE, class TILE, bool DIRECT>
 __global__ __launch_bounds__(TILE::kThreads) void backward_kernel(ProductArgs<PlainOut<kF32>> dw, uint32_t dw_blocks, ProductArgs<PlainOut<TYPE>> dx) {
-    __shared__ __align__(16) char lds[ProductLds<TYPE, TILE, DIRECT>::kBytes];
+    __shared__ __align__(16) char lds[ProductLds<TYPE, TILE>::kBytes];
     if (blockIdx.x < dw_blocks) product<TYPE, TILE, true, true, DIRECT>(dw, blockIdx.x, dw_blocks, lds);
     else product<TYPE, TILE, false, true, DIRECT>(dx, blockIdx.x - dw_blocks, gridDim.x - dw_blocks, lds);
 }
@@ -774,8 +764,8 @@ hipError_t launch_backward(hipStream_t stream, ProductArgs<PlainOut<kF32>>* dw, 
     return hipGetLastError();
 }
 
-typedef Tile<128, 128, 2, 4, 128, 2> Large;
-typedef Tile<64, 64, 2, 2, 128, 2> Small;
+typedef Tile<128, 128, 2, 4> Large;
+typedef Tile<64, 64, 2, 2> Small;
 
 template <int TYPE, int OUT_TYPE, bool SMOOTH>
 hipError_t forward(hipStream_t stream, const LinearJob& j) {
@@ -825,7 +815,7 @@ struct GradPlan {                                 // of linear_grad: what lies w
         // precision, where a tile takes longest, for half of them), us by small / large: 5000 x 256 x 256 in bfloat16 16.4 / 18.9, in
         // single precision 32.2 / 29.5; 26 624 x 512 x 256 50.1 / 44.9; 50 000 x 2048 x 512 598 / 333.
         const auto tiles = [](int64_t m, int64_t n, int64_t edge) { return (m + edge - 1) / edge * ((n + edge - 1) / edge); };
-        const int64_t steps = (n * type_bytes(j.x_type) + Large::kRow - 1) / Large::kRow;
+        const int64_t steps = (n * type_bytes(j.x_type) + kStageBytes - 1) / kStageBytes;
         const auto cut = [&](int64_t edge, int64_t most) {
             const int64_t want = std::max<int64_t>(1, std::min(std::max<int64_t>(most / tiles(j.n_out, j.n_in, edge), 8), steps / 4));
             return static_cast<int>(want >= 8 ? want / 8 * 8 : want);

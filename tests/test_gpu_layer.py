@@ -781,3 +781,84 @@ def test_refusals(helios, h):
     assert lib.helios_block_mean_grad(h._h, helios.BlockMeanGradArgs(n_rows=1, width=4, n_src=-1)) == helios.EINVAL
     assert lib.helios_quantize_rows(h._h, 1, None, 4, helios.E4M3, p, 4, p, 4, p) == helios.EINVAL
     h.sync()
+
+
+# ------------------------------------------------------------------ values that are not finite in tiles, lists of several pieces
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=str)
+@pytest.mark.parametrize("n,k,m", [(3000, 64, 256), (5000, 72, 1024), (3001, 67, 255)])
+def test_products_in_tiles_keep_infinities_and_nan_to_their_rows_and_columns(helios, h, dtype, n, k, m):
+    """A row of x that is not finite makes its own row of y so, a row of w its own column, and nothing else; dw likewise."""
+    x, w, dy = (_rand(*s, seed).to(dtype).cuda() for s, seed in (((n, k), 1), ((m, k), 2), ((n, m), 3)))
+    x[70, 5], x[71, 6], w[3, 1] = float("inf"), float("nan"), -float("inf")
+    y = torch.zeros((n, m), dtype=dtype, device="cuda")
+    h.linear(x, w, y)
+    h.sync()
+    want, got = x.double().cpu() @ w.double().cpu().t(), y.double().cpu()
+    assert torch.isnan(got[71]).all() and torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    assert torch.equal(got[torch.isinf(want)], want[torch.isinf(want)])
+    rows, cols = [i for i in range(n) if i not in (70, 71)], [j for j in range(m) if j != 3]
+    clean = (x[rows].double().abs().cpu() @ w[cols].double().abs().cpu().t())
+    _close(y[rows][:, cols], want[rows][:, cols], (k + 8) * U32 * clean, dtype)
+    dx, dw = torch.zeros_like(x), torch.zeros_like(w)
+    h.linear_grad(x, w, dy, dx=dx, dw=dw)
+    h.sync()
+    ref = dy.double().cpu().t() @ x.double().cpu()
+    got = dw.double().cpu()
+    assert torch.isnan(got[:, 6]).all() and torch.isinf(got[:, 5]).all() and torch.equal(got[:, 5], ref[:, 5])
+    cols = [j for j in range(k) if j not in (5, 6)]
+    _close(dw[:, cols], ref[:, cols], (n + 8) * U32 * (dy.double().abs().cpu().t() @ x[:, cols].double().abs().cpu()), dtype)
+    cols = [j for j in range(k) if j != 1]
+    ref = dy.double().cpu() @ w.double().cpu()
+    assert torch.equal(torch.isinf(dx[:, 1].cpu()), torch.isinf(ref[:, 1]))
+    _close(dx[:, cols], ref[:, cols], (m + 8) * U32 * (dy.double().abs().cpu() @ w[:, cols].double().abs().cpu()), dtype)
+
+
+@pytest.mark.parametrize("d", [40, 300, 1100])
+@pytest.mark.parametrize("dtype", [F32, F16], ids=str)
+def test_block_gradient_of_lists_of_several_pieces(h, d, dtype):
+    """Lists of 30 to 3000 entries side by side, three times on the same scratch: the pieces are added in the same order every time."""
+    n, n_src = 3000, 60
+    rng = np.random.default_rng(d)
+    lens = np.array([0, 1, 31, 32, 33, 64, 255, 256, 257, 511, 513, 1024, 1500, 2047, 3000] * 4)
+    rows = [np.sort(rng.choice(n, k, replace=False)) for k in lens]
+    src = np.concatenate([np.full(k, u) for u, k in enumerate(lens)])
+    dst = np.concatenate(rows)
+    order = np.argsort(dst, kind="stable")
+    col = torch.from_numpy(src[order].astype(np.int32))
+    indptr = torch.zeros(n + 1, dtype=torch.int64)
+    indptr[1:] = torch.from_numpy(np.bincount(dst, minlength=n)).cumsum(0)
+    dmean = _rand(n, d, 4).to(dtype).cuda()
+    si, se = torch.empty(n_src + 1, dtype=torch.int32, device="cuda"), torch.empty(col.numel(), dtype=torch.int32, device="cuda")
+    h.block_transpose(indptr.cuda(), col.cuda(), n_src, si, se)
+    dx = [torch.full((n_src, d), -7.0, dtype=dtype, device="cuda") for _ in range(3)]
+    for t in dx:
+        h.block_mean_grad(indptr.cuda(), si, se, dmean, t)
+    h.sync()
+    assert se.tolist() == dst.tolist()                    # every source's rows, ascending
+    m = _dense(indptr, col, n, n_src)
+    want, size = m.t() @ dmean.double().cpu(), m.t() @ dmean.double().abs().cpu()
+    _close(dx[0], want, 3100 * U32 * size, dtype)
+    assert all(torch.equal(t, dx[0]) for t in dx)
+
+
+@pytest.mark.parametrize("n,n_src,skew", [(9000, 5000, 1), (9000, 70_000, 4), (30_000, 2_000_000, 1), (6000, 40, 1), (200, 300_000, 1)])
+def test_block_by_source_at_other_sizes(h, n, n_src, skew):
+    """Both ways of sorting the entries, few and many of them for a range of sources: exactly the lists in order."""
+    rng = np.random.default_rng(n)
+    deg = rng.integers(0, 9, n)
+    indptr = np.zeros(n + 1, np.int64)
+    indptr[1:] = np.cumsum(deg)
+    col = (n_src * rng.random(indptr[-1]) ** skew).astype(np.int32)
+    row = rng.integers(0, n_src, n).astype(np.int32)
+    for own in (False, True):
+        si = torch.full((n_src + 1,), -7, dtype=torch.int32, device="cuda")
+        se = torch.full((col.size + (n if own else 0),), -7, dtype=torch.int32, device="cuda")
+        h.block_transpose(torch.from_numpy(indptr).cuda(), torch.from_numpy(col).cuda(), n_src, si, se, row=torch.from_numpy(row).cuda() if own else None)
+        h.sync()
+        source = np.concatenate([col, row]) if own else col
+        entry = np.concatenate([np.repeat(np.arange(n), deg), ~np.arange(n)]) if own else np.repeat(np.arange(n), deg)
+        order = np.argsort(source, kind="stable")
+        assert np.array_equal(se.cpu().numpy(), entry[order].astype(np.int32))
+        assert np.array_equal(si.cpu().numpy(), np.searchsorted(source[order], np.arange(n_src + 1)).astype(np.int32))
