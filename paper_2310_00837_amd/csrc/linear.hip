@@ -75,7 +75,8 @@ struct Operand {
 };
 
 // One operand's share of a stage: WIDTH rows of ROW bytes of k, or (STRIDED) as many k-strided rows of WIDTH columns.
-template <int TYPE, int WIDTH, int ROW, bool STRIDED, int THREADS>
+// (SWIZZLED: the order in which threads take the chunks is that of LDS; else that of memory.)
+template <int TYPE, int WIDTH, int ROW, bool STRIDED, int THREADS, bool SWIZZLED = true>
 struct Stage {
     static constexpr int kBytes = type_bytes(TYPE);
     static constexpr int kPer = 16 / kBytes;      // elements of a chunk
@@ -90,30 +91,24 @@ struct Stage {
         if (kBytes == 4) return ((row >> 2) & 3) << 2;
         return ((row & 3) | (((row >> 3) & 1) << 2)) % (kRowChunks / 2) << 1;
     }
-    // the chunks that thread t stages, from the tile whose first row (or column) is `first` and whose first k is k0
-    static __device__ __forceinline__ void load(const Operand& o, int64_t first, int64_t k0, i32x4 (&regs)[kLoads]) {
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) {
-            const uint32_t q = threadIdx.x + l * THREADS, row = q / kRowChunks, chunk = (q % kRowChunks) ^ swizzle(row);
-            const int64_t r = (STRIDED ? k0 : first) + row, c = (STRIDED ? first : k0) + chunk * kPer;
-            regs[l] = i32x4{0, 0, 0, 0};
-            if (r < o.rows && c < o.cols) regs[l] = load_16_of<kBytes>(o.data + r * o.ld + c * kBytes, o.cols - c);
-        }
-    }
-    // The same straight into LDS, without a trip through registers: for rows of 16-byte multiples at 16-byte addresses.  Chunks of
-    // rows that do not exist are taken from the last that does (whatever they hold stays in rows and columns that are not
-    // written); chunks of k that do not exist are zeros.
+    // Where the chunks that a thread stages begin, for the tile whose first row (k-strided: column) is `first`.  Chunks of rows or columns
+    // that do not exist are taken from the last that does: whatever they hold stays in rows and columns that are not written.
+    // Chunks of k that do not exist are zeros.
     struct Source {
         const char* at[kLoads];
+        int valid[STRIDED ? kLoads : 1];          // elements of the chunk that exist (rows of any width)
     };
+    static __device__ __forceinline__ uint32_t row_of(int l) { return (threadIdx.x + l * THREADS) / kRowChunks; }
+    static __device__ __forceinline__ uint32_t chunk_of(int l) { return ((threadIdx.x + l * THREADS) % kRowChunks) ^ (SWIZZLED ? swizzle(row_of(l)) : 0u); }
     static __device__ __forceinline__ Source source(const Operand& o, int64_t first) {
         Source s;
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) {
-            const uint32_t q = threadIdx.x + l * THREADS, row = q / kRowChunks, chunk = (q % kRowChunks) ^ swizzle(row);
+            const uint32_t row = row_of(l), chunk = chunk_of(l);
             if (STRIDED) {
-                const int64_t c = first + chunk * kPer, last = o.cols - kPer;
-                s.at[l] = o.data + row * o.ld + (c < last ? c : last) * kBytes;
+                const int64_t c = first + chunk * kPer, last = (o.cols - 1) / kPer * kPer, at = c < last ? c : last;
+                s.at[l] = o.data + row * o.ld + at * kBytes;
+                s.valid[l] = o.cols - at < kPer ? static_cast<int>(o.cols - at) : kPer;
             } else {
                 const int64_t r = first + row, last = o.rows - 1;
                 s.at[l] = o.data + (r < last ? r : last) * o.ld + chunk * 16;
@@ -121,16 +116,34 @@ struct Stage {
         }
         return s;
     }
+    // The stage whose first k is k0, into registers: rows of any width and alignment (WHOLE: of whole chunks at 16-byte addresses).
+    template <bool WHOLE>
+    static __device__ __forceinline__ void load(const Operand& o, const Source& s, int64_t k0, i32x4 (&regs)[kLoads]) {
+        const int64_t step = STRIDED ? k0 * o.ld : k0 * kBytes, left = (STRIDED ? o.rows : o.cols) - k0;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            const char* at = s.at[l] + step;
+            const int64_t there = left - (STRIDED ? row_of(l) : chunk_of(l) * kPer);       // of k
+            if (WHOLE) {
+                if (left < kK && there <= 0) at = reinterpret_cast<const char*>(&kZeroChunk);
+                regs[l] = *reinterpret_cast<const i32x4*>(at);
+            } else if (STRIDED) {
+                regs[l] = i32x4{0, 0, 0, 0};
+                if (left >= kK || there > 0) regs[l] = load_16_of<kBytes>(at, s.valid[l]);
+            } else {
+                if (left >= kK) regs[l] = load_16(at);
+                else regs[l] = load_16_of<kBytes>(at, there);
+            }
+        }
+    }
+    // The same straight into LDS, without a trip through registers, for rows of whole chunks at 16-byte addresses.
     static __device__ __forceinline__ void load_lds(const Operand& o, const Source& s, int64_t k0, char* lds) {
         const int64_t step = STRIDED ? k0 * o.ld : k0 * kBytes, left = (STRIDED ? o.rows : o.cols) - k0;
         const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) {
             const char* p = s.at[l] + step;
-            if (left < kK) {
-                const uint32_t q = threadIdx.x + l * THREADS, row = q / kRowChunks, chunk = (q % kRowChunks) ^ swizzle(row);
-                if (static_cast<int64_t>(STRIDED ? row : chunk * kPer) >= left) p = reinterpret_cast<const char*>(&kZeroChunk);
-            }
+            if (left < kK && static_cast<int64_t>(STRIDED ? row_of(l) : chunk_of(l) * kPer) >= left) p = reinterpret_cast<const char*>(&kZeroChunk);
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
                                              (__attribute__((address_space(3))) void*)(lds + (wave * kWave + l * THREADS) * 16), 16, 0, 0);
         }
@@ -181,53 +194,15 @@ struct SplitPart {
 };
 template <int WIDTH, bool STRIDED, int THREADS>
 struct SplitStage {
-    typedef Stage<kF32, WIDTH, 128, STRIDED, THREADS> Whole;
+    typedef Stage<kF32, WIDTH, 128, STRIDED, THREADS, false> Whole;                  // (loads and their order; its stage is not used)
     typedef Stage<kBF16, WIDTH, 64, STRIDED, THREADS> Plane;
     static constexpr int kLoads = Whole::kLoads, kPlane = WIDTH * 64;
-    static __device__ __forceinline__ void load(const Operand& o, int64_t first, int64_t k0, i32x4 (&regs)[kLoads]) {
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) {
-            const uint32_t q = threadIdx.x + l * THREADS, row = q / Whole::kRowChunks, chunk = q % Whole::kRowChunks;
-            const int64_t r = (STRIDED ? k0 : first) + row, c = (STRIDED ? first : k0) + chunk * 4;
-            regs[l] = i32x4{0, 0, 0, 0};
-            if (r < o.rows && c < o.cols) regs[l] = load_16_of<4>(o.data + r * o.ld + c * 4, o.cols - c);
-        }
-    }
-    // the same for rows of whole chunks at 16-byte addresses (see Stage::source)
-    struct Source {
-        const char* at[kLoads];
-    };
-    static __device__ __forceinline__ Source source(const Operand& o, int64_t first) {
-        Source s;
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) {
-            const uint32_t q = threadIdx.x + l * THREADS, row = q / Whole::kRowChunks, chunk = q % Whole::kRowChunks;
-            if (STRIDED) {
-                const int64_t c = first + chunk * 4, last = o.cols - 4;
-                s.at[l] = o.data + row * o.ld + (c < last ? c : last) * 4;
-            } else {
-                const int64_t r = first + row, last = o.rows - 1;
-                s.at[l] = o.data + (r < last ? r : last) * o.ld + chunk * 16;
-            }
-        }
-        return s;
-    }
-    static __device__ __forceinline__ void load(const Operand& o, const Source& s, int64_t k0, i32x4 (&regs)[kLoads]) {
-        const int64_t step = STRIDED ? k0 * o.ld : k0 * 4, left = (STRIDED ? o.rows : o.cols) - k0;
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) {
-            const uint32_t q = threadIdx.x + l * THREADS, row = q / Whole::kRowChunks, chunk = q % Whole::kRowChunks;
-            const char* at = s.at[l] + step;
-            if (left < Whole::kK && static_cast<int64_t>(STRIDED ? row : chunk * 4) >= left) at = reinterpret_cast<const char*>(&kZeroChunk);
-            regs[l] = *reinterpret_cast<const i32x4*>(at);
-        }
-    }
     // spoilt: 0, until a value is not finite
     static __device__ __forceinline__ void put(char* lds, const i32x4 (&regs)[kLoads], float* spoilt) {
         typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) {
-            const uint32_t q = threadIdx.x + l * THREADS, row = q / Whole::kRowChunks, chunk = q % Whole::kRowChunks;
+            const uint32_t row = Whole::row_of(l), chunk = Whole::chunk_of(l);
             uint32_t part[3][4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -336,6 +311,7 @@ template <int OUT_TYPE>
 struct PlainOut {                                 // (slice: which part of k the sums are of)
     void* y;
     int64_t ld, slice_stride;
+    bool in_32_bits;                              // the sums are parts of a sum
     struct Columns {
         int64_t at;
         int32_t valid;
@@ -343,7 +319,10 @@ struct PlainOut {                                 // (slice: which part of k the
     __device__ __forceinline__ Columns at(int32_t col, int valid, int slice) const { return Columns{slice * slice_stride + col, valid}; }
     struct Ahead {};
     __device__ __forceinline__ Ahead ahead(const Columns&, int64_t) const { return Ahead{}; }
-    __device__ __forceinline__ void row(const Columns& c, const Ahead&, int64_t row, float (&v)[8]) const { store_8_of<OUT_TYPE>(y, c.at + row * ld, c.valid, v); }
+    __device__ __forceinline__ void row(const Columns& c, const Ahead&, int64_t row, float (&v)[8]) const {
+        if (in_32_bits) store_8_of<kF32>(y, c.at + row * ld, c.valid, v);
+        else store_8_of<OUT_TYPE>(y, c.at + row * ld, c.valid, v);
+    }
 };
 
 template <class OUT>
@@ -438,9 +417,9 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
         // Two stages in turn and one barrier a step: it waits for the step's loads, and for every wave's reads of the stage before, which the
         // next loads go to.  (Three or four stages, or stages of 64 bytes, were no quicker: what the loads take is hidden by the other
         // workgroup of the CU.)
+        const typename StageA::Source sa = StageA::source(p.a, m0);
+        const typename StageB::Source sb = StageB::source(p.b, n0);
         if constexpr (DIRECT && !kSplit) {
-            const typename StageA::Source sa = StageA::source(p.a, m0);
-            const typename StageB::Source sb = StageB::source(p.b, n0);
             const auto load = [&](int64_t step) {
                 char* to = lds + ((step - step0) & 1) * kStage;
                 StageA::load_lds(p.a, sa, step * StageA::kK, to);
@@ -456,8 +435,8 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
             const auto by_registers = [&] {
                 i32x4 ra[StageA::kLoads], rb[StageB::kLoads];
                 if (step0 < step1) {
-                    StageA::load(p.a, m0, step0 * StageA::kK, ra);
-                    StageB::load(p.b, n0, step0 * StageA::kK, rb);
+                    StageA::template load<DIRECT>(p.a, sa, step0 * StageA::kK, ra);
+                    StageB::template load<DIRECT>(p.b, sb, step0 * StageA::kK, rb);
                 }
                 for (int64_t step = step0; step < step1; ++step) {
                     char* stage = lds + ((step - step0) & 1) * kStage;
@@ -465,8 +444,8 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
                     StageB::put(stage + BM * kStageBytes, rb);
                     __syncthreads();
                     if (step + 1 < step1) {
-                        StageA::load(p.a, m0, (step + 1) * StageA::kK, ra);
-                        StageB::load(p.b, n0, (step + 1) * StageA::kK, rb);
+                        StageA::template load<DIRECT>(p.a, sa, (step + 1) * StageA::kK, ra);
+                        StageB::template load<DIRECT>(p.b, sb, (step + 1) * StageA::kK, rb);
                     }
                     multiply(stage);
                 }
@@ -474,19 +453,13 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
             if constexpr (kSplit) {
                 typedef SplitStage<BM, A_STRIDED, kThreads> SplitA;
                 typedef SplitStage<BN, B_STRIDED, kThreads> SplitB;
-                typename SplitA::Source sa;
-                typename SplitB::Source sb;
-                if constexpr (DIRECT) sa = SplitA::source(p.a, m0), sb = SplitB::source(p.b, n0);
+                const typename SplitA::Whole::Source split_a = SplitA::Whole::source(p.a, m0);
+                const typename SplitB::Whole::Source split_b = SplitB::Whole::source(p.b, n0);
                 i32x4 ra[SplitA::kLoads], rb[SplitB::kLoads];
                 float spoilt = 0.0f;
                 const auto load = [&](int64_t step) {
-                    if constexpr (DIRECT) {
-                        SplitA::load(p.a, sa, step * StageA::kK, ra);
-                        SplitB::load(p.b, sb, step * StageA::kK, rb);
-                    } else {
-                        SplitA::load(p.a, m0, step * StageA::kK, ra);
-                        SplitB::load(p.b, n0, step * StageA::kK, rb);
-                    }
+                    SplitA::Whole::template load<DIRECT>(p.a, split_a, step * StageA::kK, ra);
+                    SplitB::Whole::template load<DIRECT>(p.b, split_b, step * StageA::kK, rb);
                 };
                 const auto put = [&](int64_t step) {
                     char* stage = lds + ((step - step0) & 1) * kStage;
@@ -553,15 +526,19 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
     }
 }
 
+// Waves of a SIMD that the registers are to leave room for: two workgroups to a CU where LDS has room for two (single precision: one).
+template <int TYPE, class TILE>
+constexpr int waves_that_fit() { return TYPE == kF32 ? 1 : TILE::kThreads / kWave / 2; }
+
 template <int TYPE, class TILE, bool DIRECT, class OUT>
-__global__ __launch_bounds__(TILE::kThreads) void forward_kernel(ProductArgs<OUT> p) {
+__global__ __launch_bounds__(TILE::kThreads, (waves_that_fit<TYPE, TILE>())) void forward_kernel(ProductArgs<OUT> p) {
     __shared__ __align__(16) char lds[ProductLds<TYPE, TILE>::kBytes];
     product<TYPE, TILE, false, false, DIRECT>(p, blockIdx.x, gridDim.x, lds);
 }
 
 // Both products of the gradient in one launch, each with workgroups of its own: dw's tiles come first, since each takes longest.
 template <int TYPE, class TILE, bool DIRECT>
-__global__ __launch_bounds__(TILE::kThreads) void backward_kernel(ProductArgs<PlainOut<kF32>> dw, uint32_t dw_blocks, ProductArgs<PlainOut<TYPE>> dx) {
+__global__ __launch_bounds__(TILE::kThreads, (waves_that_fit<TYPE, TILE>())) void backward_kernel(ProductArgs<PlainOut<TYPE>> dw, uint32_t dw_blocks, ProductArgs<PlainOut<TYPE>> dx) {
     __shared__ __align__(16) char lds[ProductLds<TYPE, TILE>::kBytes];
     if (blockIdx.x < dw_blocks) product<TYPE, TILE, true, true, DIRECT>(dw, blockIdx.x, dw_blocks, lds);
     else product<TYPE, TILE, false, true, DIRECT>(dx, blockIdx.x - dw_blocks, gridDim.x - dw_blocks, lds);
@@ -628,6 +605,7 @@ struct SlopeArgs {
     void* dz;                                     // nullable
     int64_t dz_ld;
     float* sums;                                  // [gridDim.y][n], nullable
+    void* dbias;                                  // with one row of workgroups: where their sums go at once, in `type`
 };
 // (LANES threads share a row of the workgroup's columns, eight each; the others go through the rows)
 template <int TYPE, int Z_TYPE, bool SLOPE, int LANES>
@@ -657,7 +635,7 @@ __global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
                 if (p.dz) store_8_of<Z_TYPE>(p.dz, (row + kSubs * k) * p.dz_ld + col, valid, d[k]);
             }
         }
-    if (!p.sums) return;
+    if (!p.sums && !p.dbias) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[sub][lane * 8 + e] = sum[e];
     __syncthreads();
@@ -665,7 +643,8 @@ __global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
         float t = 0;
 #pragma unroll 16
         for (int k = 0; k < kSubs; ++k) t += s[k][threadIdx.x];
-        p.sums[static_cast<int64_t>(blockIdx.y) * p.n + blockIdx.x * kCols + threadIdx.x] = t;
+        if (p.dbias) store_1(TYPE, p.dbias, blockIdx.x * kCols + threadIdx.x, t);
+        else p.sums[static_cast<int64_t>(blockIdx.y) * p.n + blockIdx.x * kCols + threadIdx.x] = t;
     }
 }
 
@@ -743,8 +722,8 @@ hipError_t launch_forward(hipStream_t stream, ProductArgs<OUT> p) {
 
 // dw and dx: nullptr if not asked for
 template <int TYPE, class TILE>
-hipError_t launch_backward(hipStream_t stream, ProductArgs<PlainOut<kF32>>* dw, ProductArgs<PlainOut<TYPE>>* dx) {
-    ProductArgs<PlainOut<kF32>> w{};
+hipError_t launch_backward(hipStream_t stream, ProductArgs<PlainOut<TYPE>>* dw, ProductArgs<PlainOut<TYPE>>* dx) {
+    ProductArgs<PlainOut<TYPE>> w{};
     ProductArgs<PlainOut<TYPE>> x{};
     uint32_t dw_blocks = 0, dx_blocks = 0;
     bool straight = true;
@@ -798,6 +777,7 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
     return j.act == kActGelu || j.act == kActSilu ? forward<TYPE, OUT_TYPE, true>(stream, j) : forward<TYPE, OUT_TYPE, false>(stream, j);
 }
 
+constexpr int64_t kOneSliceRows = 256;
 struct GradPlan {                                 // of linear_grad: what lies where in the scratch, and how far k is cut up
     bool needs_dz, large;                         // large: by large tiles
     int64_t dz_ld;
@@ -824,6 +804,8 @@ struct GradPlan {                                 // of linear_grad: what lies w
         large = (j.dx ? tiles(n, j.n_in, 128) : 0) + (j.dw ? tiles(j.n_out, j.n_in, 128) * slices : 0) >= (j.x_type == kF32 ? 128 : 256);
         if (!large) slices = cut(64, 1024);
         slope_blocks = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((n + 31) / 32, 512)));
+        // (few rows: one slice, whose sums need no joining; a launch less)
+        if (n <= kOneSliceRows) slices = 1, slope_blocks = 1;
         dz = 0;
         part = dz + (needs_dz ? up(static_cast<size_t>(n * dz_ld) * type_bytes(j.x_type)) : 0);
         sums = part + (j.dw ? up(static_cast<size_t>(slices) * j.n_out * j.n_in * sizeof(float)) : 0);
@@ -850,7 +832,7 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
     hipError_t e = hipSuccess;
     if (plan.needs_dz || j.dbias) {
         SlopeArgs s{j.rows, j.n_out, j.act, j.dy, j.dy_ld, j.pre, j.pre_ld, plan.needs_dz ? scratch + plan.dz : nullptr, plan.dz_ld,
-                    j.dbias ? reinterpret_cast<float*>(scratch + plan.sums) : nullptr};
+                    j.dbias && plan.slope_blocks > 1 ? reinterpret_cast<float*>(scratch + plan.sums) : nullptr, plan.slope_blocks > 1 ? nullptr : j.dbias};
         e = j.n_out <= 32 ? launch_slope<TYPE, 4>(stream, s, j, plan.slope_blocks) : launch_slope<TYPE, 16>(stream, s, j, plan.slope_blocks);
     }
     const bool has_dx = j.dx && j.rows.host > 0;
@@ -863,8 +845,8 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         x.k = j.n_out;
         x.rows = j.rows;
         x.slices = 1;
-        x.out = PlainOut<TYPE>{j.dx, j.dx_ld, 0};
-        ProductArgs<PlainOut<kF32>> w{};
+        x.out = PlainOut<TYPE>{j.dx, j.dx_ld, 0, false};
+        ProductArgs<PlainOut<TYPE>> w{};
         w.a = x.a;
         w.b = operand(j.x, j.x_ld, TYPE, j.rows.host, j.n_in);
         w.m = j.n_out;
@@ -872,13 +854,14 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         w.k = j.rows.host;
         w.rows = j.rows;
         w.slices = plan.slices;
-        w.out = PlainOut<kF32>{scratch + plan.part, j.n_in, static_cast<int64_t>(j.n_out) * j.n_in};
+        w.out = plan.slices > 1 ? PlainOut<TYPE>{scratch + plan.part, j.n_in, static_cast<int64_t>(j.n_out) * j.n_in, true} : PlainOut<TYPE>{j.dw, j.dw_ld, 0, false};
         e = plan.large ? launch_backward<TYPE, Large>(stream, j.dw ? &w : nullptr, has_dx ? &x : nullptr)
                        : launch_backward<TYPE, Small>(stream, j.dw ? &w : nullptr, has_dx ? &x : nullptr);
     }
-    if (e == hipSuccess && (j.dw || j.dbias)) {
+    const bool join_dw = j.dw && plan.slices > 1, join_dbias = j.dbias && plan.slope_blocks > 1;
+    if (e == hipSuccess && (join_dw || join_dbias)) {
         JoinArgs a{};
-        if (j.dw) {
+        if (join_dw) {
             a.part = reinterpret_cast<const float*>(scratch + plan.part);
             a.cells = static_cast<int64_t>(j.n_out) * j.n_in;
         }
@@ -894,7 +877,7 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         a.n_sums = static_cast<int>(plan.slope_blocks);
         a.sum_type = j.out_type;
         a.sum_out = j.dbias;
-        const uint32_t blocks = a.cell_blocks + (j.dbias ? tiles_of(j.n_out, kSumColumns) : 0);
+        const uint32_t blocks = a.cell_blocks + (join_dbias ? tiles_of(j.n_out, kSumColumns) : 0);
         hipLaunchKernelGGL(join_kernel, dim3(blocks), dim3(kBlock), 0, stream, a);
         e = hipGetLastError();
     }
