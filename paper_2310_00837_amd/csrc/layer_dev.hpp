@@ -67,6 +67,24 @@ __device__ __forceinline__ void widen_8(const i32x4 (&raw)[type_bytes(TYPE) / 2]
         }
     }
 }
+// Eight elements as they are in memory, in half the registers where they have 16 bits; zeros where there are none.
+template <int TYPE>
+struct Raw8 {
+    i32x4 v[type_bytes(TYPE) / 2];
+    __device__ __forceinline__ void load(const void* base, int64_t at, int valid) {
+        constexpr int kBytes = type_bytes(TYPE), kPer = 16 / kBytes;
+        const char* p = static_cast<const char*>(base) + at * kBytes;
+#pragma unroll
+        for (int k = 0; k < 8 / kPer; ++k) {
+            v[k] = i32x4{0, 0, 0, 0};
+            if (valid > k * kPer) v[k] = load_16_of<kBytes>(p + 16 * k, valid - k * kPer);
+        }
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int k = 0; k < type_bytes(TYPE) / 2; ++k) v[k] = i32x4{0, 0, 0, 0};
+    }
+};
 // ... or from memory
 template <int TYPE>
 __device__ __forceinline__ void load_8(const void* base, int64_t at, float (&v)[8]) {

@@ -46,16 +46,13 @@ __device__ __forceinline__ void copy_8_of(const void* from, int64_t at, void* to
     }
 }
 
-// Eight columns of a row that may be asked for in vain: zeros then.  (One branch, so that a group whose list is shorter than what is
-// asked for together does not go through the elements one by one.)
+// sum += eight columns of a row, times weight
 template <int TYPE>
-__device__ __forceinline__ void load_row_8(const void* base, int64_t at, bool wanted, int valid, float (&v)[8]) {
+__device__ __forceinline__ void add_8(const Raw8<TYPE>& row, float weight, float (&sum)[8]) {
+    float v[8];
+    widen_8<TYPE>(row.v, v);
 #pragma unroll
-    for (int c = 0; c < 8; ++c) v[c] = 0;
-    if (wanted) {
-        if (valid >= 8) load_8<TYPE>(base, at, v);
-        else load_8_of<TYPE>(base, at, valid, v);
-    }
+    for (int c = 0; c < 8; ++c) sum[c] += v[c] * weight;
 }
 
 template <int TYPE, int LANES>
@@ -75,19 +72,18 @@ __global__ __launch_bounds__(kBlock) void block_mean_kernel(MeanJob p) {
         const int64_t end = fits ? list.hi : list.lo;
         for (int64_t e = list.lo; e < end; e += kMeanAhead) {
             int32_t src[kMeanAhead];
-            float v[kMeanAhead][8];
+            Raw8<TYPE> v[kMeanAhead];
 #pragma unroll
             for (int k = 0; k < kMeanAhead; ++k) src[k] = p.col[e + k < end ? e + k : e];
 #pragma unroll
             for (int k = 0; k < kMeanAhead; ++k) {
                 const bool good = static_cast<uint32_t>(src[k]) < static_cast<uint64_t>(p.n_src);
                 if (!good) raise(p.err, kErrData);
-                load_row_8<TYPE>(p.x, static_cast<int64_t>(src[k]) * p.x_ld + col, e + k < end && good, valid, v[k]);
+                v[k].clear();                     // (rows asked for in vain: zeros)
+                if (e + k < end && good) v[k].load(p.x, static_cast<int64_t>(src[k]) * p.x_ld + col, valid);
             }
 #pragma unroll
-            for (int k = 0; k < kMeanAhead; ++k)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) sum[c] += v[k][c];
+            for (int k = 0; k < kMeanAhead; ++k) add_8<TYPE>(v[k], 1.0f, sum);
         }
         const float weight = 1.0f / (end > list.lo ? static_cast<float>(end - list.lo) : 1.0f);
     #pragma unroll
@@ -172,10 +168,10 @@ constexpr int kRangeBlock = 1024, kRangeMost = 1024, kRangeHeld = 8192, kRangeSt
 struct RangeLds {
     unsigned long long held[kRangeHeld];          // (source in the range, place)
     uint32_t count[kRangeMost];                   // of a source; then where its next entry goes
-    uint32_t taken[kRangeMost], placed[kRangeBlock];
+    uint32_t taken[kRangeMost];
     int32_t step[kRangeSteps + 1];                // indptr at every stride-th row
     uint32_t wave[kRangeBlock / kWave];
-    uint32_t n_held, below;
+    uint32_t n_held, below, longest;
 };
 
 // held[0, n) in ascending order, n <= 2^bits; the words from n on are the largest there is.
@@ -210,7 +206,7 @@ __global__ __launch_bounds__(kRangeBlock) void transpose_range_kernel(TransposeA
     const uint32_t steps = static_cast<uint32_t>((count + stride - 1) / stride);
     for (uint32_t i = t; i < steps; i += kRangeBlock) s.step[i] = static_cast<int32_t>(p.indptr[static_cast<int64_t>(i) * stride]);
     for (uint32_t i = t; i < sources; i += kRangeBlock) s.count[i] = s.taken[i] = 0;
-    if (t == 0) s.n_held = 0, s.below = 0;
+    if (t == 0) s.n_held = s.below = s.longest = 0;
     __syncthreads();
 
     const auto source = [&](uint32_t place) { return place < n_col ? p.col[place] : p.row[place - n_col]; };
@@ -254,6 +250,7 @@ __global__ __launch_bounds__(kRangeBlock) void transpose_range_kernel(TransposeA
     __syncthreads();
     // counts -> where a source's entries begin (a thread to a source)
     const uint32_t mine = t < sources ? s.count[t] : 0, upto = dpp_inclusive_scan(mine);
+    if (mine > kRangeBlock) atomicMax(&s.longest, mine);
     if (lane_id() == kWave - 1) s.wave[wave_id()] = upto;
     __syncthreads();
     uint32_t begin = s.below + upto - mine;
@@ -300,21 +297,31 @@ __global__ __launch_bounds__(kRangeBlock) void transpose_range_kernel(TransposeA
         }
         __syncthreads();
     };
-    if (found <= kRangeBlock) {                   // few: they are put together by source, and an entry counts those of its source before it
-        uint32_t local = 0, place = 0, at = 0;
-        if (t < found) {
-            local = static_cast<uint32_t>(s.held[t] >> 32);
-            place = static_cast<uint32_t>(s.held[t]);
-            at = s.count[local] - s.below;
-            s.placed[at + atomicAdd(&s.taken[local], 1u)] = place;
+    if (found <= kRangeHeld && s.longest <= kRangeBlock) {
+        // They are put together by source (in the memory that held them), and an entry counts those of its source that come before it.
+        constexpr int kEach = kRangeHeld / kRangeBlock;
+        unsigned long long mine[kEach];
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) mine[q] = t + q * kRangeBlock < found ? s.held[t + q * kRangeBlock] : 0;
+        __syncthreads();
+        uint32_t* placed = reinterpret_cast<uint32_t*>(s.held);
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            if (t + q * kRangeBlock >= found) continue;
+            const uint32_t local = static_cast<uint32_t>(mine[q] >> 32);
+            placed[s.count[local] - s.below + atomicAdd(&s.taken[local], 1u)] = static_cast<uint32_t>(mine[q]);
         }
         __syncthreads();
-        if (t < found) {
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            if (t + q * kRangeBlock >= found) continue;
+            const uint32_t local = static_cast<uint32_t>(mine[q] >> 32), place = static_cast<uint32_t>(mine[q]);
+            const uint32_t begin = s.count[local] - s.below, end = begin + s.taken[local];
             uint32_t before = 0;
-            const uint32_t end = at + s.taken[local];
 #pragma unroll 4
-            for (uint32_t i = at; i < end; ++i) before += s.placed[i] < place;
-            if (s.count[local] + before < a.n) p.src_entry[s.count[local] + before] = place < n_col ? row_of(place) : ~static_cast<int32_t>(place - n_col);
+            for (uint32_t i = begin; i < end; ++i) before += placed[i] < place;
+            const uint32_t to = s.count[local] + before;
+            if (to < a.n) p.src_entry[to] = place < n_col ? row_of(place) : ~static_cast<int32_t>(place - n_col);
         }
         return;
     }
@@ -360,7 +367,7 @@ struct GradScratch {
 
 // An entry's share of the gradient: a row of dmean and 1 / its samples, or of down and 1; nothing and an error if there is no such row.
 template <int TYPE>
-__device__ __forceinline__ void share_of(const MeanGradJob& p, int32_t entry, bool wanted, int col, int valid, float (&v)[8], float* weight) {
+__device__ __forceinline__ void share_of(const MeanGradJob& p, int32_t entry, bool wanted, int col, int valid, Raw8<TYPE>& v, float* weight) {
     const bool own = entry < 0;
     const int64_t row = own ? ~entry : entry;
     const bool good = row < p.n_rows && (!own || p.down);
@@ -370,22 +377,22 @@ __device__ __forceinline__ void share_of(const MeanGradJob& p, int32_t entry, bo
         const RowBounds list = row_bounds(p.indptr, static_cast<uint32_t>(row));
         *weight = 1.0f / static_cast<float>(list.hi - list.lo);
     }
-    load_row_8<TYPE>(own ? p.down : p.dmean, row * (own ? p.down_ld : p.dmean_ld) + col, wanted && good, valid, v);
+    v.clear();
+    if (wanted && good) v.load(own ? p.down : p.dmean, row * (own ? p.down_ld : p.dmean_ld) + col, valid);
 }
 // sum += the shares of the entries [lo, hi), AHEAD at a time, in order
 template <int TYPE, int AHEAD>
 __device__ __forceinline__ void add_shares(const MeanGradJob& p, int32_t lo, int32_t hi, int col, int valid, float (&sum)[8]) {
     for (int32_t k0 = lo; k0 < hi; k0 += AHEAD) {
         int32_t entry[AHEAD];
-        float v[AHEAD][8], weight[AHEAD];
+        Raw8<TYPE> v[AHEAD];
+        float weight[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) entry[k] = p.src_entry[k0 + k < hi ? k0 + k : k0];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) share_of<TYPE>(p, entry[k], k0 + k < hi, col, valid, v[k], &weight[k]);
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-            for (int c = 0; c < 8; ++c) sum[c] += v[k][c] * weight[k];
+        for (int k = 0; k < AHEAD; ++k) add_8<TYPE>(v[k], weight[k], sum);
     }
 }
 
@@ -529,7 +536,7 @@ struct RunMeanGrad {
     }
 };
 
-constexpr int64_t kRangePlaces = 1 << 16;
+constexpr int64_t kRangePlaces = 1 << 17;
 struct TransposePlan {
     int64_t n, ranges;                            // (ranges: 0 by a sort)
     size_t keys, entry, order, sort, bytes;

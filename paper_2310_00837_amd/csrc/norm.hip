@@ -155,21 +155,6 @@ struct GradShape {
     static constexpr int kThreads = LANES <= kWave && CHUNKS == 1 ? 1024 : RowShape<LANES>::kThreads, kRows = kThreads / LANES;
     static constexpr int kMostBlocks = kThreads == 1024 ? 256 : 1024;
 };
-// eight elements as they are in memory; zeros where there are none
-template <int TYPE>
-struct Raw8 {
-    i32x4 v[type_bytes(TYPE) / 2];
-    __device__ __forceinline__ void load(const void* base, int64_t at, int valid) {
-        constexpr int kBytes = type_bytes(TYPE), kPer = 16 / kBytes;
-        const char* p = static_cast<const char*>(base) + at * kBytes;
-#pragma unroll
-        for (int k = 0; k < 8 / kPer; ++k) {
-            v[k] = i32x4{0, 0, 0, 0};
-            if (valid > k * kPer) v[k] = load_16_of<kBytes>(p + 16 * k, valid - k * kPer);
-        }
-    }
-};
-
 // Every workgroup goes through rows blockIdx.x * kRows + ..., asks for a row while the one before it is worked on (rows of up to
 // eight elements a lane: more would not fit the registers), and keeps its lanes' sums for dgain until the end.
 template <int TYPE, int LANES, int CHUNKS>
