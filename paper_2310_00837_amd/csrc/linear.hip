@@ -745,6 +745,7 @@ hipError_t launch_backward(hipStream_t stream, ProductArgs<PlainOut<TYPE>>* dw, 
 
 typedef Tile<128, 128, 2, 4> Large;
 typedef Tile<64, 64, 2, 2> Small;
+typedef Tile<160, 128, 2, 2> Tall;
 
 template <int TYPE, int OUT_TYPE, bool SMOOTH>
 hipError_t forward(hipStream_t stream, const LinearJob& j) {
@@ -768,6 +769,13 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
         const dim3 grid(tiles_of(p.n, 16), tiles_of(p.m, 16));
         hipLaunchKernelGGL((product_few_kernel<TYPE, Out>), grid, dim3(kFewWaves * kWave), 0, stream, p);
         return hipGetLastError();
+    }
+    // Large lists of 16-bit elements: the height of tile that leaves the last round fullest, two tiles to a CU at a time (one of 160 rows takes a
+    // quarter longer than one of 128).  us, 128 / 160 rows: 100 000 x 2048 x 512 324 / 303, 60 000 176 / 163, 30 000 x 2048 x 1024 152 / 138,
+    // but with short k, where the epilogue weighs more, 100 000 x 256 x 512 62.6 / 66.2.
+    if constexpr (TYPE == kF16 || TYPE == kBF16) {
+        const auto rounds = [&](int height) { return (static_cast<int64_t>(tiles_of(p.m, height)) * tiles_of(p.n, 128) + 511) / 512 * height; };
+        if (steps > 8 && rounds(128) > 256 && rounds(160) < rounds(128)) return launch_forward<TYPE, Tall>(stream, p);
     }
     if (static_cast<int64_t>(tiles_of(p.m, 128)) * tiles_of(p.n, 128) >= 256) return launch_forward<TYPE, Large>(stream, p);
     return launch_forward<TYPE, Small>(stream, p);
