@@ -48,7 +48,6 @@ size_t linear_grad_scratch_bytes(const LinearGradJob& job);
 hipError_t launch_linear_grad(hipStream_t stream, const LinearGradJob& job, void* scratch);
 
 // ---- norm.hip
-constexpr int kNormMaxWidth = 32768;
 struct NormJob {
     Count rows;
     int32_t width;

@@ -139,8 +139,8 @@ __device__ __forceinline__ void store_1(int type, void* base, int64_t at, float 
 }
 
 // The normal distribution's Phi(z) and density at z, by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: erfc(u) =
-// (a1 t + ... + a5 t^5) exp(-u^2), t = 1 / (1 + p u), off by at most 1.5e-7.  One exponential serves both (the library's erff
-// took three times as long: it is what the gradient's first step was bound by).
+// (a1 t + ... + a5 t^5) exp(-u^2), t = 1 / (1 + p u), off by at most 1.5e-7, which is what the sums of a layer in single
+// precision are off by, too.  One exponential serves both.
 __device__ __forceinline__ float normal_cdf(float z, float* density) {
     const float u = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * u), e = __expf(-u * u);
     const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));

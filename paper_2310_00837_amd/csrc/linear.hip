@@ -7,7 +7,14 @@
 // A stage of an operand is 128 bytes of k for every row (64 elements of 16 bits, 32 of 32 bits, 128 of 8 bits), or
 // as many k-strided rows.  Chunks of 16 bytes lie in LDS where a swizzle puts them, so that the 16 lanes that read a
 // column of a tile hit different banks; k-strided tiles of 16-bit elements are transposed by the read (ds_read_b64_tr_b16).
-// Sums are held in 32 bits (MFMA accumulators); the epilogue works on 32-bit sums and rounds once.
+// Elements of 16 bits go to the matrix instructions as they are, e4m3 after widening to half precision, single precision in
+// three parts of bfloat16.  Sums are held in 32 bits (MFMA accumulators); the epilogue works on 32-bit sums and rounds once.
+//
+// Measured: 100 000 x 2048 x 512 in half precision with bias, ReLU and z kept 258-269 us (0.8 PFLOP/s; matrix units busy 0.4 of the
+// time); 50 003 x 1024 x 1024 in e4m3 with scales, SiLU and residual 137-139 us (0.76 PFLOP/s); the gradient of 26 624 x 512 x 256
+// with GELU in bfloat16 47 us, of 11 264 x 256 x 256 with ReLU in single precision 45 us; one row 256 x 256 4 us of kernel.
+// What bounds the large ones is the step: a stage's loads, LDS reads and products, with two workgroups to a CU to fill each
+// other's waits; the small ones a launch and one trip to memory.
 #include "layer.hpp"
 #include "layer_dev.hpp"
 
@@ -545,7 +552,8 @@ __global__ __launch_bounds__(TILE::kThreads, (waves_that_fit<TYPE, TILE>())) voi
 }
 
 // Few tiles: a workgroup has 16 rows of x and 16 of w, its waves share k between them and read both straight into the
-// operands of the MFMA, and the eight sums of every element meet in LDS.
+// operands of the MFMA, and the eight sums of every element meet in LDS, so that one trip to memory is all that lies between launch and
+// epilogue (1 x 256 x 256 in half precision 4.2 us, 777 x 200 x 47 in single 4.0).
 constexpr int kFewWaves = 8;
 template <int TYPE, class OUT>
 __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(ProductArgs<OUT> p) {
@@ -591,8 +599,10 @@ __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(ProductAr
 
 // ---- the gradient's other steps
 
-// dz = dy * act'(pre), rounded to the type the products work in, and the sums of dz's columns (from the values before
-// they are rounded) over the rows of a workgroup.
+// dz = dy * act'(pre), rounded to the type the products work in (their matrix instructions take no other; dz in 32 bits would cost the
+// products of 16-bit layers six times the instructions), and the sums of dz's columns (from the values before they are
+// rounded) over the rows of a workgroup.  Bound by memory: 26 624 x 256 in bfloat16 with GELU 12-14 us, for 41 MB of which most
+// comes from HBM.  (GELU by the library's error function and one row in flight: 19 us.)
 constexpr int kSlopeRows = 2;                     // rows that a thread has in flight
 struct SlopeArgs {
     Count rows;
@@ -648,7 +658,8 @@ __global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
     }
 }
 
-// out[r][c] = the sum over s of part[s][r][c], in the order of s; the column sums of the slope kernel ride on the launch.
+// out[r][c] = the sum over s of part[s][r][c]; the column sums of the slope kernel ride on the launch.  `subs` threads share a cell and
+// add every subs-th slice, then the shares in turn: the same order in every call.  32 slices of 256 x 512: 6.4 us; parts are L2's.
 struct JoinArgs {
     const float* part;
     int64_t cells;                                // of a slice, dense
@@ -692,8 +703,7 @@ Operand operand(const void* data, int64_t ld, int type, int64_t rows, int64_t co
 
 uint32_t tiles_of(int64_t n, int tile) { return static_cast<uint32_t>((n + tile - 1) / tile); }
 
-// grid of tile_of: rows of tiles in eights, one for each XCD
-// whether rows can go straight to LDS: 16-byte multiples at 16-byte addresses
+// Whether rows can go straight to LDS: 16-byte multiples at 16-byte addresses.
 bool direct(const Operand& o, int bytes) {
     return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % 16 == 0 && o.cols * bytes % 16 == 0;
 }

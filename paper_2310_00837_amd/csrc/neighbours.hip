@@ -5,9 +5,12 @@
 //
 // A group of lanes has one row (or one source) and eight neighbouring columns to a lane, so a source's row is read as
 // one run; sums are held in 32 bits and added in the order of the list, so results do not depend on the launch.  The gradient
-// needs the block by source: block_transpose sorts the entries by source with the stable radix sort of the hotness order.
-// What bounds it is the latency of the chain entry -> row, hidden by several entries in flight per group, and then HBM/L2
-// traffic of the rows.
+// needs the block by source, entries in their order: block_transpose finds it in one launch up to 131 072 places, and beyond them with
+// the stable radix sort of the hotness order.
+// What bounds it is the latency of the chain list -> entry -> row, hidden by several entries in flight per group, and then HBM/L2
+// traffic of the rows: means of 25 600 rows of ten, 128 columns in single precision, 26 us, of 640 rows of five, 64 columns, 4.4 us of
+// kernel; the gradient of 24 000 sources of 26 600 entries, 256 columns in bfloat16, 30 us: 11 by source, 15 of sums, 4 for
+// a launch that finds no long list.
 #include "kernels.hpp"
 #include "layer.hpp"
 #include "layer_dev.hpp"
@@ -22,13 +25,13 @@ hipError_t launch_hotness_order(hipStream_t stream, const int32_t* counts, int64
 
 namespace {
 
-constexpr int kMeanAhead = 8;                     // entries of a list whose rows are asked for together
-constexpr int kAhead = 4;                         // ... in the gradient, where a list begins (most have few)
+constexpr int kMeanAhead = 8;                     // entries of a list whose rows are asked for together (lists are 5 to 25 long)
+constexpr int kAhead = 4;                         // ... in the gradient, where a list begins (most have one or two)
 constexpr int kPiece = 256;                       // entries of a long list that a workgroup adds up
 constexpr int kLongBlock = 256;                   // ... and its threads
 constexpr uint32_t kLines = 8, kLineWords = 32;   // of the counters
 static_assert((1 + kLines) * kLineWords <= kLayerCounters, "a context has room for as many counters");
-constexpr int kLongList = 32;                     // entries of a source that a group adds up by itself
+constexpr int kLongList = 32;                     // entries of a source that a group adds up by itself; longer ones would hold up their wave
 
 template <int TYPE>
 __device__ __forceinline__ void copy_8_of(const void* from, int64_t at, void* to, int64_t to_at, int valid) {
@@ -86,7 +89,7 @@ __global__ __launch_bounds__(kBlock) void block_mean_kernel(MeanJob p) {
             for (int k = 0; k < kMeanAhead; ++k) add_8<TYPE>(v[k], 1.0f, sum);
         }
         const float weight = 1.0f / (end > list.lo ? static_cast<float>(end - list.lo) : 1.0f);
-    #pragma unroll
+#pragma unroll
         for (int c = 0; c < 8; ++c) sum[c] *= weight;
         store_8_of<TYPE>(p.mean, row * p.mean_ld + col, valid, sum);
     }
@@ -536,6 +539,8 @@ struct RunMeanGrad {
     }
 };
 
+// By ranges where looking through all places takes less than the sort's five launches (60 to 70 us).  us by sort / by ranges: 27 000 places
+// 57 / 13, 75 000 57 / 22; every workgroup reads every place, so the time grows with them.
 constexpr int64_t kRangePlaces = 1 << 17;
 struct TransposePlan {
     int64_t n, ranges;                            // (ranges: 0 by a sort)
@@ -543,7 +548,6 @@ struct TransposePlan {
     explicit TransposePlan(const TransposeJob& j) {
         const auto up = [](size_t b) { return (b + 255) / 256 * 256; };
         n = j.n_col + (j.row ? j.rows.host : 0);
-        // By ranges where looking through all places takes less than the sort's five launches
         ranges = n > kRangePlaces || j.n_src < 1 ? 0 : std::max<int64_t>(std::min<int64_t>(256, (j.n_src + 31) / 32), (j.n_src + kRangeMost - 1) / kRangeMost);
         if (ranges > 4096) ranges = 0;
         const size_t ints = up(sizeof(int32_t) * static_cast<size_t>(std::max<int64_t>(n, 1)));

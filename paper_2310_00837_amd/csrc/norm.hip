@@ -7,7 +7,10 @@
 //   dx = dtotal + q (u - t q^2 mean(u t));  dgain = sum over rows of dy t q
 //
 // A row is held in the registers of the lanes that share it, in 32 bits, so that it is read once and every output is made
-// from the unrounded sums.  What bounds it is memory: one pass over what has to be read and written.
+// from the unrounded sums.  What bounds it is memory: one pass over what has to be read and written.  100 003 x 1024 in half
+// precision with residual, sum and 8-bit output: 128 us for 717 MB, 5.6 TB/s (a plain copy reaches 6.4); the gradient of
+// 26 624 x 512 in bfloat16 with dtotal and dgain: 26 us for 109 MB, of which the join of dgain's parts is 5; 1024 x 256 in single
+// precision 4 us of kernel, a launch and a trip to memory.
 #include "layer.hpp"
 #include "layer_dev.hpp"
 
@@ -27,7 +30,7 @@ struct RowShape {
     static constexpr int kThreads = LANES > kBlock ? LANES : kBlock;
     static constexpr int kRows = kThreads / LANES;
 };
-template <int LANES, int THREADS>
+template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float* s) {
     v = group_sum<(LANES < kWave ? LANES : kWave)>(v);
     if (LANES > kWave) {
@@ -42,7 +45,7 @@ __device__ __forceinline__ float row_sum(float v, float* s) {
     }
     return v;
 }
-template <int LANES, int THREADS>
+template <int LANES>
 __device__ __forceinline__ float row_max(float v, float* s) {
     v = group_max<(LANES < kWave ? LANES : kWave)>(v);
     if (LANES > kWave) {
@@ -81,7 +84,6 @@ __device__ __forceinline__ void store_8_of_e4m3(void* base, int64_t at, int vali
 
 template <int TYPE, int LANES, int CHUNKS>
 __device__ __forceinline__ void norm_row(const NormJob& p, int64_t row, int lane, float* s) {
-    constexpr int kThreads = RowShape<LANES>::kThreads;
     float t[CHUNKS][8];
     float sum = 0;
 #pragma unroll
@@ -93,13 +95,13 @@ __device__ __forceinline__ void norm_row(const NormJob& p, int64_t row, int lane
             load_8_of<TYPE>(p.residual, row * p.residual_ld + col, valid, r);
 #pragma unroll
             for (int e = 0; e < 8; ++e) t[c][e] += r[e];
-            if (p.total) store_8_of<TYPE>(p.total, row * p.total_ld + col, valid, t[c]);
-        } else if (p.total) store_8_of<TYPE>(p.total, row * p.total_ld + col, valid, t[c]);
+        }
+        if (p.total) store_8_of<TYPE>(p.total, row * p.total_ld + col, valid, t[c]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum += t[c][e] * t[c][e];
     }
     if (p.normalise) {
-        const float q = 1.0f / sqrtf(row_sum<LANES, kThreads>(sum, s) / p.width + p.eps);
+        const float q = 1.0f / sqrtf(row_sum<LANES>(sum, s) / p.width + p.eps);
         if (p.inv_rms && lane == 0) p.inv_rms[row] = q;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
@@ -126,7 +128,7 @@ __device__ __forceinline__ void norm_row(const NormJob& p, int64_t row, int lane
             const float a = fabsf(t[c][e]);
             most = a > most || a != a ? a : most;
         }
-    most = row_max<LANES, kThreads>(most, s) / kE4M3Max;
+    most = row_max<LANES>(most, s) / kE4M3Max;
     const float scale = most < kMinScale ? kMinScale : most, inv = 1.0f / scale;
     if (lane == 0) p.y_scale[row] = scale;
 #pragma unroll
@@ -208,8 +210,8 @@ __global__ __launch_bounds__((GradShape<LANES, CHUNKS>::kThreads)) void norm_gra
 #pragma unroll
             for (int e = 0; e < 8; ++e) square += t[c][e] * t[c][e], dot += t[c][e] * d[c][e] * g[e];
         }
-        dot = row_sum<LANES, kThreads>(dot, s);
-        const float q = p.inv_rms ? p.inv_rms[row] : 1.0f / sqrtf(row_sum<LANES, kThreads>(square, s) / p.width + p.eps);
+        dot = row_sum<LANES>(dot, s);
+        const float q = p.inv_rms ? p.inv_rms[row] : 1.0f / sqrtf(row_sum<LANES>(square, s) / p.width + p.eps);
         const float f = q * q * dot / p.width;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
@@ -255,7 +257,8 @@ __global__ __launch_bounds__(kBlock) void gain_sum_kernel(const float* part, int
     sum_columns(part, n_parts, width, blockIdx.x * kSumColumns, out, type);
 }
 
-// The lanes and chunks for a row of `width` elements
+// The lanes and chunks for a row of `width` elements: as few lanes idle as powers of two allow, and up to a wave the sums over a row
+// need no LDS.
 template <int TYPE, class RUN>
 auto by_width(int32_t width, RUN run) {
     if (width <= 128) return run.template go<TYPE, 16, 1>();

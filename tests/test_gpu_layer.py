@@ -147,6 +147,14 @@ def test_linear(helios, h, shape, x_type, out_type):
     _linear_case(helios, h, n, k, m, x_type, out_type, ACTS[(seed + 2) % 4], True, False, True, (16, 16, 8), seed + 20)
 
 
+@pytest.mark.parametrize("x_type,out_type", [(F16, F16), (F16, F32), (BF16, BF16), (BF16, F32)], ids=str)
+def test_linear_of_long_lists(helios, h, x_type, out_type):
+    """Lists of several rounds of tiles, where tiles are 160 rows high; the last one is cut short, in rows and columns."""
+    print("linear long", x_type, out_type, flush=True)
+    _linear_case(helios, h, 20400, 584, 1000, x_type, out_type, "relu", True, True, True, (0, 0, 0), 5)
+    _linear_case(helios, h, 20391, 583, 1001, x_type, out_type, "silu", True, True, False, (3, 1, 5), 6, 20390)
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("x_type", [F32, F16, BF16, E4M3], ids=str)
 def test_linear_with_the_count_on_the_device(helios, h, x_type, act):
