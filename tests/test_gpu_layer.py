@@ -244,6 +244,15 @@ def test_linear_grad_of_some(helios, h, outs):
 
 
 @pytest.mark.parametrize("x_type", [F32, F16, BF16], ids=str)
+@pytest.mark.parametrize("outs", [("dw",), ("dx", "dw")], ids=str)
+def test_linear_grad_of_long_lists(helios, h, x_type, outs):
+    """Long slices of rows, as many as fill the GPU once or twice."""
+    print("linear grad long", x_type, outs, flush=True)
+    _linear_grad_case(helios, h, 12500, 1000, 504, x_type, x_type, "relu", (0, 0, 0), 7, outs=outs)
+    _linear_grad_case(helios, h, 12501, 1001, 503, x_type, x_type, "none", (3, 1, 5), 8, 12500, outs=outs)
+
+
+@pytest.mark.parametrize("x_type", [F32, F16, BF16], ids=str)
 def test_linear_grad_with_the_count_on_the_device(helios, h, x_type):
     for n, count in ((200, 0), (200, 1), (200, 130), (3000, 2049)):
         for act in ("none", "silu"):
