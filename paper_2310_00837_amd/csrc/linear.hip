@@ -12,7 +12,7 @@
 //
 // Measured: 100 000 x 2048 x 512 in half precision with bias, ReLU and z kept 258-269 us (0.8 PFLOP/s; matrix units busy 0.4 of the
 // time); 50 003 x 1024 x 1024 in e4m3 with scales, SiLU and residual 137-139 us (0.76 PFLOP/s); the gradient of 26 624 x 512 x 256
-// with GELU in bfloat16 47 us, of 11 264 x 256 x 256 with ReLU in single precision 45 us; one row 256 x 256 4 us of kernel.
+// with GELU in bfloat16 47 us, of 11 264 x 256 x 256 with ReLU in single precision 44 us; one row 256 x 256 4 us of kernel.
 // What bounds the large ones is the step: a stage's loads, LDS reads and products, with two workgroups to a CU to fill each
 // other's waits; the small ones a launch and one trip to memory.
 #include "layer.hpp"
