@@ -8,11 +8,11 @@
 // as many k-strided rows.  Chunks of 16 bytes lie in LDS where a swizzle puts them, so that the 16 lanes that read a
 // column of a tile hit different banks; k-strided tiles of 16-bit elements are transposed by the read (ds_read_b64_tr_b16).
 // Elements of 16 bits go to the matrix instructions as they are, e4m3 after widening to half precision, single precision in
-// three parts of bfloat16.  Sums are held in 32 bits (MFMA accumulators); the epilogue works on 32-bit sums and rounds once.
+// three parts of bfloat16, gradients that 16 bits cannot hold in two.  Sums are held in 32 bits (MFMA accumulators); the epilogue works on 32-bit sums and rounds once.
 //
 // Measured: 100 000 x 2048 x 512 in half precision with bias, ReLU and z kept 258-269 us (0.8 PFLOP/s; matrix units busy 0.4 of the
 // time); 50 003 x 1024 x 1024 in e4m3 with scales, SiLU and residual 137-139 us (0.76 PFLOP/s); the gradient of 26 624 x 512 x 256
-// with GELU in bfloat16 47 us, of 11 264 x 256 x 256 with ReLU in single precision 44 us; one row 256 x 256 4 us of kernel.
+// with GELU in bfloat16 65 us, of 11 264 x 256 x 256 with ReLU in single precision 44 us; one row 256 x 256 4 us of kernel.
 // What bounds the large ones is the step: a stage's loads, LDS reads and products, with two workgroups to a CU to fill each
 // other's waits; the small ones a launch and one trip to memory.
 #include "layer.hpp"
@@ -335,6 +335,7 @@ struct PlainOut {                                 // (slice: which part of k the
 template <class OUT>
 struct ProductArgs {
     Operand a, b;
+    int64_t a_low;                                // bytes from a value of A to its second part, where A comes in two (PARTS)
     int64_t m, k;                                 // the most; `rows` limits m, or k where that runs over rows
     int32_t n;
     Count rows;
@@ -373,8 +374,58 @@ struct ProductLds {
     static_assert(kTm % kOutTiles == 0, "the epilogue takes as many rows of tiles at a time");
 };
 
+// Products with A in two parts (PARTS: a gradient that 16 bits of x's type cannot hold): a = hi + lo, both in bfloat16, so 16 bits of a value in
+// the range of 32-bit ones; off by up to 2^-16 of it.  B is what it is in bfloat16, and for half precision two parts again, exact, cut when they
+// are read from LDS; of the four products lo lo', below 2^-16, is left out.  Two (three) instructions in place of one.  Rounded to x's type, as
+// the instructions would take it at once, a value is off by 2^-8 (2^-11), which shows in the results (26 624 x 512 x 256 with GELU in bfloat16:
+// off by 0.0024 of their norm in place of 0.0017, which is their own rounding, in 47 us in place of 65), and in half precision
+// gradients below 2^-25 are lost.
+template <int TYPE> struct PartsMma;
+template <> struct PartsMma<kBF16> {
+    typedef bf16x8 Part;
+    static __device__ __forceinline__ Part part(i32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+    static __device__ __forceinline__ f32x4 run(const bf16x8& hi, const bf16x8& lo, const Part& b, f32x4 c) {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, lo, c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, hi, c, 0, 0, 0);
+    }
+};
+template <> struct PartsMma<kF16> {
+    struct Part {
+        bf16x8 hi, lo;
+    };
+    static __device__ __forceinline__ Part part(i32x4 v) {
+        const f16x8 x = __builtin_bit_cast(f16x8, v);
+        Part p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float f = static_cast<float>(x[e]);
+            p.hi[e] = static_cast<__bf16>(f);
+            p.lo[e] = static_cast<__bf16>(f - static_cast<float>(p.hi[e]));
+        }
+        return p;
+    }
+    static __device__ __forceinline__ f32x4 run(const bf16x8& hi, const bf16x8& lo, const Part& b, f32x4 c) {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.hi, lo, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.lo, hi, c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.hi, hi, c, 0, 0, 0);
+    }
+};
+// The same by the instructions of single precision, for tiles with values that are not finite (an infinity would meet a lower part of
+// zero, and leave NaN where there is none).
+template <int TYPE>
+__device__ __forceinline__ f32x4 parts_in_single(i32x4 hi, i32x4 lo, i32x4 b, f32x4 c) {
+    const i32x4 h[1] = {hi}, l[1] = {lo}, o[1] = {b};
+    float x[8], y[8], z[8];
+    widen_8<kBF16>(h, x);
+    widen_8<kBF16>(l, y);
+    widen_8<TYPE>(o, z);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(z[e], x[e] + y[e], c, 0, 0, 0);
+    return c;
+}
+
 // The tiles block, block + blocks, ... of a product.
-template <int TYPE, class TILE, bool A_STRIDED, bool B_STRIDED, bool DIRECT, class OUT>
+template <int TYPE, class TILE, bool A_STRIDED, bool B_STRIDED, bool DIRECT, bool PARTS, class OUT>
 __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint32_t blocks, char* lds) {
     constexpr int BM = TILE::kM, BN = TILE::kN, WAVES_M = TILE::kWavesM, WAVES_N = TILE::kWavesN, kThreads = TILE::kThreads;
     typedef ProductLds<TYPE, TILE> Lds;
@@ -388,7 +439,8 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
     const int64_t m_end = rows_are_k ? p.m : count, k_end = rows_are_k ? count : p.k;
     if (rows_are_k) p.a.rows = p.b.rows = count;
     else p.a.rows = count;
-    const int64_t steps_all = (k_end + StageA::kK - 1) / StageA::kK, per = (steps_all + p.slices - 1) / p.slices;
+    constexpr int kK = PARTS ? StageA::kK / 2 : StageA::kK;              // of a step
+    const int64_t steps_all = (k_end + kK - 1) / kK, per = (steps_all + p.slices - 1) / p.slices;
 
     const int wave = threadIdx.x / kWave, wave_m = wave / WAVES_N, wave_n = wave % WAVES_N;
     for (uint32_t tile = block; tile < p.tiles; tile += blocks) {      // (once round, but for the longest lists)
@@ -426,7 +478,84 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
         // workgroup of the CU.)
         const typename StageA::Source sa = StageA::source(p.a, m0);
         const typename StageB::Source sb = StageB::source(p.b, n0);
-        if constexpr (DIRECT && !kSplit) {
+        if constexpr (PARTS) {
+            // (a stage: 64 bytes of k of both parts of A and of B)
+            typedef Stage<kBF16, BM, kStageBytes / 2, A_STRIDED, kThreads> PartA;
+            typedef Stage<TYPE, BN, kStageBytes / 2, B_STRIDED, kThreads> PartB;
+            constexpr int kLow = BM * kStageBytes / 2, kB = 2 * kLow;
+            const Operand low{p.a.data + p.a_low, p.a.ld, p.a.rows, p.a.cols};
+            const typename PartA::Source s_hi = PartA::source(p.a, m0), s_lo = PartA::source(low, m0);
+            const typename PartB::Source s_b = PartB::source(p.b, n0);
+            const auto through = [&](auto multiply_stage) {
+                if constexpr (DIRECT) {
+                    const auto load = [&](int64_t step) {
+                        char* to = lds + ((step - step0) & 1) * kStage;
+                        PartA::load_lds(p.a, s_hi, step * kK, to);
+                        PartA::load_lds(low, s_lo, step * kK, to + kLow);
+                        PartB::load_lds(p.b, s_b, step * kK, to + kB);
+                    };
+                    if (step0 < step1) load(step0);
+                    for (int64_t step = step0; step < step1; ++step) {
+                        wait_and_meet();
+                        if (step + 1 < step1) load(step + 1);
+                        multiply_stage(lds + ((step - step0) & 1) * kStage);
+                    }
+                } else {
+                    i32x4 r_hi[PartA::kLoads], r_lo[PartA::kLoads], r_b[PartB::kLoads];
+                    const auto load = [&](int64_t step) {
+                        PartA::template load<false>(p.a, s_hi, step * kK, r_hi);
+                        PartA::template load<false>(low, s_lo, step * kK, r_lo);
+                        PartB::template load<false>(p.b, s_b, step * kK, r_b);
+                    };
+                    if (step0 < step1) load(step0);
+                    for (int64_t step = step0; step < step1; ++step) {
+                        char* stage = lds + ((step - step0) & 1) * kStage;
+                        PartA::put(stage, r_hi);
+                        PartA::put(stage + kLow, r_lo);
+                        PartB::put(stage + kB, r_b);
+                        __syncthreads();
+                        if (step + 1 < step1) load(step + 1);
+                        multiply_stage(stage);
+                    }
+                }
+            };
+            through([&](const char* stage) {
+                bf16x8 hi[kTm], lo[kTm];
+                typename PartsMma<TYPE>::Part b[kTn];
+#pragma unroll
+                for (int i = 0; i < kTm; ++i) {
+                    hi[i] = __builtin_bit_cast(bf16x8, PartA::fragment(stage, (wave_m * kTm + i) * 16, 0));
+                    lo[i] = __builtin_bit_cast(bf16x8, PartA::fragment(stage + kLow, (wave_m * kTm + i) * 16, 0));
+                }
+#pragma unroll
+                for (int j = 0; j < kTn; ++j) b[j] = PartsMma<TYPE>::part(PartB::fragment(stage + kB, (wave_n * kTn + j) * 16, 0));
+#pragma unroll
+                for (int i = 0; i < kTm; ++i)
+#pragma unroll
+                    for (int j = 0; j < kTn; ++j) acc[i][j] = PartsMma<TYPE>::run(hi[i], lo[i], b[j], acc[i][j]);
+            });
+            // (a value that is not finite leaves a sum that is not)
+            float spoilt = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kTm; ++i)
+#pragma unroll
+                for (int j = 0; j < kTn; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) spoilt = __builtin_fmaf(acc[i][j][e], 0.0f, spoilt);
+            if (__syncthreads_or(spoilt != 0.0f)) {
+                clear();
+                through([&](const char* stage) {
+#pragma unroll
+                    for (int j = 0; j < kTn; ++j) {
+                        const i32x4 b = PartB::fragment(stage + kB, (wave_n * kTn + j) * 16, 0);
+#pragma unroll
+                        for (int i = 0; i < kTm; ++i)
+                            acc[i][j] = parts_in_single<TYPE>(PartA::fragment(stage, (wave_m * kTm + i) * 16, 0),
+                                                              PartA::fragment(stage + kLow, (wave_m * kTm + i) * 16, 0), b, acc[i][j]);
+                    }
+                });
+            }
+        } else if constexpr (DIRECT && !kSplit) {
             const auto load = [&](int64_t step) {
                 char* to = lds + ((step - step0) & 1) * kStage;
                 StageA::load_lds(p.a, sa, step * StageA::kK, to);
@@ -540,15 +669,15 @@ constexpr int waves_that_fit() { return TYPE == kF32 ? 1 : TILE::kThreads / kWav
 template <int TYPE, class TILE, bool DIRECT, class OUT>
 __global__ __launch_bounds__(TILE::kThreads, (waves_that_fit<TYPE, TILE>())) void forward_kernel(ProductArgs<OUT> p) {
     __shared__ __align__(16) char lds[ProductLds<TYPE, TILE>::kBytes];
-    product<TYPE, TILE, false, false, DIRECT>(p, blockIdx.x, gridDim.x, lds);
+    product<TYPE, TILE, false, false, DIRECT, false>(p, blockIdx.x, gridDim.x, lds);
 }
 
 // Both products of the gradient in one launch, each with workgroups of its own: dw's tiles come first, since each takes longest.
-template <int TYPE, class TILE, bool DIRECT>
+template <int TYPE, class TILE, bool DIRECT, bool PARTS>
 __global__ __launch_bounds__(TILE::kThreads, (waves_that_fit<TYPE, TILE>())) void backward_kernel(ProductArgs<PlainOut<TYPE>> dw, uint32_t dw_blocks, ProductArgs<PlainOut<TYPE>> dx) {
     __shared__ __align__(16) char lds[ProductLds<TYPE, TILE>::kBytes];
-    if (blockIdx.x < dw_blocks) product<TYPE, TILE, true, true, DIRECT>(dw, blockIdx.x, dw_blocks, lds);
-    else product<TYPE, TILE, false, true, DIRECT>(dx, blockIdx.x - dw_blocks, gridDim.x - dw_blocks, lds);
+    if (blockIdx.x < dw_blocks) product<TYPE, TILE, true, true, DIRECT, PARTS>(dw, blockIdx.x, dw_blocks, lds);
+    else product<TYPE, TILE, false, true, DIRECT, PARTS>(dx, blockIdx.x - dw_blocks, gridDim.x - dw_blocks, lds);
 }
 
 // Few tiles: a workgroup has 16 rows of x and 16 of w, its waves share k between them and read both straight into the
@@ -599,9 +728,9 @@ __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(ProductAr
 
 // ---- the gradient's other steps
 
-// dz = dy * act'(pre), rounded to the type the products work in (their matrix instructions take no other; dz in 32 bits would cost the
-// products of 16-bit layers six times the instructions), and the sums of dz's columns (from the values before they are
-// rounded) over the rows of a workgroup.  Bound by memory: 26 624 x 256 in bfloat16 with GELU 12-14 us, for 41 MB of which most
+// dz = dy * act'(pre) for the products: in 32 bits if they are in single precision, in x's type if that holds it exactly (no activation or ReLU,
+// and dy of x's type), else in two parts of bfloat16; and the sums of dz's columns (from the values before they are
+// cut) over the rows of a workgroup.  Bound by memory: 26 624 x 256 in bfloat16 with GELU 12-14 us, for 41 MB of which most
 // comes from HBM.  (GELU by the library's error function and one row in flight: 19 us.)
 constexpr int kSlopeRows = 2;                     // rows that a thread has in flight
 struct SlopeArgs {
@@ -614,10 +743,25 @@ struct SlopeArgs {
     int64_t pre_ld;
     void* dz;                                     // nullable
     int64_t dz_ld;
+    int64_t dz_low;                               // elements from a value's first part to its second
     float* sums;                                  // [gridDim.y][n], nullable
     void* dbias;                                  // with one row of workgroups: where their sums go at once, in `type`
 };
+// The two parts of eight values: what is nearest in bfloat16 (the largest there is, for what is finite and would not be), and what is left.
+__device__ __forceinline__ void store_8_parts(void* base, int64_t at, int64_t low, int valid, const float (&v)[8]) {
+    float hi[8], lo[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float most = 0x1.fep127f, near = static_cast<float>(static_cast<__bf16>(v[e]));
+        hi[e] = fabsf(v[e]) > most && fabsf(v[e]) < __builtin_inff() ? __builtin_copysignf(most, v[e]) : near;
+        const float rest = v[e] - hi[e];
+        lo[e] = rest - rest == 0.0f ? rest : 0.0f;
+    }
+    store_8_of<kBF16>(base, at, valid, hi);
+    store_8_of<kBF16>(base, at + low, valid, lo);
+}
 // (LANES threads share a row of the workgroup's columns, eight each; the others go through the rows)
+constexpr int kInParts = -1;
 template <int TYPE, int Z_TYPE, bool SLOPE, int LANES>
 __global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
     constexpr int kSubs = kBlock / LANES, kCols = LANES * 8;
@@ -642,7 +786,9 @@ __global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
                 if (SLOPE) scale_by_slope_8(p.act, z[k], d[k]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += d[k][e];
-                if (p.dz) store_8_of<Z_TYPE>(p.dz, (row + kSubs * k) * p.dz_ld + col, valid, d[k]);
+                if (!p.dz) continue;
+                if constexpr (Z_TYPE == kInParts) store_8_parts(p.dz, (row + kSubs * k) * p.dz_ld + col, p.dz_low, valid, d[k]);
+                else store_8_of<Z_TYPE>(p.dz, (row + kSubs * k) * p.dz_ld + col, valid, d[k]);
             }
         }
     if (!p.sums && !p.dbias) return;
@@ -731,7 +877,7 @@ hipError_t launch_forward(hipStream_t stream, ProductArgs<OUT> p) {
 }
 
 // dw and dx: nullptr if not asked for
-template <int TYPE, class TILE>
+template <int TYPE, class TILE, bool PARTS>
 hipError_t launch_backward(hipStream_t stream, ProductArgs<PlainOut<TYPE>>* dw, ProductArgs<PlainOut<TYPE>>* dx) {
     ProductArgs<PlainOut<TYPE>> w{};
     ProductArgs<PlainOut<TYPE>> x{};
@@ -748,8 +894,8 @@ hipError_t launch_backward(hipStream_t stream, ProductArgs<PlainOut<TYPE>>* dw, 
         x = *dx;
     }
     const dim3 grid(dw_blocks + dx_blocks);
-    if (straight) hipLaunchKernelGGL((backward_kernel<TYPE, TILE, true>), grid, dim3(TILE::kThreads), 0, stream, w, dw_blocks, x);
-    else hipLaunchKernelGGL((backward_kernel<TYPE, TILE, false>), grid, dim3(TILE::kThreads), 0, stream, w, dw_blocks, x);
+    if (straight) hipLaunchKernelGGL((backward_kernel<TYPE, TILE, true, PARTS>), grid, dim3(TILE::kThreads), 0, stream, w, dw_blocks, x);
+    else hipLaunchKernelGGL((backward_kernel<TYPE, TILE, false, PARTS>), grid, dim3(TILE::kThreads), 0, stream, w, dw_blocks, x);
     return hipGetLastError();
 }
 
@@ -797,8 +943,8 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
 
 constexpr int64_t kOneSliceRows = 256;
 struct GradPlan {                                 // of linear_grad: what lies where in the scratch, and how far k is cut up
-    bool needs_dz, large;                         // large: by large tiles
-    int64_t dz_ld;
+    bool needs_dz, in_parts, large;               // in_parts: dz in two parts; large: by large tiles
+    int64_t dz_ld, dz_low;                        // elements from a part of dz to the other
     int slices;                                   // of dw's k
     unsigned slope_blocks;                        // workgroups along the rows of the slope kernel
     size_t dz, part, sums, bytes;
@@ -806,7 +952,9 @@ struct GradPlan {                                 // of linear_grad: what lies w
         const auto up = [](size_t b) { return (b + 255) / 256 * 256; };
         const int64_t n = j.rows.host;
         needs_dz = (j.dx || j.dw) && (j.act != kActNone || j.out_type != j.x_type);
+        in_parts = needs_dz && j.x_type != kF32 && (j.act == kActGelu || j.act == kActSilu || j.out_type != j.x_type);
         dz_ld = (j.n_out + 7) / 8 * 8;
+        dz_low = in_parts ? (n * dz_ld + 127) / 128 * 128 : 0;
         // dw's k, the rows, is cut so that there are about 1024 small tiles or 256 large ones, in eights (one for each XCD) of at least
         // four steps.  us, dw of 26 624 x 512 x 256 in bfloat16: small tiles 16 slices 21.7, 32 17.4; large ones 32 20.5, 64 19.3;
         // 50 000 x 2048 x 512: large ones 4 slices 223, 8 141, 16 150.  Large tiles where there are enough of them for the CUs (in single
@@ -830,20 +978,26 @@ struct GradPlan {                                 // of linear_grad: what lies w
         // (few rows: one slice, whose sums need no joining; a launch less)
         if (n <= kOneSliceRows) slices = 1, slope_blocks = 1;
         dz = 0;
-        part = dz + (needs_dz ? up(static_cast<size_t>(n * dz_ld) * type_bytes(j.x_type)) : 0);
+        part = dz + (needs_dz ? up(static_cast<size_t>(n * dz_ld + dz_low) * type_bytes(j.x_type)) : 0);
         sums = part + (j.dw ? up(static_cast<size_t>(slices) * j.n_out * j.n_in * sizeof(float)) : 0);
         bytes = sums + (j.dbias ? up(static_cast<size_t>(slope_blocks) * j.n_out * sizeof(float)) : 0);
     }
 };
 
 template <int TYPE, int LANES>
-hipError_t launch_slope(hipStream_t stream, const SlopeArgs& s, const LinearGradJob& j, unsigned blocks) {
+hipError_t launch_slope(hipStream_t stream, const SlopeArgs& s, const LinearGradJob& j, unsigned blocks, bool in_parts) {
     const dim3 grid(tiles_of(j.n_out, LANES * 8), blocks), block(kBlock);
     const bool slope = j.act != kActNone;
-    if (j.out_type == TYPE && slope) hipLaunchKernelGGL((slope_kernel<TYPE, TYPE, true, LANES>), grid, block, 0, stream, s);
-    else if (j.out_type == TYPE) hipLaunchKernelGGL((slope_kernel<TYPE, TYPE, false, LANES>), grid, block, 0, stream, s);
-    else if (slope) hipLaunchKernelGGL((slope_kernel<kF32, TYPE, true, LANES>), grid, block, 0, stream, s);
-    else hipLaunchKernelGGL((slope_kernel<kF32, TYPE, false, LANES>), grid, block, 0, stream, s);
+    if constexpr (TYPE != kF32) {
+        if (in_parts || j.out_type != TYPE) {
+            if (j.out_type == TYPE) hipLaunchKernelGGL((slope_kernel<TYPE, kInParts, true, LANES>), grid, block, 0, stream, s);
+            else if (slope) hipLaunchKernelGGL((slope_kernel<kF32, kInParts, true, LANES>), grid, block, 0, stream, s);
+            else hipLaunchKernelGGL((slope_kernel<kF32, kInParts, false, LANES>), grid, block, 0, stream, s);
+            return hipGetLastError();
+        }
+    }
+    if (slope) hipLaunchKernelGGL((slope_kernel<TYPE, TYPE, true, LANES>), grid, block, 0, stream, s);
+    else hipLaunchKernelGGL((slope_kernel<TYPE, TYPE, false, LANES>), grid, block, 0, stream, s);
     return hipGetLastError();
 }
 
@@ -854,15 +1008,16 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
     const int64_t dz_ld = plan.needs_dz ? plan.dz_ld : j.dy_ld;
     hipError_t e = hipSuccess;
     if (plan.needs_dz || j.dbias) {
-        SlopeArgs s{j.rows, j.n_out, j.act, j.dy, j.dy_ld, j.pre, j.pre_ld, plan.needs_dz ? scratch + plan.dz : nullptr, plan.dz_ld,
+        SlopeArgs s{j.rows, j.n_out, j.act, j.dy, j.dy_ld, j.pre, j.pre_ld, plan.needs_dz ? scratch + plan.dz : nullptr, plan.dz_ld, plan.dz_low,
                     j.dbias && plan.slope_blocks > 1 ? reinterpret_cast<float*>(scratch + plan.sums) : nullptr, plan.slope_blocks > 1 ? nullptr : j.dbias};
-        e = j.n_out <= 32 ? launch_slope<TYPE, 4>(stream, s, j, plan.slope_blocks) : launch_slope<TYPE, 16>(stream, s, j, plan.slope_blocks);
+        e = j.n_out <= 32 ? launch_slope<TYPE, 4>(stream, s, j, plan.slope_blocks, plan.in_parts) : launch_slope<TYPE, 16>(stream, s, j, plan.slope_blocks, plan.in_parts);
     }
     const bool has_dx = j.dx && j.rows.host > 0;
     if (e == hipSuccess && (has_dx || j.dw)) {
         ProductArgs<PlainOut<TYPE>> x{};
         x.a = operand(dz, dz_ld, TYPE, j.rows.host, j.n_out);
         x.b = operand(j.w, j.w_ld, TYPE, j.n_out, j.n_in);
+        x.a_low = plan.dz_low * type_bytes(TYPE);
         x.m = j.rows.host;
         x.n = j.n_in;
         x.k = j.n_out;
@@ -871,6 +1026,7 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         x.out = PlainOut<TYPE>{j.dx, j.dx_ld, 0, false};
         ProductArgs<PlainOut<TYPE>> w{};
         w.a = x.a;
+        w.a_low = x.a_low;
         w.b = operand(j.x, j.x_ld, TYPE, j.rows.host, j.n_in);
         w.m = j.n_out;
         w.n = j.n_in;
@@ -878,8 +1034,11 @@ hipError_t backward(hipStream_t stream, const LinearGradJob& j, char* scratch) {
         w.rows = j.rows;
         w.slices = plan.slices;
         w.out = plan.slices > 1 ? PlainOut<TYPE>{scratch + plan.part, j.n_in, static_cast<int64_t>(j.n_out) * j.n_in, true} : PlainOut<TYPE>{j.dw, j.dw_ld, 0, false};
-        e = plan.large ? launch_backward<TYPE, Large>(stream, j.dw ? &w : nullptr, has_dx ? &x : nullptr)
-                       : launch_backward<TYPE, Small>(stream, j.dw ? &w : nullptr, has_dx ? &x : nullptr);
+        ProductArgs<PlainOut<TYPE>>*dw = j.dw ? &w : nullptr, *dx = has_dx ? &x : nullptr;
+        if constexpr (TYPE != kF32) {
+            if (plan.in_parts) e = plan.large ? launch_backward<TYPE, Large, true>(stream, dw, dx) : launch_backward<TYPE, Small, true>(stream, dw, dx);
+        }
+        if (!plan.in_parts) e = plan.large ? launch_backward<TYPE, Large, false>(stream, dw, dx) : launch_backward<TYPE, Small, false>(stream, dw, dx);
     }
     const bool join_dw = j.dw && plan.slices > 1, join_dbias = j.dbias && plan.slope_blocks > 1;
     if (e == hipSuccess && (join_dw || join_dbias)) {

@@ -1,0 +1,89 @@
+"""What the operators of a layer lose of their values: gradients in 16 bits, and values at the ends of the types' ranges.
+
+Bounds are worked out from the formulas, as in test_gpu_layer.py, whose helpers are used."""
+import pytest
+import torch
+
+from test_gpu_layer import BF16, F16, F32, U32, _close, _rand, _slope
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def helios():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU")
+    from paper_2310_00837_amd import helios as hl
+    return hl
+
+
+@pytest.fixture(scope="module")
+def h(helios):
+    ctx = helios.Helios(0)
+    yield ctx
+    ctx.close()
+
+
+def _gradients(helios, h, x, w, dy, act, pre):
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    h.linear_grad(x, w, dy, act=getattr(helios, "ACT_" + act.upper()), pre=pre, dx=dx, dw=dw)
+    h.sync()
+    return dx.double().cpu(), dw.double().cpu()
+
+
+# ------------------------------------------------------------------ gradients in 16 bits
+
+
+@pytest.mark.parametrize("n,k,m", [(1500, 264, 136), (12500, 520, 264), (1501, 67, 131)])
+@pytest.mark.parametrize("x_type,out_type,act", [(BF16, BF16, "gelu"), (BF16, BF16, "silu"), (BF16, F32, "none"), (F16, F16, "gelu"), (F16, F16, "silu"),
+                                                 (F16, F32, "relu")], ids=str)
+def test_gradients_in_16_bits_are_off_by_their_own_rounding(helios, h, n, k, m, x_type, out_type, act):
+    """In the norm.  dz is held to 2^-16 of each value (and so is its product), a sum of t terms in 32 bits wanders by at most 4 sqrt(t) 2^-24
+    of its terms' norm, the slope is good to 2^-20, and the result is rounded once.  (dz in 16 bits would be off by as much as the result.)"""
+    print("gradient", n, k, m, x_type, out_type, act, flush=True)
+    x, w = _rand(n, k, 1).to(x_type), _rand(m, k, 2, k ** -0.5).to(x_type)
+    dy, pre = _rand(n, m, 3).to(out_type), _rand(n, m, 4).to(out_type)
+    got = _gradients(helios, h, x.cuda(), w.cuda(), dy.cuda(), act, pre.cuda() if act != "none" else None)
+    xd, wd, d, p = x.double(), w.double(), dy.double(), pre.double()
+    dz, off = d * _slope(p, act), 2.0 ** -20 * d.abs() * (1 + p.abs())
+    for have, want, terms, length, slopes in ((got[0], dz @ wd, dz.square() @ wd.square(), m, off.square() @ wd.square()),
+                                              (got[1], dz.t() @ xd, dz.square().t() @ xd.square(), n, off.square().t() @ xd.square())):
+        rounding = (want.to(x_type).double() - want).norm()
+        limit = rounding + (2.0 ** -16 + 4 * length ** 0.5 * U32) * terms.sum().sqrt() + slopes.sum().sqrt()
+        assert float((have - want).norm()) <= float(limit)
+
+
+@pytest.mark.parametrize("n,k,m", [(40, 72, 48), (3000, 72, 136)])
+@pytest.mark.parametrize("size,other", [(2.0 ** -27, 64.0), (1e6, 2.0 ** -12)], ids=["small", "large"])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_gradients_of_half_precision_keep_values_beyond_its_range(helios, h, n, k, m, size, other, act):
+    """A loss in single precision, divided by the batch or scaled up: dz is below half precision's smallest value or above its
+    largest, the gradients are not."""
+    rows = n ** -0.5 if size > 1 else 1.0                              # (so that sums over many rows fit)
+    x, w = _rand(n, k, 1, other * rows).to(F16), _rand(m, k, 2, other).to(F16)
+    dy, pre = _rand(n, m, 3, size).float(), _rand(n, m, 4).float()
+    got = _gradients(helios, h, x.cuda(), w.cuda(), dy.cuda(), act, pre.cuda() if act != "none" else None)
+    xd, wd, d, p = x.double(), w.double(), dy.double(), pre.double()
+    dz, off = d * _slope(p, act), 2.0 ** -20 * d.abs() * (1 + p.abs()) + 2.0 ** -15 * d.abs()
+    for have, want, bound in ((got[0], dz @ wd, off @ wd.abs() + 3 * (m + 8) * U32 * (dz.abs() @ wd.abs())),
+                              (got[1], dz.t() @ xd, off.t() @ xd.abs() + 3 * (n + 8) * U32 * (dz.abs().t() @ xd.abs()))):
+        assert float(want.abs().max()) < 60000
+        _close(have, want, bound, F16)
+
+
+@pytest.mark.parametrize("x_type,out_type,act", [(BF16, BF16, "gelu"), (BF16, F32, "none"), (F16, F16, "silu"), (F16, F32, "none")], ids=str)
+@pytest.mark.parametrize("n,k,m", [(100, 64, 256), (5000, 72, 1024), (3001, 67, 255)])
+def test_gradients_in_16_bits_keep_infinities_and_nan_to_their_rows_and_columns(helios, h, n, k, m, x_type, out_type, act):
+    print("gradient, not finite", n, k, m, x_type, out_type, act, flush=True)
+    x, w, dy, pre = (_rand(*s, seed).to(t) for s, seed, t in (((n, k), 1, x_type), ((m, k), 2, x_type), ((n, m), 3, out_type), ((n, m), 4, out_type)))
+    x[70, 5], x[71, 6], w[3, 1], dy[10, 2] = float("inf"), float("nan"), -float("inf"), float("inf")
+    got = _gradients(helios, h, x.cuda(), w.cuda(), dy.cuda(), act, pre.cuda() if act != "none" else None)
+    xd, wd, d, p = x.double(), w.double(), dy.double(), pre.double()
+    dz, off = d * _slope(p, act), 2.0 ** -20 * d.abs() * (1 + p.abs()) + 2.0 ** -15 * d.abs()
+    for have, want, a, b, a_off in ((got[0], dz @ wd, dz, wd, off), (got[1], dz.t() @ xd, dz.t(), xd, off.t())):
+        assert torch.equal(torch.isnan(have), torch.isnan(want)) and torch.equal(torch.isinf(have), torch.isinf(want))
+        assert torch.equal(have[torch.isinf(want)], want[torch.isinf(want)])
+        rows, cols = torch.isfinite(a).all(1), torch.isfinite(b).all(0)
+        clean, size = b[:, cols].abs(), a[rows].abs()
+        assert int(rows.sum()) >= a.shape[0] - 1 and int(cols.sum()) >= b.shape[1] - 2
+        _close(have[rows][:, cols], want[rows][:, cols], a_off[rows] @ clean + 3 * (a.shape[1] + 8) * U32 * (size @ clean), x_type)
