@@ -661,8 +661,12 @@ int helios_block_mean(helios_ctx *ctx, const helios_block_mean_args *args);
 /* A block's entries by source, for helios_block_mean_grad: those of source u
  * are src_entry[src_indptr[u] .. src_indptr[u+1]), a row i where a sample of
  * row i is u (in the order of col), then ~i where row[i] is u (row NULL: no
- * such entries).  src_indptr int32[n_src + 1]; src_entry int32 with room for
- * n_col entries, and n_rows more if row is given (fewer than 2^31 in all). */
+ * such entries).  Places of col that no list has are no entries, so part of a
+ * hop's rows may be given with all of its col.  src_indptr int32[n_src + 1];
+ * src_entry int32 with room for n_col entries, and n_rows more if row is given
+ * (fewer than 2^31 in all).  A list outside col and a source outside
+ * [0, n_src) are reported as HELIOS_EDATA by the next helios_sync; what is
+ * written then is safe to pass on, and means nothing. */
 int helios_block_transpose(helios_ctx *ctx, int64_t n_rows, const int64_t *n_rows_dev, const int64_t *indptr,
                            const int32_t *col, int64_t n_col, const int32_t *row, int64_t n_src,
                            int32_t *src_indptr, int32_t *src_entry);

@@ -58,6 +58,9 @@ __device__ __forceinline__ void add_8(const Raw8<TYPE>& row, float weight, float
     for (int c = 0; c < 8; ++c) sum[c] += v[c] * weight;
 }
 
+// Whether a row's list lies in col.
+__device__ __forceinline__ bool good_list(const RowBounds& list, int64_t n_col) { return list.lo >= 0 && list.lo <= list.hi && list.hi <= n_col; }
+
 template <int TYPE, int LANES>
 __global__ __launch_bounds__(kBlock) void block_mean_kernel(MeanJob p) {
     const int64_t count = p.rows.get();
@@ -69,7 +72,7 @@ __global__ __launch_bounds__(kBlock) void block_mean_kernel(MeanJob p) {
             if (self >= 0 && self < p.n_src) copy_8_of<TYPE>(p.x, self * p.x_ld + col, p.own, row * p.own_ld + col, valid);
             else raise(p.err, kErrData);
         }
-        const bool fits = list.lo >= 0 && list.lo <= list.hi && list.hi <= p.n_col;
+        const bool fits = good_list(list, p.n_col);
         if (!fits) raise(p.err, kErrData);
         float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         const int64_t end = fits ? list.hi : list.lo;
@@ -104,8 +107,13 @@ struct TransposeArgs {
 };
 
 // Sort keys: n_src - source, so that the descending order of the sort is the ascending order of the sources, and 0, behind all of
-// them, for places that hold no entry.
+// them, for places that hold no entry: those in front of the first list and behind the last, and those of lists that are not good.  All
+// keys are 0 before the lists' own are written.
 constexpr int kKeyLanes = 8;
+__global__ __launch_bounds__(kBlock) void transpose_clear_kernel(TransposeArgs a) {
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kBlock;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x; i < a.n; i += stride) a.keys[i] = 0;
+}
 __global__ __launch_bounds__(kBlock) void transpose_keys_kernel(TransposeArgs a) {
     const TransposeJob& p = a.job;
     const int64_t count = p.rows.get(), stride = static_cast<int64_t>(gridDim.x) * kBlock, t = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x;
@@ -118,19 +126,14 @@ __global__ __launch_bounds__(kBlock) void transpose_keys_kernel(TransposeArgs a)
     for (int64_t k = t; k < count * kKeyLanes; k += stride) {
         const int64_t row = k / kKeyLanes;
         const RowBounds list = row_bounds(p.indptr, static_cast<uint32_t>(row));
-        if (list.lo < 0 || list.lo > list.hi || list.hi > p.n_col) {
+        if (!good_list(list, p.n_col)) {
             raise(p.err, kErrData);
             continue;
         }
         for (int64_t e = list.lo + k % kKeyLanes; e < list.hi; e += kKeyLanes) put(e, p.col[e], static_cast<int32_t>(row));
     }
-    const int64_t used = count > 0 ? p.indptr[count] : 0;
-    for (int64_t e = (used < 0 ? 0 : used) + t; e < p.n_col; e += stride) a.keys[e] = 0;
     if (p.row)
-        for (int64_t i = t; i < a.n - p.n_col; i += stride) {
-            if (i < count) put(p.n_col + i, p.row[i], ~static_cast<int32_t>(i));
-            else a.keys[p.n_col + i] = 0;
-        }
+        for (int64_t i = t; i < count; i += stride) put(p.n_col + i, p.row[i], ~static_cast<int32_t>(i));
 }
 
 // The sorted entries and where every source's begin.
@@ -197,13 +200,18 @@ __global__ __launch_bounds__(kRangeBlock) void transpose_range_kernel(TransposeA
     const int64_t count = p.rows.get();
     const uint32_t first = blockIdx.x * range, t = threadIdx.x;
     const uint32_t sources = first >= p.n_src ? 0u : static_cast<uint32_t>(p.n_src - first < range ? p.n_src - first : range);
+    // (the lists are looked at by all workgroups together)
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kRangeBlock + t; i < count; i += static_cast<int64_t>(gridDim.x) * kRangeBlock)
+        if (!good_list(row_bounds(p.indptr, static_cast<uint32_t>(i)), p.n_col)) raise(p.err, kErrData);
     if (sources == 0) return;
-    int64_t used = count > 0 ? p.indptr[count] : 0;
-    if (used < 0 || used > p.n_col) {
+    // The lists are neighbours, so they take the places [n_first, n_col), and the rows' own sources those from there to n.
+    RowBounds all{0, 0};
+    if (count > 0) all = RowBounds{p.indptr[0], p.indptr[count]};
+    if (!good_list(all, p.n_col)) {
         raise(p.err, kErrData);
-        used = 0;
+        all = RowBounds{0, 0};
     }
-    const uint32_t n_col = static_cast<uint32_t>(used), n = n_col + (p.row ? static_cast<uint32_t>(count) : 0u);     // places in use: samples, then rows
+    const uint32_t n_first = static_cast<uint32_t>(all.lo), n_col = static_cast<uint32_t>(all.hi), n = n_col + (p.row ? static_cast<uint32_t>(count) : 0u);
     // where rows begin, roughly: the row of a place is looked up there first
     const uint32_t stride = static_cast<uint32_t>((count + kRangeSteps - 1) / kRangeSteps) > 0 ? static_cast<uint32_t>((count + kRangeSteps - 1) / kRangeSteps) : 1u;
     const uint32_t steps = static_cast<uint32_t>((count + stride - 1) / stride);
@@ -246,7 +254,7 @@ __global__ __launch_bounds__(kRangeBlock) void transpose_range_kernel(TransposeA
             }
         }
     };
-    look_through(p.col, n_col, 0);
+    look_through(p.col + n_first, n_col - n_first, n_first);
     if (p.row) look_through(p.row, n - n_col, n_col);
     below = dpp_sum(below);
     if (lane_id() == 0) atomicAdd(&s.below, below);
@@ -332,7 +340,7 @@ __global__ __launch_bounds__(kRangeBlock) void transpose_range_kernel(TransposeA
         place_held(found);
         return;
     }
-    for (uint32_t base = 0; base < n; base += kRangeHeld) {
+    for (uint32_t base = n_first; base < n; base += kRangeHeld) {
         if (t == 0) s.n_held = 0;
         __syncthreads();
         for (uint32_t k = t; k < kRangeHeld; k += kRangeBlock)
@@ -539,7 +547,7 @@ struct RunMeanGrad {
     }
 };
 
-// By ranges where looking through all places takes less than the sort's five launches (60 to 70 us).  us by sort / by ranges: 27 000 places
+// By ranges where looking through all places takes less than the sort's eight launches (60 to 70 us).  us by sort / by ranges: 27 000 places
 // 57 / 13, 75 000 57 / 22; every workgroup reads every place, so the time grows with them.
 constexpr int64_t kRangePlaces = 1 << 17;
 struct TransposePlan {
@@ -580,6 +588,7 @@ hipError_t launch_block_transpose(hipStream_t stream, const TransposeJob& job, v
     hipError_t e = hipSuccess;
     const auto blocks = [](int64_t n) { return dim3(static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((n + kBlock - 1) / kBlock, 4096)))); };
     if (a.n > 0) {
+        hipLaunchKernelGGL(transpose_clear_kernel, blocks(a.n), dim3(kBlock), 0, stream, a);
         hipLaunchKernelGGL(transpose_keys_kernel, blocks(std::max(a.n, job.rows.host * kKeyLanes)), dim3(kBlock), 0, stream, a);
         e = hipGetLastError();
         if (e == hipSuccess) e = launch_hotness_order(stream, a.keys, a.n, a.order, at + plan.sort, job.err);
