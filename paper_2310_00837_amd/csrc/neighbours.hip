@@ -70,7 +70,11 @@ __global__ __launch_bounds__(kBlock) void block_mean_kernel(MeanJob p) {
         if (p.own) {
             const int64_t self = p.row ? p.row[row] : row;
             if (self >= 0 && self < p.n_src) copy_8_of<TYPE>(p.x, self * p.x_ld + col, p.own, row * p.own_ld + col, valid);
-            else raise(p.err, kErrData);
+            else {
+                const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                store_8_of<TYPE>(p.own, row * p.own_ld + col, valid, none);
+                raise(p.err, kErrData);
+            }
         }
         const bool fits = good_list(list, p.n_col);
         if (!fits) raise(p.err, kErrData);

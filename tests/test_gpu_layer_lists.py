@@ -92,3 +92,28 @@ def test_transposing_lists_that_lie_wrong_is_reported(helios, h, n, fan):
             assert e.value.code == helios.EDATA, name
     _transposed(h, indptr, col, row, n_src)
     h.sync()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("d", [1, 16, 300])
+def test_own_row_of_a_source_that_there_is_none_of_is_zeros(helios, h, dtype, d):
+    """Whatever own held before, with `row` and without; the rows around it are theirs."""
+    x = _rand(10, d, 1).to(dtype).cuda()
+    indptr, col = torch.zeros(13, dtype=torch.int64, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    for bad in (-1, 10, 2 ** 31 - 1, None):
+        mean, own = (torch.full((12, d), float("nan"), dtype=dtype, device="cuda") for _ in range(2))
+        at = torch.arange(12, dtype=torch.int32) % 10
+        row = None
+        if bad is not None:
+            at[[0, 7]] = bad
+            row = at.cuda()
+        else:
+            at = torch.arange(12)
+        h.block_mean(x, indptr, col, mean, row=row, own=own)
+        with pytest.raises(helios.HeliosError) as e:
+            h.sync()
+        assert e.value.code == helios.EDATA
+        there = (at >= 0) & (at < 10)
+        want = torch.zeros((12, d), dtype=dtype)
+        want[there] = x.cpu()[at[there].long()]
+        assert torch.equal(own.cpu(), want) and bool((mean == 0).all())
