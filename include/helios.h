@@ -676,8 +676,8 @@ int helios_block_transpose(helios_ctx *ctx, int64_t n_rows, const int64_t *n_row
  * source is u; zeros where there are none.  indptr as in helios_block_mean,
  * src_indptr and src_entry (n_entries: its room) from helios_block_transpose;
  * down is needed if that was given `row`.  dmean, down and dx [n_src x width]
- * are of x_type.  Entries that fit no row are left out and reported as
- * HELIOS_EDATA. */
+ * are of x_type.  Entries that fit no row, or a row without samples, are
+ * left out and reported as HELIOS_EDATA. */
 typedef struct {
     int64_t n_rows, width, n_src, n_entries;
     int32_t x_type, reserved;

@@ -385,13 +385,14 @@ template <int TYPE>
 __device__ __forceinline__ void share_of(const MeanGradJob& p, int32_t entry, bool wanted, int col, int valid, Raw8<TYPE>& v, float* weight) {
     const bool own = entry < 0;
     const int64_t row = own ? ~entry : entry;
-    const bool good = row < p.n_rows && (!own || p.down);
-    if (wanted && !good) raise(p.err, kErrData);
+    bool good = row < p.n_rows && (!own || p.down);
     *weight = 1.0f;
     if (wanted && good && !own) {
         const RowBounds list = row_bounds(p.indptr, static_cast<uint32_t>(row));
-        *weight = 1.0f / static_cast<float>(list.hi - list.lo);
+        good = list.lo < list.hi;                 // (a row without samples has no share)
+        *weight = good ? 1.0f / static_cast<float>(list.hi - list.lo) : 0.0f;
     }
+    if (wanted && !good) raise(p.err, kErrData);
     v.clear();
     if (wanted && good) v.load(own ? p.down : p.dmean, row * (own ? p.down_ld : p.dmean_ld) + col, valid);
 }

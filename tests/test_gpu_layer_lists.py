@@ -117,3 +117,15 @@ def test_own_row_of_a_source_that_there_is_none_of_is_zeros(helios, h, dtype, d)
         want = torch.zeros((12, d), dtype=dtype)
         want[there] = x.cpu()[at[there].long()]
         assert torch.equal(own.cpu(), want) and bool((mean == 0).all())
+
+
+def test_gradient_of_a_sample_of_a_row_without_samples_is_left_out(helios, h):
+    """An entry that names row 1, whose list is empty (or backwards), adds nothing, and is reported; those of row 0 count."""
+    dmean, si, se = _rand(3, 16, 1).float().cuda(), torch.tensor([0, 2, 3, 3], dtype=torch.int32, device="cuda"), torch.tensor([0, 1, 1], dtype=torch.int32, device="cuda")
+    for indptr in ([0, 2, 2, 3], [0, 2, 1, 3]):
+        dx = torch.full((3, 16), -7.0, device="cuda")
+        h.block_mean_grad(torch.tensor(indptr, dtype=torch.int64, device="cuda"), si, se, dmean, dx)
+        with pytest.raises(helios.HeliosError) as e:
+            h.sync()
+        assert e.value.code == helios.EDATA
+        assert torch.equal(dx[0], dmean[0] / 2) and bool((dx[1:] == 0).all())
