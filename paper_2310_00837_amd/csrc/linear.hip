@@ -340,13 +340,20 @@ struct ProductArgs {
     int32_t n;
     Count rows;
     uint32_t tiles_n, members, tiles;             // (members: of a group)
+    bool dealt;                                   // fewer groups than XCDs
     int slices;                                   // parts that k is cut into where it runs over rows, each with sums of its own
     OUT out;
 };
 
 // Workgroups go round the eight XCDs, each of which has an L2 of its own.  The tiles that share what is long (rows of A; where k runs
-// over rows, a slice of it) are a group, and a group's tiles are neighbours on one XCD.
-__device__ __forceinline__ void tile_of(uint32_t block, uint32_t members, uint32_t* group, uint32_t* member) {
+// over rows, a slice of it) are a group, and a group's tiles are neighbours on one XCD; fewer than eight groups are dealt out to all
+// XCDs (gradient of 64 x 2048 x 1024 in bfloat16, all of dw one group: 22.6 us on one XCD, 11.5 on all; 200 x 2048 x 1024 31 and 12).
+__device__ __forceinline__ void tile_of(uint32_t block, uint32_t members, bool dealt, uint32_t* group, uint32_t* member) {
+    if (dealt) {
+        *group = block / members;
+        *member = block % members;
+        return;
+    }
     const uint32_t xcd = block % 8, at = block / 8;
     *group = at / members * 8 + xcd;
     *member = at % members;
@@ -445,7 +452,7 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
     const int wave = threadIdx.x / kWave, wave_m = wave / WAVES_N, wave_n = wave % WAVES_N;
     for (uint32_t tile = block; tile < p.tiles; tile += blocks) {      // (once round, but for the longest lists)
         uint32_t group, member;
-        tile_of(tile, p.members, &group, &member);
+        tile_of(tile, p.members, p.dealt, &group, &member);
         const int slice = rows_are_k ? static_cast<int>(group) : 0;
         const int64_t m0 = static_cast<int64_t>(rows_are_k ? member / p.tiles_n : group) * BM;
         const int32_t n0 = static_cast<int32_t>(rows_are_k ? member % p.tiles_n : member) * BN;
@@ -859,7 +866,8 @@ template <class TILE, class OUT>
 bool lay_out(ProductArgs<OUT>* p, bool by_slices, uint32_t* blocks) {
     p->tiles_n = tiles_of(p->n, TILE::kN);
     const int64_t tiles_m = tiles_of(p->m, TILE::kM), members = by_slices ? tiles_m * p->tiles_n : p->tiles_n, groups = by_slices ? p->slices : tiles_m;
-    const int64_t tiles = (groups + 7) / 8 * 8 * members;
+    p->dealt = groups < 8;
+    const int64_t tiles = (p->dealt ? groups : (groups + 7) / 8 * 8) * members;
     p->members = static_cast<uint32_t>(members);
     p->tiles = static_cast<uint32_t>(tiles);
     *blocks = static_cast<uint32_t>(std::min<int64_t>(tiles, kMostBlocks));
@@ -942,6 +950,7 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
 }
 
 constexpr int64_t kOneSliceRows = 256;
+constexpr int64_t kManyTiles = 256;               // of dw
 struct GradPlan {                                 // of linear_grad: what lies where in the scratch, and how far k is cut up
     bool needs_dz, in_parts, large;               // in_parts: dz in two parts; large: by large tiles
     int64_t dz_ld, dz_low;                        // elements from a part of dz to the other
@@ -957,13 +966,15 @@ struct GradPlan {                                 // of linear_grad: what lies w
         dz_low = in_parts ? (n * dz_ld + 127) / 128 * 128 : 0;
         // dw's k, the rows, is cut so that there are about 1024 small tiles or 256 large ones, in eights (one for each XCD) of at least
         // four steps.  us, dw of 26 624 x 512 x 256 in bfloat16: small tiles 16 slices 21.7, 32 17.4; large ones 32 20.5, 64 19.3;
-        // 50 000 x 2048 x 512: large ones 4 slices 223, 8 141, 16 150.  Large tiles where there are enough of them for the CUs (in single
+        // 50 000 x 2048 x 512: large ones 4 slices 223, 8 141, 16 150.  Where dw's tiles alone fill the CUs, parts of its sums are only more to write
+        // (and scratch of eight times dw in 32 bits), us in bfloat16 by eight / one: 4096 x 4096 x 2048 228 / 77, 4096 x 4096 x 4096 457 / 149,
+        // 2048 x 8192 x 8192 1345 / 300, 4096 x 2048 x 2048 (256 tiles) 84 / 67; in single precision 530 / 378, 1030 / 760, 2447 / 1541, 246 / 192.  Large tiles where there are enough of them for the CUs (in single
         // precision, where a tile takes longest, for half of them), us by small / large: 5000 x 256 x 256 in bfloat16 16.4 / 18.9, in
         // single precision 32.2 / 29.5; 26 624 x 512 x 256 50.1 / 44.9; 50 000 x 2048 x 512 598 / 333.
         const auto tiles = [](int64_t m, int64_t n, int64_t edge) { return (m + edge - 1) / edge * ((n + edge - 1) / edge); };
         const int64_t steps = (n * type_bytes(j.x_type) + kStageBytes - 1) / kStageBytes;
         const auto cut = [&](int64_t edge, int64_t most) {
-            const int64_t want = std::max<int64_t>(1, std::min(std::max<int64_t>(most / tiles(j.n_out, j.n_in, edge), 8), steps / 4));
+            const int64_t alone = tiles(j.n_out, j.n_in, edge), want = std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(most / alone, alone < kManyTiles ? 8 : 1), steps / 4));
             return static_cast<int>(want >= 8 ? want / 8 * 8 : want);
         };
         // Where dx is asked for, too, its tiles fill the CUs beside dw's, and in single precision, where a CU has one tile at a time, fewer and longer
