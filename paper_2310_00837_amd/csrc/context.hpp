@@ -21,6 +21,7 @@ constexpr int kCntList = 48;        // [kBatchTables] length of the ID list that
 constexpr int kCntHoles = 56;       // not 0: the hotness order left a node without a rank
 constexpr int kCntStage = 64;       // [HELIOS_MAX_HOPS][kStageWords] totals after every stage of a batch's compaction
 constexpr int kNumCounters = kCntStage + HELIOS_MAX_HOPS * kStageWords;
+constexpr int kMostOutgrown = 64;     // scratches of the operators of a layer that larger ones have replaced
 constexpr uint32_t kVarsRing = 256;   // batch launches that may be queued on a context without a helios_sync
 
 // rows of the scan status buffer: the two compactions that share a launch scan at the same time
@@ -146,10 +147,10 @@ struct helios_ctx {
     bool map_cursors_used = false;             // a build of the map has failed half way
 
     // scratch of the operators of a layer: what a larger call has outgrown stays, since a HIP graph may hold it (every
-    // growth at least doubles it, so there are few)
+    // growth doubles it while there is memory for that, so there are few)
     void* layer_scratch = nullptr;
     size_t layer_scratch_bytes = 0;
-    void* layer_outgrown[64] = {nullptr};
+    void* layer_outgrown[helios::kMostOutgrown] = {nullptr};
     int n_layer_outgrown = 0;
 };
 

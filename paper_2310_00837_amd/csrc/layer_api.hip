@@ -74,11 +74,21 @@ int scratch(helios_ctx* c, size_t bytes, char** at) {
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     HIP_TRY(c, hipStreamIsCapturing(c->stream, &capture));
     if (capture != hipStreamCaptureStatusNone) return fail(c, HELIOS_ESTATE, "the call needs scratch that it cannot allocate in a capture: make it once outside before");
+    const size_t needed = bytes;
     bytes = std::max<size_t>({bytes, 2 * c->layer_scratch_bytes, size_t{1} << 20});
     void* p = nullptr;
-    if (c->n_layer_outgrown >= 64) return fail(c, HELIOS_EINVAL, "scratch of %zu bytes", bytes);
-    HIP_TRY(c, hipMalloc(&p, bytes));
-    const hipError_t e = hipMemsetAsync(p, 0, kCounterBytes, c->stream);
+    if (c->n_layer_outgrown >= kMostOutgrown) return fail(c, HELIOS_ESTATE, "scratch has grown %d times in short steps: create the context anew", kMostOutgrown);
+    hipError_t e = hipMalloc(&p, bytes);
+    if (e != hipSuccess && needed < bytes) {      // (no room to grow into: what the call needs may still fit)
+        (void)hipGetLastError();
+        bytes = needed;
+        e = hipMalloc(&p, bytes);
+    }
+    if (e != hipSuccess) {
+        (void)hipGetLastError();                  // (not the next launch's)
+        return fail(c, HELIOS_EHIP, "scratch of %zu bytes: %s", bytes, hipGetErrorString(e));
+    }
+    e = hipMemsetAsync(p, 0, kCounterBytes, c->stream);
     if (e != hipSuccess) {
         (void)hipFree(p);
         return fail(c, HELIOS_EHIP, "hipMemsetAsync: %s", hipGetErrorString(e));

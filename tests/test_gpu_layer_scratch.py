@@ -57,3 +57,35 @@ def test_gradients_of_few_rows_with_wide_weights(helios, h, n, dtype):
     _close(dx, d @ wd, (m + 8) * U32 * (d.abs() @ wd.abs()), dtype)
     _close(dw, d.t() @ xd, (n + 8) * U32 * (d.abs().t() @ xd.abs()), dtype)
     _close(y, xd @ wd.t(), (k + 8) * U32 * (xd.abs() @ wd.abs().t()), dtype)
+
+
+def test_scratch_that_cannot_be_doubled_is_what_the_call_needs(helios, h):
+    """1 GiB of scratch, and 1.25 GiB asked for where 2 GiB are not to be had; then more than there is, which is an error of this call only."""
+    gib, width = 1 << 30, 1024
+    w, row = torch.ones((width, 8), device="cuda"), torch.ones((1, width), device="cuda")
+    rows = {q: int(q * gib / 4 / width) for q in (1.0, 1.25, 3.0)}
+    dx = torch.empty((rows[3.0], 8), device="cuda")
+
+    def call(q):                                  # (its scratch: dz, in single precision)
+        n = rows[q]
+        dx[:n].fill_(-7.0)
+        h.linear_grad(dx[:n], w, row.expand(n, width), act=helios.ACT_RELU, pre=row.expand(n, width), dx=dx[:n])
+        h.sync()
+        return bool((dx[:n] == width).all())
+
+    assert call(1.0)
+    room = []
+    try:
+        for _ in range(4):                        # (what is free afterwards is not to the byte what was asked to be left)
+            if _free() > 1.8 * gib:
+                room.append(torch.empty(_free() - int(1.6 * gib), dtype=torch.uint8, device="cuda"))
+        assert 1.3 * gib < _free() < 1.9 * gib
+        assert call(1.25)
+        with pytest.raises(helios.HeliosError) as e:
+            call(3.0)
+        assert e.value.code == helios.EHIP and "scratch" in str(e.value)
+        assert call(1.25) and call(1.0)
+    finally:
+        room.clear()
+        torch.cuda.empty_cache()
+    assert call(3.0)
