@@ -346,8 +346,8 @@ struct ProductArgs {
 };
 
 // Workgroups go round the eight XCDs, each of which has an L2 of its own.  The tiles that share what is long (rows of A; where k runs
-// over rows, a slice of it) are a group, and a group's tiles are neighbours on one XCD; fewer than eight groups are dealt out to all
-// XCDs (gradient of 64 x 2048 x 1024 in bfloat16, all of dw one group: 22.6 us on one XCD, 11.5 on all; 200 x 2048 x 1024 31 and 12).
+// over rows, a slice of it) are a group, and a group's tiles are neighbours on one XCD; in gradients
+// fewer than eight groups are dealt out to all XCDs (gradient of 64 x 2048 x 1024 in bfloat16, all of dw one group: 22.6 us on one XCD, 11.5 on all; 200 x 2048 x 1024 31 and 12).
 __device__ __forceinline__ void tile_of(uint32_t block, uint32_t members, bool dealt, uint32_t* group, uint32_t* member) {
     if (dealt) {
         *group = block / members;
@@ -452,7 +452,7 @@ __device__ __forceinline__ void product(ProductArgs<OUT> p, uint32_t block, uint
     const int wave = threadIdx.x / kWave, wave_m = wave / WAVES_N, wave_n = wave % WAVES_N;
     for (uint32_t tile = block; tile < p.tiles; tile += blocks) {      // (once round, but for the longest lists)
         uint32_t group, member;
-        tile_of(tile, p.members, p.dealt, &group, &member);
+        tile_of(tile, p.members, B_STRIDED && p.dealt, &group, &member);
         const int slice = rows_are_k ? static_cast<int>(group) : 0;
         const int64_t m0 = static_cast<int64_t>(rows_are_k ? member / p.tiles_n : group) * BM;
         const int32_t n0 = static_cast<int32_t>(rows_are_k ? member % p.tiles_n : member) * BN;
@@ -861,12 +861,12 @@ bool direct(const Operand& o, int bytes) {
     return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % 16 == 0 && o.cols * bytes % 16 == 0;
 }
 
-// The tiles of a product (by_slices: k runs over rows and is cut up) and the workgroups for them; false if there are too many.
+// The tiles of a product (by_slices: k runs over rows and is cut up; deal: fewer groups than XCDs are dealt out to all of them) and the workgroups for them; false if there are too many.
 template <class TILE, class OUT>
-bool lay_out(ProductArgs<OUT>* p, bool by_slices, uint32_t* blocks) {
+bool lay_out(ProductArgs<OUT>* p, bool by_slices, bool deal, uint32_t* blocks) {
     p->tiles_n = tiles_of(p->n, TILE::kN);
     const int64_t tiles_m = tiles_of(p->m, TILE::kM), members = by_slices ? tiles_m * p->tiles_n : p->tiles_n, groups = by_slices ? p->slices : tiles_m;
-    p->dealt = groups < 8;
+    p->dealt = deal && groups < 8;
     const int64_t tiles = (p->dealt ? groups : (groups + 7) / 8 * 8) * members;
     p->members = static_cast<uint32_t>(members);
     p->tiles = static_cast<uint32_t>(tiles);
@@ -877,7 +877,7 @@ bool lay_out(ProductArgs<OUT>* p, bool by_slices, uint32_t* blocks) {
 template <int TYPE, class TILE, class OUT>
 hipError_t launch_forward(hipStream_t stream, ProductArgs<OUT> p) {
     uint32_t blocks = 0;
-    if (!lay_out<TILE>(&p, false, &blocks)) return hipErrorInvalidValue;
+    if (!lay_out<TILE>(&p, false, false, &blocks)) return hipErrorInvalidValue;
     if (direct(p.a, type_bytes(TYPE)) && direct(p.b, type_bytes(TYPE)))
         hipLaunchKernelGGL((forward_kernel<TYPE, TILE, true, OUT>), dim3(blocks), dim3(TILE::kThreads), 0, stream, p);
     else hipLaunchKernelGGL((forward_kernel<TYPE, TILE, false, OUT>), dim3(blocks), dim3(TILE::kThreads), 0, stream, p);
@@ -892,12 +892,12 @@ hipError_t launch_backward(hipStream_t stream, ProductArgs<PlainOut<TYPE>>* dw, 
     uint32_t dw_blocks = 0, dx_blocks = 0;
     bool straight = true;
     if (dw) {
-        if (!lay_out<TILE>(dw, true, &dw_blocks)) return hipErrorInvalidValue;
+        if (!lay_out<TILE>(dw, true, true, &dw_blocks)) return hipErrorInvalidValue;
         straight = straight && direct(dw->a, type_bytes(TYPE)) && direct(dw->b, type_bytes(TYPE));
         w = *dw;
     }
     if (dx) {
-        if (!lay_out<TILE>(dx, false, &dx_blocks)) return hipErrorInvalidValue;
+        if (!lay_out<TILE>(dx, false, true, &dx_blocks)) return hipErrorInvalidValue;
         straight = straight && direct(dx->a, type_bytes(TYPE)) && direct(dx->b, type_bytes(TYPE));
         x = *dx;
     }
