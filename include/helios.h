@@ -508,7 +508,7 @@ typedef enum {
 typedef enum {
     HELIOS_ACT_NONE = 0,
     HELIOS_ACT_RELU = 1,
-    HELIOS_ACT_GELU = 2, /* z * Phi(z), with the error function */
+    HELIOS_ACT_GELU = 2, /* z * Phi(z), with the error function (16-bit results: Phi to 1.5e-7) */
     HELIOS_ACT_SILU = 3  /* z / (1 + exp(-z)) */
 } helios_act;
 

@@ -301,7 +301,7 @@ struct ForwardOut {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += c.bias[e];
         if (pre) store_8_of<OUT_TYPE>(pre, row * pre_ld + c.col, c.valid, v);
-        if (SMOOTH) act_8(act, v);
+        if (SMOOTH) act_8<OUT_TYPE == kF32>(act, v);
         else
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = v[e] < c.least ? c.least : v[e];        // NaN stays
@@ -790,7 +790,7 @@ __global__ __launch_bounds__(kBlock) void slope_kernel(SlopeArgs p) {
 #pragma unroll
             for (int k = 0; k < kSlopeRows; ++k) {
                 if (row + kSubs * k >= row1) continue;
-                if (SLOPE) scale_by_slope_8(p.act, z[k], d[k]);
+                if (SLOPE) scale_by_slope_8<TYPE == kF32>(p.act, z[k], d[k]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += d[k][e];
                 if (!p.dz) continue;

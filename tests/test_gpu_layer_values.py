@@ -87,3 +87,52 @@ def test_gradients_in_16_bits_keep_infinities_and_nan_to_their_rows_and_columns(
         clean, size = b[:, cols].abs(), a[rows].abs()
         assert int(rows.sum()) >= a.shape[0] - 1 and int(cols.sum()) >= b.shape[1] - 2
         _close(have[rows][:, cols], want[rows][:, cols], a_off[rows] @ clean + 3 * (a.shape[1] + 8) * U32 * (size @ clean), x_type)
+
+
+# ------------------------------------------------------------------ activations in single precision
+
+
+def _line(lo, hi, n):
+    return torch.linspace(lo, hi, n, dtype=torch.float64).float()
+
+
+def _relative(have, want, bound, what):
+    """bound: relative to want's size, per element (and what subnormal values lose)"""
+    off = (have.double().cpu() - want).abs()
+    worse = off - bound - 2.0 ** -126
+    assert float(worse.max()) <= 0, f"{what}: {int((worse > 0).sum())} off, the worst {float((off / want.abs().clamp_min(1e-300))[worse > 0].max()):.3g} of its value"
+
+
+@pytest.mark.parametrize("out", ["few", "tiles"])
+@pytest.mark.parametrize("x_type", [F32, F16, BF16], ids=str)
+def test_activations_with_results_in_single_precision(helios, h, x_type, out):
+    """x of one column and weights of 1: z is x.  GELU is z erfc(-z / sqrt 2) / 2: the argument is off by 2^-23, which changes erfc(u) by 2 u^2 = z^2
+    times as much; the functions themselves are good to four units in the last place, and a few roundings follow."""
+    n, m = (2000, 64) if out == "tiles" else (500, 16)
+    for act, lo, hi in (("gelu", -9.0, 9.0), ("silu", -80.0, 80.0)):
+        x = _line(lo, hi, n).to(x_type)[:, None]
+        y = torch.empty((n, m), device="cuda")
+        h.linear(x.cuda(), torch.ones((m, 1), dtype=x_type, device="cuda"), y, act=getattr(helios, "ACT_" + act.upper()))
+        h.sync()
+        z = x.double()
+        want = z * 0.5 * torch.special.erfc(-z / 2 ** 0.5) if act == "gelu" else z * torch.sigmoid(z)
+        bound = (8 + z * z) * 2.0 ** -23 if act == "gelu" else 8 * 2.0 ** -23
+        for col in (0, m - 1):
+            _relative(y[:, col:col + 1], want, bound * want.abs(), f"{act} {x_type}")
+
+
+@pytest.mark.parametrize("x_type", [F32, F16, BF16], ids=str)
+def test_slopes_in_single_precision(helios, h, x_type):
+    """dbias of one row is dz.  GELU's slope is the sum of Phi and z times the density, each good to (8 + z^2) 2^-23, SiLU's of p and z p (1 - p)."""
+    n = 4001
+    for act, lo, hi in (("gelu", -9.0, 9.0), ("silu", -80.0, 80.0)):
+        z = _line(lo, hi, n)[None, :]
+        x, w, db = torch.ones((1, 1), dtype=x_type, device="cuda"), torch.ones((n, 1), dtype=x_type, device="cuda"), torch.empty(n, device="cuda")
+        h.linear_grad(x, w, torch.ones((1, n), device="cuda"), act=getattr(helios, "ACT_" + act.upper()), pre=z.cuda(), dbias=db)
+        h.sync()
+        z = z.double()[0]
+        if act == "gelu":
+            a, b, good = 0.5 * torch.special.erfc(-z / 2 ** 0.5), z * torch.exp(-z * z / 2) * 0.3989422804014327, (8 + z * z) * 2.0 ** -23
+        else:
+            a, b, good = torch.sigmoid(z), z * torch.sigmoid(z) * torch.sigmoid(-z), 8 * 2.0 ** -23
+        _relative(db, a + b, good * (a.abs() + b.abs()), act)
