@@ -136,3 +136,40 @@ def test_slopes_in_single_precision(helios, h, x_type):
         else:
             a, b, good = torch.sigmoid(z), z * torch.sigmoid(z) * torch.sigmoid(-z), 8 * 2.0 ** -23
         _relative(db, a + b, good * (a.abs() + b.abs()), act)
+
+
+# ------------------------------------------------------------------ products of single precision in three parts
+
+
+def _products(helios, h, a, b):
+    """Every product of two values that the three products of a layer make of them, in tiles: k is 1."""
+    n, m = a.numel(), b.numel()
+    x, w, y = a[:, None].cuda(), b[:, None].cuda(), torch.empty((n, m), device="cuda")
+    h.linear(x, w, y)
+    dx, dw = torch.empty((n, m), device="cuda"), torch.empty((m, n), device="cuda")
+    h.linear_grad(torch.empty((n, m), device="cuda"), b[None, :].cuda(), x, dx=dx)                       # n_out 1: dx = x w
+    h.linear_grad(a[None, :].cuda(), torch.empty((m, n), device="cuda"), b[None, :].cuda(), dw=dw)       # one row: dw = dy^T x
+    h.sync()
+    return y.double().cpu(), dx.double().cpu(), dw.double().cpu().t()
+
+
+def test_products_of_single_values(helios, h):
+    """What is left out of a product is at most 2^-23 of it, the last addition is off by at most 2^-23 (if it is not rounded to the nearest), the
+    four before it by that of what they add, which is below 2^-7 of the product.  Values next to where a part changes are among them."""
+    near = [1 + 2.0 ** -i + s * 2.0 ** -23 for i in (7, 8, 9, 15, 16) for s in (-2, -1, 0, 1, 2)]
+    a = torch.cat([torch.tensor(near, dtype=torch.float64).float(), (_rand(1, 1975, 1)[0]).float()])
+    b = torch.cat([torch.tensor(near, dtype=torch.float64).float(), (_rand(1, 295, 2)[0]).float()])
+    want = a.double()[:, None] * b.double()[None, :]
+    for name, got in zip(("y", "dx", "dw"), _products(helios, h, a, b)):
+        worst = float(((got - want).abs() / want.abs()).max())
+        assert worst <= 2.0 ** -22 * (1 + 2.0 ** -4), f"{name}: {worst * 2 ** 24:.3g} 2^-24"
+
+
+def test_products_of_the_largest_values(helios, h):
+    """Values that bfloat16 has none as large as: the parts are not finite, the products are."""
+    top = torch.finfo(torch.float32).max
+    a = torch.cat([torch.tensor([top, -top, 0.999 * top, 0.996 * top, 1.0]), torch.ones(1995)])
+    b = torch.cat([torch.tensor([0.5, 2.0 ** -20, 1.0]), torch.full((317,), 2.0 ** -100)])
+    want = a.double()[:, None] * b.double()[None, :]
+    for got in _products(helios, h, a, b):
+        assert float(((got - want).abs() / want.abs()).max()) <= 2.0 ** -22
