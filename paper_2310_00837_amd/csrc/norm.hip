@@ -129,13 +129,18 @@ __device__ __forceinline__ void norm_row(const NormJob& p, int64_t row, int lane
             most = a > most || a != a ? a : most;
         }
     most = row_max<LANES>(most, s) / kE4M3Max;
+    // (y / scale, correctly rounded, by way of the reciprocal and one step of Newton's: by the reciprocal alone a quotient can fall to the wrong
+    // side of the middle between two values of 8 bits.  An infinite scale leaves 0 of what is finite.)
     const float scale = most < kMinScale ? kMinScale : most, inv = 1.0f / scale;
     if (lane == 0) p.y_scale[row] = scale;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int col = (c * LANES + lane) * 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[c][e] *= inv;
+        for (int e = 0; e < 8; ++e) {
+            const float near = t[c][e] * inv;     // t / scale, but for its last bit
+            t[c][e] = inv > 0.0f ? __builtin_fmaf(__builtin_fmaf(-near, scale, t[c][e]), inv, near) : near;
+        }
         store_8_of_e4m3(p.y, row * p.y_ld + col, p.width - col, t[c]);
     }
 }

@@ -173,3 +173,46 @@ def test_products_of_the_largest_values(helios, h):
     want = a.double()[:, None] * b.double()[None, :]
     for got in _products(helios, h, a, b):
         assert float(((got - want).abs() / want.abs()).max()) <= 2.0 ** -22
+
+
+# ------------------------------------------------------------------ rows in 8 bits
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+def test_rows_in_8_bits_are_their_quotients_rounded(helios, h, dtype):
+    """Quotients that lie in the middle between two values of 8 bits go to the even one: x / scale in 32 bits is exact there, x times 1 / scale is not
+    always."""
+    values = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    middle = (values[1:] + values[:-1]) / 2
+    middle = middle[middle >= 2.0 ** -4]
+    rows = []
+    for s in range(1, 400 if dtype == F32 else 8, 2):
+        rows.append(torch.cat([torch.tensor([448.0]), middle, -middle]) * s)
+    x = torch.stack(rows) * (1.0 if dtype != F16 else 2.0 ** -2)
+    want_s = x[:, 0] / 448
+    exact = x.to(dtype).float() == x
+    assert bool(exact.all())
+    quotient = (x / want_s[:, None])
+    want = quotient.to(torch.float8_e4m3fn)
+    if dtype == F32:
+        assert not torch.equal((x * (1 / want_s)[:, None]).to(torch.float8_e4m3fn).view(torch.uint8), want.view(torch.uint8))
+    q, scale = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(len(rows), device="cuda")
+    h.quantize_rows(x.to(dtype).cuda(), q, scale)
+    h.sync()
+    assert torch.equal(scale.cpu(), want_s)
+    assert torch.equal(q.cpu().view(torch.uint8), want.view(torch.uint8))
+
+
+@pytest.mark.parametrize("d", [40, 700, 5000])
+def test_rows_in_8_bits_with_infinities(helios, h, d):
+    """The scale is infinite: what is finite is 0, what is not is NaN, as x / scale is; and a row of NaN is NaN."""
+    x = _rand(4, d, 1).float()
+    x[1, d // 2], x[2, 3] = -float("inf"), float("nan")
+    q, scale = torch.empty((4, d), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(4, device="cuda")
+    h.quantize_rows(x.cuda(), q, scale)
+    h.sync()
+    q, scale = q.float().cpu(), scale.cpu()
+    assert float(scale[1]) == float("inf") and bool(torch.isnan(q[1, d // 2])) and int((q[1] == 0).sum()) == d - 1
+    assert bool(torch.isnan(scale[2])) and bool(torch.isnan(q[2]).all())
+    for i in (0, 3):
+        assert torch.equal(q[i], (x[i] / (x[i].abs().max() / 448)).to(torch.float8_e4m3fn).float())
