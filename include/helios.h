@@ -544,7 +544,8 @@ int helios_linear(helios_ctx *ctx, const helios_linear_args *args);
 /* Gradients of helios_linear: dz = dy * act'(pre), dx = dz w, dw = dz^T x,
  * dbias = the sum of dz's rows.  x, w and dx, dw are of x_type (not
  * HELIOS_E4M3), dy, pre and dbias of out_type.  pre is needed only with an
- * activation (relu's slope at 0 is 0); dx, dw and dbias are nullable.  The residual's gradient is
+ * activation (relu's slope at 0 is 0; at the infinities slopes are their
+ * limits); dx, dw and dbias are nullable.  The residual's gradient is
  * dy itself.  dbias is summed from the unrounded dz.  In 16 bits the products
  * take dz as it is where x_type holds it (no activation or relu, and out_type =
  * x_type), else in two parts of bfloat16: to 2^-16 of its value, in the range

@@ -180,18 +180,19 @@ __device__ __forceinline__ void act_8(int act, float (&v)[8]) {
     else if (act == kActGelu) act_each<kActGelu, PRECISE>(v);
     else if (act == kActSilu) act_each<kActSilu, PRECISE>(v);
 }
+// (at the infinities, which half precision keeps of a z beyond 65504, the slopes are their limits, 0 and 1)
 template <bool PRECISE>
 __device__ __forceinline__ float act_slope(int act, float z) {
     if (act == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
     if (act == kActGelu) {
         float density;
         const float phi = normal_cdf<PRECISE>(z, &density);
-        return phi + z * density;
+        return phi + __builtin_amdgcn_fmed3f(z, -128.0f, 128.0f) * density;            // (beyond, the density is 0)
     }
     if (act == kActSilu) {
         float e;
         const float p = logistic<PRECISE>(z, &e), q = z > 0.0f ? e * p : 1.0f - p;     // (q: 1 - p, also where p is all but 1)
-        return p * (1.0f + z * q);
+        return p * (1.0f + __builtin_amdgcn_fmed3f(z, -128.0f, 128.0f) * q);           // (beyond, p or q is 0)
     }
     return 1.0f;
 }

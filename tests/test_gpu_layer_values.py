@@ -216,3 +216,47 @@ def test_rows_in_8_bits_with_infinities(helios, h, d):
     assert bool(torch.isnan(scale[2])) and bool(torch.isnan(q[2]).all())
     for i in (0, 3):
         assert torch.equal(q[i], (x[i] / (x[i].abs().max() / 448)).to(torch.float8_e4m3fn).float())
+
+
+# ------------------------------------------------------------------ slopes far out
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=str)
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+@pytest.mark.parametrize("n", [5, 3000])
+def test_slopes_far_out_are_their_limits(helios, h, n, act, dtype):
+    """0 and 1 at the infinities and at values that any type's exponential is 0 or infinite for; a NaN stays one."""
+    m, k = 64, 40
+    far = torch.tensor([float("inf"), 300.0, 60000.0, -float("inf"), -300.0, -60000.0, 1.0, float("nan")])
+    pre = far.repeat(n, m // 8).to(dtype)
+    dy, w = _rand(n, m, 1).to(dtype), _rand(m, k, 2).to(dtype)
+    slope = torch.tensor([1.0, 1.0, 1.0, 0.0, 0.0, 0.0]).double()
+    db, dx = torch.empty(m, dtype=dtype, device="cuda"), torch.empty((n, k), dtype=dtype, device="cuda")
+    code = getattr(helios, "ACT_" + act.upper())
+    h.linear_grad(torch.empty((n, k), dtype=dtype, device="cuda"), w.cuda(), dy.cuda(), act=code, pre=pre.cuda(), dbias=db)
+    h.sync()
+    got, d = db.double().cpu().view(-1, 8), dy.double().view(n, -1, 8)
+    want = d[:, :, :6].sum(0) * slope
+    _close(got[:, :6].reshape(-1, 6), want, (n + 8) * U32 * d[:, :, :6].abs().sum(0), dtype)
+    assert bool(torch.isfinite(got[:, 6]).all())
+    assert bool((torch.isnan(got[:, 7]) == (act != "relu")).all())
+    keep = torch.arange(m) % 8 < 6                # without the NaN: dx in full
+    h.linear_grad(torch.empty((n, k), dtype=dtype, device="cuda"), w[keep].contiguous().cuda(), dy[:, keep].contiguous().cuda(), act=code,
+                  pre=pre[:, keep].contiguous().cuda(), dx=dx)
+    h.sync()
+    dz, wd = (d[:, :, :6] * slope).reshape(n, -1), w[keep].double()
+    _close(dx, dz @ wd, 3 * (m + 8) * U32 * (dz.abs() @ wd.abs()), dtype)
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_gradient_where_half_precision_keeps_an_infinite_z(helios, h, act):
+    """z is -1e5: the result is 0, the z that is kept is -inf, and its gradients are 0."""
+    n, k, m = 20, 8, 24
+    x, w = torch.full((n, k), 125.0, dtype=F16, device="cuda"), torch.full((m, k), -100.0, dtype=F16, device="cuda")
+    y, z, dx, dw = torch.empty((n, m), dtype=F16, device="cuda"), torch.empty((n, m), dtype=F16, device="cuda"), torch.empty_like(x), torch.empty_like(w)
+    code = getattr(helios, "ACT_" + act.upper())
+    h.linear(x, w, y, act=code, pre=z)
+    h.linear_grad(x, w, torch.ones_like(y), act=code, pre=z, dx=dx, dw=dw)
+    h.sync()
+    assert bool((y == 0).all()) and bool((z == -float("inf")).all())
+    assert bool((dx == 0).all()) and bool((dw == 0).all())
