@@ -160,55 +160,43 @@ __device__ __forceinline__ float logistic(float z, float* e) {
     *e = PRECISE ? expf(-z) : __expf(-z);
     return PRECISE ? 1.0f / (1.0f + *e) : __builtin_amdgcn_rcpf(1.0f + *e);
 }
-template <bool PRECISE>
-__device__ __forceinline__ float act_of(int act, float z) {
-    if (act == kActRelu) return z < 0.0f ? 0.0f : z;                                   // NaN stays NaN
-    float other;
-    if (act == kActGelu) return z * normal_cdf<PRECISE>(z, &other);
-    if (act == kActSilu) return z * logistic<PRECISE>(z, &other);
-    return z;
-}
-// the same for eight values (one branch for all of them)
-template <int ACT, bool PRECISE>
-__device__ __forceinline__ void act_each(float (&v)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act_of<PRECISE>(ACT, v[e]);
-}
+// GELU or SiLU of eight values (one branch for all of them)
 template <bool PRECISE>
 __device__ __forceinline__ void act_8(int act, float (&v)[8]) {
-    if (act == kActRelu) act_each<kActRelu, PRECISE>(v);
-    else if (act == kActGelu) act_each<kActGelu, PRECISE>(v);
-    else if (act == kActSilu) act_each<kActSilu, PRECISE>(v);
+    float other;
+    if (act == kActGelu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= normal_cdf<PRECISE>(v[e], &other);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= logistic<PRECISE>(v[e], &other);
+    }
 }
 // (at the infinities, which half precision keeps of a z beyond 65504, the slopes are their limits, 0 and 1)
 template <bool PRECISE>
-__device__ __forceinline__ float act_slope(int act, float z) {
-    if (act == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
-    if (act == kActGelu) {
-        float density;
-        const float phi = normal_cdf<PRECISE>(z, &density);
-        return phi + __builtin_amdgcn_fmed3f(z, -128.0f, 128.0f) * density;            // (beyond, the density is 0)
-    }
-    if (act == kActSilu) {
-        float e;
-        const float p = logistic<PRECISE>(z, &e), q = z > 0.0f ? e * p : 1.0f - p;     // (q: 1 - p, also where p is all but 1)
-        return p * (1.0f + __builtin_amdgcn_fmed3f(z, -128.0f, 128.0f) * q);           // (beyond, p or q is 0)
-    }
-    return 1.0f;
+__device__ __forceinline__ float gelu_slope(float z) {
+    float density;
+    const float phi = normal_cdf<PRECISE>(z, &density);
+    return phi + __builtin_amdgcn_fmed3f(z, -128.0f, 128.0f) * density;                // (beyond, the density is 0)
 }
-
+template <bool PRECISE>
+__device__ __forceinline__ float silu_slope(float z) {
+    float e;
+    const float p = logistic<PRECISE>(z, &e), q = z > 0.0f ? e * p : 1.0f - p;         // (q: 1 - p, also where p is all but 1)
+    return p * (1.0f + __builtin_amdgcn_fmed3f(z, -128.0f, 128.0f) * q);               // (beyond, p or q is 0)
+}
 // v *= the slopes at z
 template <bool PRECISE>
 __device__ __forceinline__ void scale_by_slope_8(int act, const float (&z)[8], float (&v)[8]) {
     if (act == kActRelu) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= act_slope<PRECISE>(kActRelu, z[e]);
+        for (int e = 0; e < 8; ++e) v[e] *= z[e] > 0.0f ? 1.0f : 0.0f;
     } else if (act == kActGelu) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= act_slope<PRECISE>(kActGelu, z[e]);
-    } else if (act == kActSilu) {
+        for (int e = 0; e < 8; ++e) v[e] *= gelu_slope<PRECISE>(z[e]);
+    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= act_slope<PRECISE>(kActSilu, z[e]);
+        for (int e = 0; e < 8; ++e) v[e] *= silu_slope<PRECISE>(z[e]);
     }
 }
 
