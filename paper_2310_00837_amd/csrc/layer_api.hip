@@ -14,6 +14,7 @@ constexpr int64_t kMaxCount = (1ll << 31) - 1024;
 int bytes_of(int type) { return type == HELIOS_F32 ? 4 : type == HELIOS_E4M3 ? 1 : 2; }
 bool is_float(int type) { return type == HELIOS_F32 || type == HELIOS_F16 || type == HELIOS_BF16; }
 
+constexpr int64_t kMaxSpan = 1ll << 57;           // bytes from a matrix's first row to the end of its last: more than can be addressed
 // An array of a call, as its checks see it.
 struct Matrix {
     const char* name;
@@ -43,7 +44,7 @@ int check(helios_ctx* c, const Matrix* m, int n, const uint32_t* twins) {
         if (reinterpret_cast<uintptr_t>(m[i].data) % m[i].bytes != 0) return fail(c, HELIOS_EINVAL, "%s is not aligned to its elements", m[i].name);
         if (m[i].ld < m[i].cols && (m[i].written || m[i].ld != 0))
             return fail(c, HELIOS_EINVAL, "%s: rows are %lld elements apart, narrower than %lld", m[i].name, (long long)m[i].ld, (long long)m[i].cols);
-        if (m[i].ld > (1ll << 40)) return fail(c, HELIOS_EINVAL, "%s: rows are too far apart", m[i].name);
+        if (m[i].ld > kMaxSpan / m[i].bytes / std::max<int64_t>(m[i].rows, 1)) return fail(c, HELIOS_EINVAL, "%s: rows are too far apart", m[i].name);
     }
     for (int i = 0; i < n; ++i)
         for (int j = 0; j < n; ++j) {

@@ -89,3 +89,14 @@ def test_scratch_that_cannot_be_doubled_is_what_the_call_needs(helios, h):
         room.clear()
         torch.cuda.empty_cache()
     assert call(3.0)
+
+
+def test_rows_too_far_apart_are_refused(helios, h):
+    """Where the bytes from the first row to the last are more than 64 bits hold, or than can be addressed: such rows' places cannot be told apart."""
+    p, q = (torch.zeros(64, device="cuda").data_ptr() for _ in range(2))
+    lib = helios._lib
+    for rows, ld in ((1 << 30, 1 << 40), (1 << 30, 1 << 32), (1 << 20, 1 << 38)):
+        assert lib.helios_quantize_rows(h._h, rows, None, 4, helios.F32, p, ld, q, 4, q) == helios.EINVAL
+        assert b"too far apart" in lib.helios_last_error(h._h)
+        assert lib.helios_linear(h._h, helios.LinearArgs(n_rows=rows, n_in=4, n_out=4, x=p, x_ld=4, w=p, w_ld=4, y=q, y_ld=ld)) == helios.EINVAL
+        assert b"too far apart" in lib.helios_last_error(h._h)
