@@ -10,9 +10,9 @@
 // Elements of 16 bits go to the matrix instructions as they are, e4m3 after widening to half precision, single precision in
 // three parts of bfloat16, gradients that 16 bits cannot hold in two.  Sums are held in 32 bits (MFMA accumulators); the epilogue works on 32-bit sums and rounds once.
 //
-// Measured: 100 000 x 2048 x 512 in half precision with bias, ReLU and z kept 258-269 us (0.8 PFLOP/s; matrix units busy 0.4 of the
-// time); 50 003 x 1024 x 1024 in e4m3 with scales, SiLU and residual 137-139 us (0.76 PFLOP/s); the gradient of 26 624 x 512 x 256
-// with GELU in bfloat16 65 us, of 11 264 x 256 x 256 with ReLU in single precision 44 us; one row 256 x 256 4 us of kernel.
+// Measured: 100 000 x 2048 x 512 in half precision with bias, ReLU and z kept 256-267 us (0.8 PFLOP/s; matrix units busy 0.41 of the
+// time); 50 003 x 1024 x 1024 in e4m3 with scales, SiLU and residual 131-138 us (0.78 PFLOP/s; 0.33); the gradient of 26 624 x 512 x 256
+// with GELU in bfloat16 64-66 us (0.23), of 11 264 x 256 x 256 with ReLU in single precision 45 us (0.17); one row 256 x 256 4 us of kernel.
 // What bounds the large ones is the step: a stage's loads, LDS reads and products, with two workgroups to a CU to fill each
 // other's waits; the small ones a launch and one trip to memory.
 #include "layer.hpp"
@@ -743,8 +743,8 @@ __global__ __launch_bounds__(kFewWaves* kWave) void product_few_kernel(ProductAr
 
 // dz = dy * act'(pre) for the products: in 32 bits if they are in single precision, in x's type if that holds it exactly (no activation or ReLU,
 // and dy of x's type), else in two parts of bfloat16; and the sums of dz's columns (from the values before they are
-// cut) over the rows of a workgroup.  Bound by memory: 26 624 x 256 in bfloat16 with GELU 12-14 us, for 41 MB of which most
-// comes from HBM.  (GELU by the library's error function and one row in flight: 19 us.)
+// cut) over the rows of a workgroup.  Bound by memory: 26 624 x 256 in bfloat16 with GELU 18 us, for 54 MB of which most
+// is HBM's.  (GELU by the library's error function and one row in flight: 19 us.)
 constexpr int kSlopeRows = 2;                     // rows that a thread has in flight
 struct SlopeArgs {
     Count rows;
@@ -932,8 +932,8 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
     // Few tiles: 16 x 16 with k shared by eight waves, 3 us + (2 + 0.45 steps) ns a tile, against 3 us + a step's latency (0.33 us with
     // elements of 16 bits, 0.27 with 8, 0.9 with 32) a step, a step being 128 bytes of k.  us, few / small tiles, half precision: 16 x 1024 x 256
     // 4.4 / 8.3, 256 x 1024 x 256 4.7 / 8.8, 777 x 1024 x 256 10.5 / 9.0; single: 777 x 200 x 48 3.4 / 9.5, 1536 x 1024 x 256
-    // 27 / 29, 3000 x 256 x 256 17.5 / 11.2.  Large tiles from where they fill the CUs: 3000 x 2048 x 1024 in half precision small 23.6, large 27.5
-    // (192 large tiles), 6000 48.0 and 36.0 (376).
+    // 27 / 29, 3000 x 256 x 256 17.5 / 11.2.  Large tiles from where they fill the CUs: 3000 x 2048 x 1024 in half precision small 23.8, large 25.5
+    // (192 large tiles), 6000 45.4 and 34.3 (376).
     const int64_t steps = (p.k * type_bytes(TYPE) + kStageBytes - 1) / kStageBytes, latency = TYPE == kF32 ? 900 : TYPE == kE4M3 ? 270 : 330;
     if (static_cast<int64_t>(tiles_of(p.m, 16)) * tiles_of(p.n, 16) * (200 + 45 * steps) <= 100 * latency * steps && tiles_of(p.m, 16) <= 65535) {
         const dim3 grid(tiles_of(p.n, 16), tiles_of(p.m, 16));
@@ -941,8 +941,8 @@ hipError_t forward(hipStream_t stream, const LinearJob& j) {
         return hipGetLastError();
     }
     // Large lists of 16-bit elements: the height of tile that leaves the last round fullest, two tiles to a CU at a time (one of 160 rows takes a
-    // quarter longer than one of 128).  us, 128 / 160 rows: 100 000 x 2048 x 512 324 / 303, 60 000 176 / 163, 30 000 x 2048 x 1024 152 / 138,
-    // but with short k, where the epilogue weighs more, 100 000 x 256 x 512 62.6 / 66.2.
+    // quarter longer than one of 128).  us, 128 / 160 rows (bias and ReLU, z not kept): 100 000 x 2048 x 512 271 / 243, 60 000 159 / 147,
+    // 30 000 x 2048 x 1024 145 / 137, but with short k, where the epilogue weighs more, 100 000 x 256 x 512 52.8 / 56.6.
     if constexpr (TYPE == kF16 || TYPE == kBF16) {
         const auto rounds = [&](int height) { return (static_cast<int64_t>(tiles_of(p.m, height)) * tiles_of(p.n, 128) + 511) / 512 * height; };
         if (steps > 8 && rounds(128) > 256 && rounds(160) < rounds(128)) return launch_forward<TYPE, Tall>(stream, p);
@@ -976,7 +976,8 @@ struct GradPlan {                                 // of linear_grad: what lies w
         // (and scratch of eight times dw in 32 bits), us in bfloat16 by eight / one: 4096 x 4096 x 2048 228 / 77, 4096 x 4096 x 4096 457 / 149,
         // 2048 x 8192 x 8192 1345 / 300, 4096 x 2048 x 2048 (256 tiles) 84 / 67; in single precision 530 / 378, 1030 / 760, 2447 / 1541, 246 / 192.  Large tiles where there are enough of them for the CUs (in single
         // precision, where a tile takes longest, for half of them), us by small / large: 5000 x 256 x 256 in bfloat16 16.4 / 18.9, in
-        // single precision 32.2 / 29.5; 26 624 x 512 x 256 50.1 / 44.9; 50 000 x 2048 x 512 598 / 333.
+        // single precision 32.2 / 29.5; 26 624 x 512 x 256 50.1 / 44.9; 50 000 x 2048 x 512 598 / 333.  The same numbers hold for dz in two parts: with
+        // GELU in bfloat16 5000 x 256 x 256 23.4 / 27.0, 26 624 x 512 x 256 68 / 60 (16 slices 70, 32 60, 64 67), 50 000 x 2048 x 512 714 / 529.
         const auto tiles = [](int64_t m, int64_t n, int64_t edge) { return (m + edge - 1) / edge * ((n + edge - 1) / edge); };
         const int64_t steps = (n * type_bytes(j.x_type) + kStageBytes - 1) / kStageBytes;
         const auto cut = [&](int64_t edge, int64_t most) {

@@ -552,8 +552,9 @@ struct RunMeanGrad {
     }
 };
 
-// By ranges where looking through all places takes less than the sort's eight launches (60 to 70 us).  us by sort / by ranges: 27 000 places
-// 57 / 13, 75 000 57 / 22; every workgroup reads every place, so the time grows with them.
+// By ranges where looking through all places takes less than the sort's eight launches.  us by sort / by ranges: 27 000 places
+// 59 / 11, 65 000 59 / 18, 105 000 60 / 26 (of 4000 sources 57 / 29), 131 000 64 / 31 (of 2000 sources, where a range holds more than its
+// LDS, 36 / 46); every workgroup reads every place, so the time grows with them (282 000 72 / 62).
 constexpr int64_t kRangePlaces = 1 << 17;
 struct TransposePlan {
     int64_t n, ranges;                            // (ranges: 0 by a sort)

@@ -262,8 +262,9 @@ __global__ __launch_bounds__(kBlock) void gain_sum_kernel(const float* part, int
     sum_columns(part, n_parts, width, blockIdx.x * kSumColumns, out, type);
 }
 
-// The lanes and chunks for a row of `width` elements: as few lanes idle as powers of two allow, and up to a wave the sums over a row
-// need no LDS.
+// The lanes and chunks for a row of `width` elements: sixteen lanes or a wave, whose sums need no LDS, while a lane has at most two chunks, then a
+// workgroup.  Widths far below a shape's most leave lanes idle (of 256 elements half the wave, of 1032 half the workgroup), which
+// short rows hide behind the launch and long lists behind memory.
 template <int TYPE, class RUN>
 auto by_width(int32_t width, RUN run) {
     if (width <= 128) return run.template go<TYPE, 16, 1>();
