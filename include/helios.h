@@ -476,8 +476,9 @@ int helios_gather_times(helios_ctx *ctx, float *hbm_ms, float *host_ms,
  * Operators of a model's layer on the rows of a prepared mini-batch
  * (`out` of helios_prepare_batch, blocks of helios_make_blocks): the mean over
  * a block's sampled neighbours, a matrix product with bias, activation and
- * residual, a root-mean-square norm, their gradients, and product and norm in
- * 8 bits for serving.  They need neither a graph nor a cache.
+ * residual, a root-mean-square norm, learnt rows by ID, dropout, the join of a
+ * layer with what went around it, their gradients, and product and norms in 8
+ * bits for serving.  They need neither a graph nor a cache.
  *
  *  - A matrix is a device pointer to its first element and the distance `ld`
  *    from one row to the next in elements; a row's elements are neighbours.
@@ -693,6 +694,180 @@ typedef struct {
     int64_t dx_ld;
 } helios_block_mean_grad_args;
 int helios_block_mean_grad(helios_ctx *ctx, const helios_block_mean_grad_args *args);
+
+/* Learnt rows, looked up by ID: y[i] = add[i] + scale * table[ids[i]] (add nullable).
+ * table [n_table x width] is of table_type; add and y [n_rows x width] of y_type,
+ * which is table_type, or any of the three where the table is HELIOS_F32.  ids
+ * int32[n_rows], device; an ID may appear any number of times.  -1 stands for no
+ * row, zeros; so does any other ID outside [0, n_table), which is reported as
+ * HELIOS_EDATA by the next helios_sync.  y may be add's matrix.  For rows of a
+ * prepared batch: ids = unique, add = out. */
+typedef struct {
+    int64_t n_rows;
+    const int64_t *n_rows_dev;
+    int64_t width, n_table;
+    int32_t table_type, y_type;
+    float scale;
+    int32_t reserved;
+    const void *table;
+    int64_t table_ld;
+    const int32_t *ids;
+    const void *add;
+    int64_t add_ld;
+    void *y;
+    int64_t y_ld;
+} helios_embedding_args;
+int helios_embedding(helios_ctx *ctx, const helios_embedding_args *args);
+
+/* Gradient of helios_embedding: for an ID k, scale times the sum of dy[i] over the
+ * positions i with ids[i] = k, as the gradient of a whole table or of the rows
+ * that the list meets.  Exactly one of
+ *  - dtable [n_table x width]: every row is written, zeros where no position has
+ *    the ID;
+ *  - drow, row_id and n_distinct: row j of drow belongs to row_id[j]; row_id are
+ *    the list's distinct IDs in ascending order, *n_distinct (device-accessible)
+ *    how many.  drow and row_id have room for min(n_rows, n_table) rows; what lies
+ *    behind the last one that is written stays as it was.
+ * dtable and drow are of table_type, dy [n_rows x width] of y_type (types as in
+ * helios_embedding).  Positions with -1 count for nothing, with any other ID
+ * outside [0, n_table) neither, and are reported.  The sums are taken in the order
+ * of the sorted list, which keeps the positions of an ID in theirs.  add's
+ * gradient is dy itself.  Needs scratch: 16 bytes for a row of dy, and 8 (width + 1)
+ * for every 16 of them, at most 8192 times that, and 1 MB. */
+typedef struct {
+    int64_t n_rows;
+    const int64_t *n_rows_dev;
+    int64_t width, n_table;
+    int32_t table_type, y_type;
+    float scale;
+    int32_t reserved;
+    const int32_t *ids;
+    const void *dy;
+    int64_t dy_ld;
+    void *dtable;
+    int64_t dtable_ld;
+    void *drow;
+    int64_t drow_ld;
+    int32_t *row_id;
+    int64_t *n_distinct;
+} helios_embedding_grad_args;
+int helios_embedding_grad(helios_ctx *ctx, const helios_embedding_grad_args *args);
+
+/* Which elements of a matrix are dropped.  p is taken to the nearest multiple of
+ * 2^-16, t / 65536.  Element (i, j) has 16 bits of its own, half j % 2 (0: the low
+ * one) of word j % 8 / 2 of Philox4x32-10 with the counter (i, j / 8, site,
+ * 0x44524f50) and the key (low, high word of the seed); it is dropped where they
+ * are less than t.  No mask is stored: the same numbers give the same elements
+ * wherever the matrix lies, however it is strided, and for its gradient.  What is
+ * kept is multiplied by 65536 / (65536 - t).  seed_dev (device-accessible) is read
+ * on the device in place of seed if it is not NULL, so that a replayed HIP graph
+ * drops other elements every time; site tells the places of a model apart. */
+typedef struct {
+    double p;                /* 0 (nothing is dropped) to 1 (everything)            */
+    uint64_t seed;
+    const uint64_t *seed_dev;
+    uint32_t site, reserved;
+} helios_drop;
+
+/* y = x where elements are kept, times 65536 / (65536 - t), and 0 where they are
+ * dropped, whatever x holds there.  The gradient is the same call on y's.  x and y
+ * are of x_type; y may be x's matrix. */
+typedef struct {
+    int64_t n_rows;
+    const int64_t *n_rows_dev;
+    int64_t width;
+    int32_t x_type, reserved;
+    helios_drop drop;
+    const void *x;
+    int64_t x_ld;
+    void *y;
+    int64_t y_ld;
+} helios_dropout_args;
+int helios_dropout(helios_ctx *ctx, const helios_dropout_args *args);
+
+/* A layer's output joined with the rows that went around the layer, and the norm in
+ * front of the next one, row by row (rows of 1 to HELIOS_NORM_MAX_WIDTH elements):
+ *     u     = x * gain_x / sqrt(mean(x^2) + eps)       (norm_x 0: u = x)
+ *     total = residual_scale * residual + gate * drop(u)
+ *     y     = total * gain / sqrt(mean(total^2) + eps)
+ * x, residual, total [n_rows x width], gain_x, gain [width] and gate are of x_type;
+ * gate [n_rows x width], or with gate_ld 0 one row for all.  y is of y_type =
+ * x_type, or HELIOS_E4M3 with y_scale [n_rows] as in helios_rms_norm.  gain_x and
+ * gain (ones), gate (ones), residual (zeros), inv_rms_x and inv_rms (float
+ * [n_rows]: 1 / sqrt(mean + eps), for the gradient) are nullable, and one of
+ * total and y is.  Everything is made from unrounded values.  total and y (if of
+ * x_type) may each be the matrix of x or of residual, but not both the same. */
+typedef struct {
+    int64_t n_rows;
+    const int64_t *n_rows_dev;
+    int64_t width;
+    int32_t x_type, y_type, norm_x, reserved;
+    float eps, residual_scale;
+    helios_drop drop;
+    const void *x;
+    int64_t x_ld;
+    const void *gain_x;
+    const void *gate;
+    int64_t gate_ld;
+    const void *residual;
+    int64_t residual_ld;
+    const void *gain;
+    void *total;
+    int64_t total_ld;
+    void *y;
+    int64_t y_ld;
+    float *y_scale;
+    float *inv_rms_x;
+    float *inv_rms;
+} helios_join_norm_args;
+int helios_join_norm(helios_ctx *ctx, const helios_join_norm_args *args);
+
+/* Gradients of helios_join_norm.  With q = 1 / sqrt(mean(total^2) + eps), qx = 1 /
+ * sqrt(mean(x^2) + eps), a = dy * gain and drop() that of the forward call:
+ *     dt        = dtotal + q (a - total q^2 mean(a total))
+ *     dresidual = residual_scale * dt
+ *     dgate     = drop(dt) * x qx gain_x          (gate_ld 0: summed over the rows)
+ *     w         = drop(dt) * gate
+ *     dx        = qx (w gain_x - x qx^2 mean(w gain_x x))        (norm_x 0: dx = w)
+ *     dgain_x   = the sum over the rows of w x qx,  dgain = that of dy total q
+ * dy is the gradient of y (NULL: y was not used; total, gain and dgain are not
+ * either), dtotal that which reaches total by other ways; one of them is nullable.
+ * dgate [n_rows x width], or with gate_ld 0 [width] (dgate_ld is not read).  gain_x,
+ * gate, gain, dresidual, dgate, dgain_x, dgain, inv_rms_x and inv_rms (as
+ * helios_join_norm left them; else they are computed) are nullable.  All of
+ * x_type but the last two.  dx may be the matrix of x, dy, total or dtotal,
+ * dresidual that of dy, total or dtotal, but not both the same. */
+typedef struct {
+    int64_t n_rows;
+    const int64_t *n_rows_dev;
+    int64_t width;
+    int32_t x_type, norm_x;
+    float eps, residual_scale;
+    helios_drop drop;
+    const void *x;
+    int64_t x_ld;
+    const void *gain_x;
+    const void *gate;
+    int64_t gate_ld;
+    const void *gain;
+    const void *total;
+    int64_t total_ld;
+    const void *dy;
+    int64_t dy_ld;
+    const void *dtotal;
+    int64_t dtotal_ld;
+    const float *inv_rms_x;
+    const float *inv_rms;
+    void *dx;
+    int64_t dx_ld;
+    void *dresidual;
+    int64_t dresidual_ld;
+    void *dgate;
+    int64_t dgate_ld;
+    void *dgain_x;
+    void *dgain;
+} helios_join_norm_grad_args;
+int helios_join_norm_grad(helios_ctx *ctx, const helios_join_norm_grad_args *args);
 
 #ifdef __cplusplus
 }

@@ -1,4 +1,5 @@
-// Launchers of the operators of a model's layer on a prepared mini-batch (linear.hip, norm.hip, neighbours.hip).
+// Launchers of the operators of a model's layer on a prepared mini-batch (linear.hip, norm.hip, neighbours.hip,
+// embedding.hip, join.hip).
 // Every launcher enqueues on `stream` and returns the hipError_t of the launch.
 #pragma once
 #include "common.hpp"
@@ -137,5 +138,116 @@ struct MeanGradJob {
 // counters: uint32[kLayerCounters], zero, and left so
 size_t block_mean_grad_scratch_bytes(const MeanGradJob& job);
 hipError_t launch_block_mean_grad(hipStream_t stream, const MeanGradJob& job, uint32_t* counters, void* scratch);
+
+// ---- embedding.hip
+struct EmbeddingJob {
+    Count rows;
+    int32_t width;
+    int table_type, y_type;
+    float scale;
+    int64_t n_table;
+    const void* table;
+    int64_t table_ld;
+    const int32_t* ids;
+    const void* add;                              // nullable
+    int64_t add_ld;
+    void* y;
+    int64_t y_ld;
+    int32_t* err;
+};
+hipError_t launch_embedding(hipStream_t stream, const EmbeddingJob& job);
+
+struct EmbeddingGradJob {
+    Count rows;
+    int32_t width;
+    int table_type, y_type;
+    float scale;
+    int64_t n_table;
+    const int32_t* ids;
+    const void* dy;
+    int64_t dy_ld;
+    void* out;                                    // dtable, or drow where n_distinct is not null
+    int64_t out_ld;
+    int32_t* row_id;
+    int64_t* n_distinct;
+    int32_t* err;
+};
+size_t embedding_grad_scratch_bytes(const EmbeddingGradJob& job);
+hipError_t launch_embedding_grad(hipStream_t stream, const EmbeddingGradJob& job, void* scratch);
+
+// ---- join.hip
+struct Drop {
+    uint64_t seed;
+    const uint64_t* seed_dev;                     // nullable: read in place of seed
+    uint32_t site;
+    uint32_t threshold;                           // elements whose 16 bits are less are dropped; 0: none are
+    float scale;                                  // of what is kept
+};
+struct DropoutJob {
+    Count rows;
+    int32_t width;
+    int type;
+    Drop drop;
+    const void* x;
+    int64_t x_ld;
+    void* y;
+    int64_t y_ld;
+};
+hipError_t launch_dropout(hipStream_t stream, const DropoutJob& job);
+
+struct JoinJob {
+    Count rows;
+    int32_t width;
+    int x_type;
+    bool norm_x;
+    float eps, residual_scale;
+    Drop drop;
+    const void* x;
+    int64_t x_ld;
+    const void* gain_x;
+    const void* gate;
+    int64_t gate_ld;                              // 0: one row for all
+    const void* residual;
+    int64_t residual_ld;
+    const void* gain;
+    void* total;
+    int64_t total_ld;
+    void* y;
+    int64_t y_ld;
+    float* y_scale;                               // not null: y is of kE4M3
+    float *inv_rms_x, *inv_rms;
+};
+hipError_t launch_join(hipStream_t stream, const JoinJob& job);
+
+struct JoinGradJob {
+    Count rows;
+    int32_t width;
+    int type;
+    bool norm_x;
+    float eps, residual_scale;
+    Drop drop;
+    const void* x;
+    int64_t x_ld;
+    const void* gain_x;
+    const void* gate;
+    int64_t gate_ld;
+    const void* gain;
+    const void* total;
+    int64_t total_ld;
+    const void* dy;
+    int64_t dy_ld;
+    const void* dtotal;
+    int64_t dtotal_ld;
+    const float *inv_rms_x, *inv_rms;
+    void* dx;
+    int64_t dx_ld;
+    void* dresidual;
+    int64_t dresidual_ld;
+    void* dgate;
+    int64_t dgate_ld;
+    void *dgain_x, *dgain;
+};
+size_t join_grad_scratch_bytes(const JoinGradJob& job);
+hipError_t launch_join_grad(hipStream_t stream, const JoinGradJob& job, void* scratch);
 
 }  // namespace helios

@@ -66,6 +66,20 @@ int check_width(helios_ctx* c, const char* call, const char* what, int64_t width
 }
 constexpr int64_t kMaxWidth = 1 << 24;            // of a product's rows
 
+// A table of learnt rows, and the types of its rows and of what is looked up.
+int check_table(helios_ctx* c, const char* call, int64_t n_table, int table_type, int y_type) {
+    if (n_table < 0 || n_table >= kMaxCount) return fail(c, HELIOS_EINVAL, "%s: n_table must be 0 to 2^31 - 1025 (got %lld)", call, (long long)n_table);
+    if (!is_float(table_type)) return fail(c, HELIOS_EINVAL, "%s: unknown table_type %d", call, table_type);
+    if (!is_float(y_type) || (y_type != table_type && table_type != HELIOS_F32)) return fail(c, HELIOS_EINVAL, "%s: y_type %d does not go with table_type %d", call, y_type, table_type);
+    return HELIOS_OK;
+}
+int check_drop(helios_ctx* c, const char* call, const helios_drop& d, Drop* out) {
+    if (!(d.p >= 0.0 && d.p <= 1.0)) return fail(c, HELIOS_EINVAL, "%s: the share of dropped elements must be 0 to 1", call);
+    const uint32_t t = static_cast<uint32_t>(d.p * 65536.0 + 0.5);
+    *out = Drop{d.seed, d.seed_dev, d.site, t, t < 65536 ? static_cast<float>(65536.0 / (65536.0 - t)) : 0.0f};
+    return HELIOS_OK;
+}
+
 // Scratch of at least `bytes` bytes (*at), behind a line of counters that are zero between calls.
 constexpr size_t kCounterBytes = sizeof(uint32_t) * kLayerCounters;
 int scratch(helios_ctx* c, size_t bytes, char** at) {
@@ -326,6 +340,160 @@ int helios_block_mean_grad(helios_ctx* c, const helios_block_mean_grad_args* a) 
     char* at = nullptr;
     TRY(scratch(c, block_mean_grad_scratch_bytes(job), &at));
     HIP_TRY(c, launch_block_mean_grad(c->stream, job, reinterpret_cast<uint32_t*>(at - kCounterBytes), at));
+    return HELIOS_OK;
+}
+
+int helios_embedding(helios_ctx* c, const helios_embedding_args* a) {
+    if (!c) return HELIOS_EINVAL;
+    if (!a) return fail(c, HELIOS_EINVAL, "helios_embedding: NULL arguments");
+    TRY(check_counts(c, "helios_embedding", a->n_rows, a->n_rows_dev));
+    TRY(check_width(c, "helios_embedding", "width", a->width, kMaxWidth));
+    TRY(check_table(c, "helios_embedding", a->n_table, a->table_type, a->y_type));
+    if (a->n_rows == 0) return HELIOS_OK;
+    if (!a->ids || !a->y || (a->n_table > 0 && !a->table)) return fail(c, HELIOS_EINVAL, "helios_embedding: NULL pointer");
+    const int tb = bytes_of(a->table_type), yb = bytes_of(a->y_type);
+    const Matrix m[] = {{"table", a->table, a->n_table, a->width, a->table_ld, tb, false},
+                        {"ids", a->ids, 1, a->n_rows, a->n_rows, 4, false},
+                        {"add", a->add, a->n_rows, a->width, a->add_ld, yb, false},
+                        {"y", a->y, a->n_rows, a->width, a->y_ld, yb, true}};
+    const uint32_t twins[4] = {0, 0, 0, 1u << 2};
+    TRY(check(c, m, 4, twins));
+    DeviceGuard guard(c->device);
+    const EmbeddingJob job{Count{a->n_rows_dev, a->n_rows}, static_cast<int32_t>(a->width), a->table_type, a->y_type, a->scale, a->n_table, a->table,
+                           a->table_ld, a->ids, a->add, a->add_ld, a->y, a->y_ld, c->err};
+    HIP_TRY(c, launch_embedding(c->stream, job));
+    return HELIOS_OK;
+}
+
+int helios_embedding_grad(helios_ctx* c, const helios_embedding_grad_args* a) {
+    if (!c) return HELIOS_EINVAL;
+    if (!a) return fail(c, HELIOS_EINVAL, "helios_embedding_grad: NULL arguments");
+    TRY(check_counts(c, "helios_embedding_grad", a->n_rows, a->n_rows_dev));
+    TRY(check_width(c, "helios_embedding_grad", "width", a->width, kMaxWidth));
+    TRY(check_table(c, "helios_embedding_grad", a->n_table, a->table_type, a->y_type));
+    const bool by_row = !a->dtable && (a->n_table > 0 || a->n_distinct);              // (a table without rows may lie anywhere)
+    const int64_t n_out = by_row ? std::min(a->n_rows, a->n_table) : a->n_table;
+    if (!by_row && (a->drow || a->row_id || a->n_distinct))
+        return fail(c, HELIOS_EINVAL, "helios_embedding_grad: dtable, or drow with row_id and n_distinct, but not both");
+    if ((by_row && (!a->n_distinct || (n_out > 0 && (!a->drow || !a->row_id)))) || (a->n_rows > 0 && (!a->ids || !a->dy)))
+        return fail(c, HELIOS_EINVAL, "helios_embedding_grad: NULL pointer");
+    const int tb = bytes_of(a->table_type), yb = bytes_of(a->y_type);
+    const Matrix m[] = {{"ids", a->ids, 1, a->n_rows, a->n_rows, 4, false},
+                        {"dy", a->dy, a->n_rows, a->width, a->dy_ld, yb, false},
+                        {"dtable", a->dtable, n_out, a->width, a->dtable_ld, tb, true},
+                        {"drow", a->drow, n_out, a->width, a->drow_ld, tb, true},
+                        {"row_id", a->row_id, 1, n_out, n_out, 4, true},
+                        {"n_distinct", a->n_distinct, 1, 1, 1, 8, true}};
+    const uint32_t twins[6] = {0};
+    TRY(check(c, m, 6, twins));
+    if (!by_row && n_out == 0) return HELIOS_OK;
+    DeviceGuard guard(c->device);
+    const EmbeddingGradJob job{Count{a->n_rows_dev, a->n_rows}, static_cast<int32_t>(a->width), a->table_type, a->y_type, a->scale, a->n_table, a->ids, a->dy,
+                               a->dy_ld, by_row ? a->drow : a->dtable, by_row ? a->drow_ld : a->dtable_ld, a->row_id, a->n_distinct, c->err};
+    char* at = nullptr;
+    TRY(scratch(c, embedding_grad_scratch_bytes(job), &at));
+    HIP_TRY(c, launch_embedding_grad(c->stream, job, at));
+    return HELIOS_OK;
+}
+
+int helios_dropout(helios_ctx* c, const helios_dropout_args* a) {
+    if (!c) return HELIOS_EINVAL;
+    if (!a) return fail(c, HELIOS_EINVAL, "helios_dropout: NULL arguments");
+    TRY(check_counts(c, "helios_dropout", a->n_rows, a->n_rows_dev));
+    TRY(check_width(c, "helios_dropout", "width", a->width, kMaxWidth));
+    if (!is_float(a->x_type)) return fail(c, HELIOS_EINVAL, "helios_dropout: unknown x_type %d", a->x_type);
+    Drop drop;
+    TRY(check_drop(c, "helios_dropout", a->drop, &drop));
+    if (a->n_rows == 0) return HELIOS_OK;
+    if (!a->x || !a->y) return fail(c, HELIOS_EINVAL, "helios_dropout: NULL pointer");
+    const int xb = bytes_of(a->x_type);
+    const Matrix m[] = {{"x", a->x, a->n_rows, a->width, a->x_ld, xb, false},
+                        {"y", a->y, a->n_rows, a->width, a->y_ld, xb, true},
+                        {"seed_dev", a->drop.seed_dev, 1, 1, 1, 8, false}};
+    const uint32_t twins[3] = {0, 1u << 0, 0};
+    TRY(check(c, m, 3, twins));
+    DeviceGuard guard(c->device);
+    HIP_TRY(c, launch_dropout(c->stream, DropoutJob{Count{a->n_rows_dev, a->n_rows}, static_cast<int32_t>(a->width), a->x_type, drop, a->x, a->x_ld, a->y, a->y_ld}));
+    return HELIOS_OK;
+}
+
+int helios_join_norm(helios_ctx* c, const helios_join_norm_args* a) {
+    if (!c) return HELIOS_EINVAL;
+    if (!a) return fail(c, HELIOS_EINVAL, "helios_join_norm: NULL arguments");
+    TRY(check_counts(c, "helios_join_norm", a->n_rows, a->n_rows_dev));
+    TRY(check_width(c, "helios_join_norm", "width", a->width, HELIOS_NORM_MAX_WIDTH));
+    if (!is_float(a->x_type)) return fail(c, HELIOS_EINVAL, "helios_join_norm: unknown x_type %d", a->x_type);
+    const bool to_8_bits = a->y && a->y_type == HELIOS_E4M3;
+    if (a->y && !to_8_bits && a->y_type != a->x_type) return fail(c, HELIOS_EINVAL, "helios_join_norm: y_type %d does not go with x_type %d", a->y_type, a->x_type);
+    if (!(a->eps >= 0.0f)) return fail(c, HELIOS_EINVAL, "helios_join_norm: eps must not be negative");
+    Drop drop;
+    TRY(check_drop(c, "helios_join_norm", a->drop, &drop));
+    if (!a->norm_x && (a->gain_x || a->inv_rms_x)) return fail(c, HELIOS_EINVAL, "helios_join_norm: gain_x and inv_rms_x go with a norm of x (norm_x)");
+    if (a->n_rows == 0) return HELIOS_OK;
+    if (!a->x || (!a->total && !a->y)) return fail(c, HELIOS_EINVAL, "helios_join_norm: NULL pointer");
+    if (!a->y && (a->gain || a->inv_rms)) return fail(c, HELIOS_EINVAL, "helios_join_norm: gain and inv_rms go with y");
+    if ((a->y_scale != nullptr) != to_8_bits) return fail(c, HELIOS_EINVAL, "helios_join_norm: y_scale goes with an output in 8 bits, and only with it");
+    const int xb = bytes_of(a->x_type), yb = bytes_of(a->y ? a->y_type : a->x_type);
+    const Matrix m[] = {{"x", a->x, a->n_rows, a->width, a->x_ld, xb, false},
+                        {"residual", a->residual, a->n_rows, a->width, a->residual_ld, xb, false},
+                        {"total", a->total, a->n_rows, a->width, a->total_ld, xb, true},
+                        {"y", a->y, a->n_rows, a->width, a->y_ld, yb, true},
+                        {"gain_x", a->gain_x, 1, a->width, a->width, xb, false},
+                        {"gate", a->gate, a->gate_ld ? a->n_rows : 1, a->width, a->gate_ld ? a->gate_ld : a->width, xb, false},
+                        {"gain", a->gain, 1, a->width, a->width, xb, false},
+                        {"y_scale", a->y_scale, 1, a->n_rows, a->n_rows, 4, true},
+                        {"inv_rms_x", a->inv_rms_x, 1, a->n_rows, a->n_rows, 4, true},
+                        {"inv_rms", a->inv_rms, 1, a->n_rows, a->n_rows, 4, true},
+                        {"seed_dev", a->drop.seed_dev, 1, 1, 1, 8, false}};
+    const uint32_t twins[11] = {0, 0, 3, 3, 0, 0, 0, 0, 0, 0, 0};
+    TRY(check(c, m, 11, twins));
+    DeviceGuard guard(c->device);
+    const JoinJob job{Count{a->n_rows_dev, a->n_rows}, static_cast<int32_t>(a->width), a->x_type, a->norm_x != 0, a->eps, a->residual_scale, drop, a->x, a->x_ld,
+                      a->gain_x, a->gate, a->gate_ld, a->residual, a->residual_ld, a->gain, a->total, a->total_ld, a->y, a->y_ld, a->y_scale, a->inv_rms_x, a->inv_rms};
+    HIP_TRY(c, launch_join(c->stream, job));
+    return HELIOS_OK;
+}
+
+int helios_join_norm_grad(helios_ctx* c, const helios_join_norm_grad_args* a) {
+    if (!c) return HELIOS_EINVAL;
+    if (!a) return fail(c, HELIOS_EINVAL, "helios_join_norm_grad: NULL arguments");
+    TRY(check_counts(c, "helios_join_norm_grad", a->n_rows, a->n_rows_dev));
+    TRY(check_width(c, "helios_join_norm_grad", "width", a->width, HELIOS_NORM_MAX_WIDTH));
+    if (!is_float(a->x_type)) return fail(c, HELIOS_EINVAL, "helios_join_norm_grad: unknown x_type %d", a->x_type);
+    if (!(a->eps >= 0.0f)) return fail(c, HELIOS_EINVAL, "helios_join_norm_grad: eps must not be negative");
+    Drop drop;
+    TRY(check_drop(c, "helios_join_norm_grad", a->drop, &drop));
+    if (!a->norm_x && (a->gain_x || a->inv_rms_x || a->dgain_x)) return fail(c, HELIOS_EINVAL, "helios_join_norm_grad: gain_x, inv_rms_x and dgain_x go with a norm of x (norm_x)");
+    if (a->n_rows > 0 && (!a->x || !a->dx || (!a->dy && !a->dtotal) || (a->dy && !a->total))) return fail(c, HELIOS_EINVAL, "helios_join_norm_grad: NULL pointer");
+    if (a->n_rows > 0 && !a->dy && (a->gain || a->inv_rms || a->dgain)) return fail(c, HELIOS_EINVAL, "helios_join_norm_grad: gain, inv_rms and dgain go with dy");
+    if (a->dgate && !a->gate && a->n_rows > 0) return fail(c, HELIOS_EINVAL, "helios_join_norm_grad: dgate goes with a gate");
+    const bool one_gate = a->gate_ld == 0;
+    if (a->n_rows == 0 && !a->dgain && !a->dgain_x && !(a->dgate && one_gate)) return HELIOS_OK;
+    const int xb = bytes_of(a->x_type);
+    const Matrix m[] = {{"x", a->x, a->n_rows, a->width, a->x_ld, xb, false},
+                        {"dy", a->dy, a->n_rows, a->width, a->dy_ld, xb, false},
+                        {"total", a->dy ? a->total : nullptr, a->n_rows, a->width, a->total_ld, xb, false},
+                        {"dtotal", a->dtotal, a->n_rows, a->width, a->dtotal_ld, xb, false},
+                        {"dx", a->dx, a->n_rows, a->width, a->dx_ld, xb, true},
+                        {"dresidual", a->dresidual, a->n_rows, a->width, a->dresidual_ld, xb, true},
+                        {"dgate", a->dgate, one_gate ? 1 : a->n_rows, a->width, one_gate ? a->width : a->dgate_ld, xb, true},
+                        {"dgain_x", a->dgain_x, 1, a->width, a->width, xb, true},
+                        {"dgain", a->dgain, 1, a->width, a->width, xb, true},
+                        {"gain_x", a->gain_x, 1, a->width, a->width, xb, false},
+                        {"gate", a->gate, one_gate ? 1 : a->n_rows, a->width, one_gate ? a->width : a->gate_ld, xb, false},
+                        {"gain", a->gain, 1, a->width, a->width, xb, false},
+                        {"inv_rms_x", a->inv_rms_x, 1, a->n_rows, a->n_rows, 4, false},
+                        {"inv_rms", a->inv_rms, 1, a->n_rows, a->n_rows, 4, false},
+                        {"seed_dev", a->drop.seed_dev, 1, 1, 1, 8, false}};
+    const uint32_t twins[15] = {0, 0, 0, 0, 15u, 14u, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    TRY(check(c, m, 15, twins));
+    DeviceGuard guard(c->device);
+    const JoinGradJob job{Count{a->n_rows_dev, a->n_rows}, static_cast<int32_t>(a->width), a->x_type, a->norm_x != 0, a->eps, a->residual_scale, drop, a->x, a->x_ld,
+                          a->gain_x, a->gate, a->gate_ld, a->gain, a->total, a->total_ld, a->dy, a->dy_ld, a->dtotal, a->dtotal_ld, a->inv_rms_x, a->inv_rms, a->dx,
+                          a->dx_ld, a->dresidual, a->dresidual_ld, a->dgate, a->dgate_ld, a->dgain_x, a->dgain};
+    char* at = nullptr;
+    TRY(scratch(c, join_grad_scratch_bytes(job), &at));
+    HIP_TRY(c, launch_join_grad(c->stream, job, at));
     return HELIOS_OK;
 }
 

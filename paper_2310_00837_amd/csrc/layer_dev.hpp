@@ -246,6 +246,115 @@ __device__ __forceinline__ float group_max(float v) {
     return group_reduce<G>(v, [](float a, float b) { return a > b || a != a ? a : b; });
 }
 
+// Where the items of a workgroup are, from number `base` on: an item is eight neighbouring columns of a row, items are numbered along the rows
+// (of `blocks` items each, fewer than 2^22).
+struct ItemPlaces {
+    int64_t row0;
+    uint32_t rem0, blocks;
+    __device__ __forceinline__ ItemPlaces(int64_t base, uint32_t row_blocks) : row0(base / row_blocks), rem0(static_cast<uint32_t>(base % row_blocks)), blocks(row_blocks) {}
+    __device__ __forceinline__ void get(uint32_t i, int64_t* row, int32_t* col) const {
+        const uint32_t at = rem0 + i, down = at / blocks;
+        *row = row0 + down;
+        *col = static_cast<int32_t>(at - down * blocks) * 8;
+    }
+};
+
+// Lanes that share a row: LANES (a power of two), each with CHUNKS times eight elements; up to a wave several rows to a workgroup, else
+// the workgroup has one.
+template <int LANES>
+struct RowShape {
+    static constexpr int kThreads = LANES > kBlock ? LANES : kBlock;
+    static constexpr int kRows = kThreads / LANES;
+};
+template <int LANES>
+__device__ __forceinline__ float row_sum(float v, float* s) {
+    v = group_sum<(LANES < kWave ? LANES : kWave)>(v);
+    if (LANES > kWave) {
+        constexpr int kWaves = LANES / kWave;
+        __syncthreads();
+        if (lane_id() == 0) s[wave_id()] = v;
+        __syncthreads();
+        v = 0;
+        const int first = wave_id() / kWaves * kWaves;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += s[first + w];
+    }
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ float row_max(float v, float* s) {
+    v = group_max<(LANES < kWave ? LANES : kWave)>(v);
+    if (LANES > kWave) {
+        constexpr int kWaves = LANES / kWave;
+        __syncthreads();
+        if (lane_id() == 0) s[wave_id()] = v;
+        __syncthreads();
+        const int first = wave_id() / kWaves * kWaves;
+        v = s[first];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+            const float o = s[first + w];
+            v = o > v || o != o ? o : v;
+        }
+    }
+    return v;
+}
+
+__device__ __forceinline__ void store_8_of_e4m3(void* base, int64_t at, int valid, const float (&v)[8]) {
+    typedef int32_t i32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+    int32_t w[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        w[k] = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * k], v[4 * k + 1], 0, false);
+        w[k] = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * k + 2], v[4 * k + 3], w[k], true);
+    }
+    uint8_t* p = static_cast<uint8_t*>(base) + at;
+    if (valid >= 8) {
+        *reinterpret_cast<i32x2_any*>(p) = i32x2_any{w[0], w[1]};
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < valid) p[e] = static_cast<uint8_t>(static_cast<uint32_t>(w[e / 4]) >> (8 * (e % 4)));
+}
+
+// A row's finished values to memory at element `at` of y: rounded to TYPE, or (to_scale) to 8 bits with the row's scale.
+constexpr float kE4M3Max = 448.0f, kMinScale = 0x1p-126f;
+template <int TYPE, int LANES, int CHUNKS>
+__device__ __forceinline__ void finish_row(float (&t)[CHUNKS][8], int32_t width, int lane, float* s, void* y, int64_t at, float* to_scale) {
+    if (!to_scale) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int col = (c * LANES + lane) * 8;
+            store_8_of<TYPE>(y, at + col, width - col, t[c]);
+        }
+        return;
+    }
+    float most = 0;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float a = fabsf(t[c][e]);
+            most = a > most || a != a ? a : most;
+        }
+    most = row_max<LANES>(most, s) / kE4M3Max;
+    // (y / scale, correctly rounded, by way of the reciprocal and one step of Newton's: by the reciprocal alone a quotient can fall to the wrong
+    // side of the middle between two values of 8 bits.  An infinite scale leaves 0 of what is finite.)
+    const float scale = most < kMinScale ? kMinScale : most, inv = 1.0f / scale;
+    if (lane == 0) *to_scale = scale;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        const int col = (c * LANES + lane) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float near = t[c][e] * inv;     // t / scale, but for its last bit
+            t[c][e] = inv > 0.0f ? __builtin_fmaf(__builtin_fmaf(-near, scale, t[c][e]), inv, near) : near;
+        }
+        store_8_of_e4m3(y, at + col, width - col, t[c]);
+    }
+}
+
 // out[c] = the sum over p of part[p][c], p < n_parts, for the 16 columns from `first` on, by a workgroup of kBlock threads.  Four of
 // them share a part's columns and 64 go through the parts, so that few loads follow on one another; the order of the additions
 // is the same in every call.

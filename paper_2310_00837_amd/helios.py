@@ -38,7 +38,8 @@ EXPORTS = ["helios_create", "helios_destroy", "helios_last_error", "helios_reser
            "helios_gather_times", "helios_batch_ticks", "helios_missq_create", "helios_missq_submit", "helios_missq_complete",
            "helios_missq_attach", "helios_missq_faulted", "helios_missq_counters", "helios_missq_destroy",
            "helios_linear", "helios_linear_grad", "helios_rms_norm", "helios_rms_norm_grad", "helios_quantize_rows", "helios_block_mean",
-           "helios_block_transpose", "helios_block_mean_grad"]
+           "helios_block_transpose", "helios_block_mean_grad", "helios_embedding", "helios_embedding_grad", "helios_dropout", "helios_join_norm",
+           "helios_join_norm_grad"]
 
 
 class HopOut(C.Structure):
@@ -60,8 +61,8 @@ MAX_GANG = 4
 
 
 def _args_struct(name: str, fields: str):
-    """A ctypes structure from "name:type" words (p pointer, l int64, i int32, f float), in the order of the header."""
-    kinds = {"p": C.c_void_p, "l": C.c_int64, "i": C.c_int32, "f": C.c_float}
+    """A ctypes structure from "name:type" words (p pointer, l int64, i int32, f float, u uint64, w uint32, d double), in the order of the header."""
+    kinds = {"p": C.c_void_p, "l": C.c_int64, "i": C.c_int32, "f": C.c_float, "u": C.c_uint64, "w": C.c_uint32, "d": C.c_double}
     return type(name, (C.Structure,), {"_fields_": [(w[:-2], kinds[w[-1]]) for w in fields.split()]})
 
 
@@ -77,6 +78,18 @@ BlockMeanArgs = _args_struct("BlockMeanArgs", "n_rows:l n_rows_dev:p width:l n_s
                              "mean_ld:l own:p own_ld:l")
 BlockMeanGradArgs = _args_struct("BlockMeanGradArgs", "n_rows:l width:l n_src:l n_entries:l x_type:i reserved:i indptr:p src_indptr:p src_entry:p dmean:p "
                                  "dmean_ld:l down:p down_ld:l dx:p dx_ld:l")
+
+EmbeddingArgs = _args_struct("EmbeddingArgs", "n_rows:l n_rows_dev:p width:l n_table:l table_type:i y_type:i scale:f reserved:i table:p table_ld:l ids:p "
+                             "add:p add_ld:l y:p y_ld:l")
+EmbeddingGradArgs = _args_struct("EmbeddingGradArgs", "n_rows:l n_rows_dev:p width:l n_table:l table_type:i y_type:i scale:f reserved:i ids:p dy:p dy_ld:l "
+                                 "dtable:p dtable_ld:l drow:p drow_ld:l row_id:p n_distinct:p")
+_DROP = "p:d seed:u seed_dev:p site:w drop_reserved:w "          # helios_drop, field by field
+DropoutArgs = _args_struct("DropoutArgs", "n_rows:l n_rows_dev:p width:l x_type:i reserved:i " + _DROP + "x:p x_ld:l y:p y_ld:l")
+JoinNormArgs = _args_struct("JoinNormArgs", "n_rows:l n_rows_dev:p width:l x_type:i y_type:i norm_x:i reserved:i eps:f residual_scale:f " + _DROP +
+                            "x:p x_ld:l gain_x:p gate:p gate_ld:l residual:p residual_ld:l gain:p total:p total_ld:l y:p y_ld:l y_scale:p inv_rms_x:p inv_rms:p")
+JoinNormGradArgs = _args_struct("JoinNormGradArgs", "n_rows:l n_rows_dev:p width:l x_type:i norm_x:i eps:f residual_scale:f " + _DROP + "x:p x_ld:l gain_x:p "
+                                "gate:p gate_ld:l gain:p total:p total_ld:l dy:p dy_ld:l dtotal:p dtotal_ld:l inv_rms_x:p inv_rms:p dx:p dx_ld:l "
+                                "dresidual:p dresidual_ld:l dgate:p dgate_ld:l dgain_x:p dgain:p")
 
 
 class RoleTicks(C.Structure):
@@ -153,6 +166,11 @@ def load_library() -> C.CDLL:
     lib.helios_block_mean.argtypes = [vp, C.POINTER(BlockMeanArgs)]
     lib.helios_block_transpose.argtypes = [vp, i64, vp, vp, vp, i64, vp, i64, vp, vp]
     lib.helios_block_mean_grad.argtypes = [vp, C.POINTER(BlockMeanGradArgs)]
+    lib.helios_embedding.argtypes = [vp, C.POINTER(EmbeddingArgs)]
+    lib.helios_embedding_grad.argtypes = [vp, C.POINTER(EmbeddingGradArgs)]
+    lib.helios_dropout.argtypes = [vp, C.POINTER(DropoutArgs)]
+    lib.helios_join_norm.argtypes = [vp, C.POINTER(JoinNormArgs)]
+    lib.helios_join_norm_grad.argtypes = [vp, C.POINTER(JoinNormGradArgs)]
     return lib
 
 
@@ -221,6 +239,22 @@ def _type(t: torch.Tensor, what: str) -> int:
 
 def _count(t: Optional[torch.Tensor], what: str) -> Optional[int]:
     return None if t is None else _dev_accessible(t, torch.int64, what).data_ptr()
+
+
+def _drop(p: float, seed, site: int):
+    """The fields of helios_drop; seed: a number, or an int64 tensor that is read on the device."""
+    if isinstance(seed, torch.Tensor):
+        if seed.numel() != 1:
+            raise TypeError("seed: expected one number")
+        return p, 0, _dev_accessible(seed, torch.int64, "seed").data_ptr(), site, 0
+    return p, seed, None, site, 0
+
+
+def _gate(t: Optional[torch.Tensor], shape, dtype: torch.dtype, what: str):
+    """A matrix, or one row for all (a vector)."""
+    if t is not None and t.dim() == 1:
+        return _vec(t, shape[1], dtype, what), 0
+    return _mat(t, shape, dtype, what)
 
 
 class PinnedBuffer:
@@ -799,6 +833,95 @@ class Helios:
         a = BlockMeanGradArgs(n, d, n_src, src_entry.numel(), x_type, 0, indptr.data_ptr(), src_indptr.data_ptr(), src_entry.data_ptr(),
                               *_mat(dmean, (n, d), dt, "dmean"), *_mat(down, (n, d), dt, "down"), *_mat(dx, (n_src, d), dt, "dx"))
         rc = _lib.helios_block_mean_grad(self._h, a)
+        if rc != OK:
+            self._check(rc)
+
+    def embedding(self, table: torch.Tensor, ids: torch.Tensor, y: torch.Tensor, scale: float = 1.0, add: Optional[torch.Tensor] = None,
+                  n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """y[i] = add[i] + scale * table[ids[i]]; -1 stands for no row."""
+        table_type, y_type = _type(table, "table"), _type(y, "y")
+        n_table, d = table.shape
+        n = y.shape[0]
+        _dev(ids, torch.int32, "ids")
+        assert ids.numel() == n
+        a = EmbeddingArgs(n, _count(n_rows_dev, "n_rows_dev"), d, n_table, table_type, y_type, scale, 0, *_mat(table, (n_table, d), table.dtype, "table"),
+                          ids.data_ptr(), *_mat(add, (n, d), y.dtype, "add"), *_mat(y, (n, d), y.dtype, "y"))
+        rc = _lib.helios_embedding(self._h, a)
+        if rc != OK:
+            self._check(rc)
+
+    def embedding_grad(self, ids: torch.Tensor, dy: torch.Tensor, n_table: int, scale: float = 1.0, dtable: Optional[torch.Tensor] = None,
+                       drow: Optional[torch.Tensor] = None, row_id: Optional[torch.Tensor] = None, n_distinct: Optional[torch.Tensor] = None,
+                       n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """The gradient of embedding's table: all of it (dtable), or the rows of the list's distinct IDs (drow, row_id, n_distinct)."""
+        out = dtable if dtable is not None else drow
+        if out is None:
+            raise TypeError("one of dtable and drow is needed")
+        table_type, y_type = _type(out, "dtable or drow"), _type(dy, "dy")
+        n, d = dy.shape
+        _dev(ids, torch.int32, "ids")
+        need = min(n, n_table)
+        assert ids.numel() == n
+        if row_id is not None:
+            _dev(row_id, torch.int32, "row_id")
+        if n_distinct is not None:
+            _dev_accessible(n_distinct, torch.int64, "n_distinct")
+        assert drow is None or drow.shape[0] >= need
+        assert row_id is None or row_id.numel() >= need
+        assert n_distinct is None or n_distinct.numel() >= 1
+        a = EmbeddingGradArgs(n, _count(n_rows_dev, "n_rows_dev"), d, n_table, table_type, y_type, scale, 0, ids.data_ptr(), *_mat(dy, (n, d), dy.dtype, "dy"),
+                              *_mat(dtable, (n_table, d), out.dtype, "dtable"), *_mat(drow, (drow.shape[0] if drow is not None else 0, d), out.dtype, "drow"),
+                              _ptr(row_id), _ptr(n_distinct))
+        rc = _lib.helios_embedding_grad(self._h, a)
+        if rc != OK:
+            self._check(rc)
+
+    def dropout(self, x: torch.Tensor, y: torch.Tensor, p: float, seed, site: int = 0, n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """y = x with a share p of its elements dropped (0) and the others scaled; on y's gradient, the gradient.  seed: a number, or an int64
+        tensor that is read on the device."""
+        n, d = x.shape
+        a = DropoutArgs(n, _count(n_rows_dev, "n_rows_dev"), d, _type(x, "x"), 0, *_drop(p, seed, site), *_mat(x, (n, d), x.dtype, "x"),
+                        *_mat(y, (n, d), x.dtype, "y"))
+        rc = _lib.helios_dropout(self._h, a)
+        if rc != OK:
+            self._check(rc)
+
+    def join_norm(self, x: torch.Tensor, eps: float, y: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None, norm_x: bool = True,
+                  gain_x: Optional[torch.Tensor] = None, p: float = 0.0, seed=0, site: int = 0, gate: Optional[torch.Tensor] = None,
+                  residual: Optional[torch.Tensor] = None, residual_scale: float = 1.0, gain: Optional[torch.Tensor] = None,
+                  y_scale: Optional[torch.Tensor] = None, inv_rms_x: Optional[torch.Tensor] = None, inv_rms: Optional[torch.Tensor] = None,
+                  n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """total = residual_scale * residual + gate * drop(norm(x) * gain_x), y = norm(total) * gain, in 8 bits with y_scale if y is float8_e4m3fn.
+        gate: a matrix, or a vector for all rows."""
+        x_type = _type(x, "x")
+        n, d = shape = x.shape
+        dt = x.dtype
+        y_type = x_type if y is None else _type(y, "y")
+        a = JoinNormArgs(n, _count(n_rows_dev, "n_rows_dev"), d, x_type, y_type, norm_x, 0, eps, residual_scale, *_drop(p, seed, site), *_mat(x, shape, dt, "x"),
+                         _vec(gain_x, d, dt, "gain_x"), *_gate(gate, shape, dt, "gate"), *_mat(residual, shape, dt, "residual"), _vec(gain, d, dt, "gain"),
+                         *_mat(total, shape, dt, "total"), *_mat(y, shape, dt if y is None else y.dtype, "y"), _vec(y_scale, n, torch.float32, "y_scale"),
+                         _vec(inv_rms_x, n, torch.float32, "inv_rms_x"), _vec(inv_rms, n, torch.float32, "inv_rms"))
+        rc = _lib.helios_join_norm(self._h, a)
+        if rc != OK:
+            self._check(rc)
+
+    def join_norm_grad(self, x: torch.Tensor, dx: torch.Tensor, eps: float, total: Optional[torch.Tensor] = None, dy: Optional[torch.Tensor] = None,
+                       dtotal: Optional[torch.Tensor] = None, norm_x: bool = True, gain_x: Optional[torch.Tensor] = None, p: float = 0.0, seed=0, site: int = 0,
+                       gate: Optional[torch.Tensor] = None, residual_scale: float = 1.0, gain: Optional[torch.Tensor] = None,
+                       dresidual: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None, dgain_x: Optional[torch.Tensor] = None,
+                       dgain: Optional[torch.Tensor] = None, inv_rms_x: Optional[torch.Tensor] = None, inv_rms: Optional[torch.Tensor] = None,
+                       n_rows_dev: Optional[torch.Tensor] = None) -> None:
+        """The gradients of join_norm that are given room for, from y's (dy, with total as join_norm left it) and total's (dtotal)."""
+        n, d = shape = x.shape
+        dt = x.dtype
+        gate_at, gate_ld = _gate(gate, shape, dt, "gate")
+        dgate_at, dgate_ld = _mat(dgate, shape, dt, "dgate") if gate_ld else (_vec(dgate, d, dt, "dgate"), 0)
+        a = JoinNormGradArgs(n, _count(n_rows_dev, "n_rows_dev"), d, _type(x, "x"), norm_x, eps, residual_scale, *_drop(p, seed, site), *_mat(x, shape, dt, "x"),
+                             _vec(gain_x, d, dt, "gain_x"), gate_at, gate_ld, _vec(gain, d, dt, "gain"), *_mat(total, shape, dt, "total"), *_mat(dy, shape, dt, "dy"),
+                             *_mat(dtotal, shape, dt, "dtotal"), _vec(inv_rms_x, n, torch.float32, "inv_rms_x"), _vec(inv_rms, n, torch.float32, "inv_rms"),
+                             *_mat(dx, shape, dt, "dx"), *_mat(dresidual, shape, dt, "dresidual"), dgate_at, dgate_ld, _vec(dgain_x, d, dt, "dgain_x"),
+                             _vec(dgain, d, dt, "dgain"))
+        rc = _lib.helios_join_norm_grad(self._h, a)
         if rc != OK:
             self._check(rc)
 
