@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(CSRC, "libhelios.so")
 SOURCES = ["pipeline.hip", "sample.hip", "dedup.hip", "cache.hip", "gather.hip", "blocks.hip", "hotness.hip", "missq.hip",
            "noalloc.hip", "helios_api.hip", "linear.hip", "norm.hip", "neighbours.hip",
-           "embedding.hip", "join.hip", "layer_api.hip"]
+           "embedding.hip", "join.hip", "join_grad.hip", "layer_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -22,39 +22,45 @@ constexpr int64_t kMostBlocks = 1 << 21;            // of a launch
 // ---- lookup
 
 constexpr int kItems = 2;                           // of a thread, in flight together
-template <int TABLE, int Y>
+// (An ID without a row loads the table's first, so that the load depends on no branch)
+template <int TABLE, int Y, int ROWS>
 __global__ __launch_bounds__(kBlock) void embedding_kernel(EmbeddingJob p) {
     const uint32_t blocks = static_cast<uint32_t>(p.width + 7) / 8;
     const int64_t items = p.rows.get() * blocks, step = static_cast<int64_t>(gridDim.x) * kBlock * kItems;
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * kBlock * kItems; base < items; base += step) {
         const ItemPlaces places(base, blocks);
+        const uint32_t left = items - base < kBlock * kItems ? static_cast<uint32_t>(items - base) : kBlock * kItems;
         Raw8<TABLE> row_raw[kItems];
         Raw8<Y> add_raw[kItems];
-        int64_t row[kItems];
-        int32_t col[kItems], valid[kItems], id[kItems];
+        uint32_t down[kItems];
+        int32_t col[kItems], id[kItems];
+        bool there[kItems];
 #pragma unroll
         for (int k = 0; k < kItems; ++k) {
             const uint32_t i = k * kBlock + threadIdx.x;
-            places.get(i, &row[k], &col[k]);
-            valid[k] = base + i < items ? p.width - col[k] : 0;
-            id[k] = valid[k] > 0 ? p.ids[row[k]] : -1;
+            places.get(i < left ? i : left - 1, &down[k], &col[k]);
+            id[k] = (p.ids + places.row0)[down[k]];
         }
 #pragma unroll
         for (int k = 0; k < kItems; ++k) {
-            const bool there = id[k] >= 0 && id[k] < p.n_table;
-            if (!there && id[k] != -1) raise(p.err, kErrData);
-            row_raw[k].load(p.table, there ? id[k] * p.table_ld + col[k] : 0, there ? valid[k] : 0);
-            if (p.add) add_raw[k].load(p.add, row[k] * p.add_ld + col[k], valid[k]);
+            there[k] = id[k] >= 0 && id[k] < p.n_table;
+            if (!there[k] && id[k] != -1) raise(p.err, kErrData);
+            row_raw[k].clear();
+            if (p.n_table > 0) row_raw[k].template load_row<ROWS>(p.table, (there[k] ? id[k] : 0) * p.table_ld, col[k], p.width);
+            if (p.add) add_raw[k].template load_row<ROWS>(p.add, places.row(p.add_ld, down[k]), col[k], p.width);
         }
 #pragma unroll
         for (int k = 0; k < kItems; ++k) {
-            const bool there = id[k] >= 0 && id[k] < p.n_table;
             float v[8], a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            row_raw[k].template align<ROWS>(col[k], p.width);
             widen_8<TABLE>(row_raw[k].v, v);
-            if (p.add) widen_8<Y>(add_raw[k].v, a);
+            if (p.add) {
+                add_raw[k].template align<ROWS>(col[k], p.width);
+                widen_8<Y>(add_raw[k].v, a);
+            }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = there ? __builtin_fmaf(v[e], p.scale, a[e]) : a[e];
-            store_8_of<Y>(p.y, row[k] * p.y_ld + col[k], valid[k], v);
+            for (int e = 0; e < 8; ++e) v[e] = there[k] ? __builtin_fmaf(v[e], p.scale, a[e]) : a[e];
+            if (k * kBlock + threadIdx.x < left) store_row_8<Y, ROWS>(p.y, places.row(p.y_ld, down[k]), col[k], p.width, v);
         }
     }
 }
@@ -66,13 +72,13 @@ typedef unsigned long long Entry;
 __device__ __forceinline__ uint32_t id_of(Entry e) { return static_cast<uint32_t>(e >> 32); }
 __device__ __forceinline__ uint32_t position_of(Entry e) { return static_cast<uint32_t>(e); }
 
-constexpr int kSmall = 2048;                        // lists that are ranked by comparing all with all
-constexpr int kSortBlock = 512, kSortItems = 8, kSortTile = kSortBlock * kSortItems, kSortWaves = kSortBlock / kWave;
-constexpr int kMostDigitBits = 8, kMostBins = 1 << kMostDigitBits, kLeastDigitBits = 4;
+constexpr int kFew = 2048;                          // lists that are not sorted (few_kernel)
+constexpr int kSortBlock = 512, kSortItems = 4, kSortTile = kSortBlock * kSortItems, kSortWaves = kSortBlock / kWave;
+constexpr int kMostDigitBits = 9, kMostBins = 1 << kMostDigitBits, kLeastDigitBits = 4;
 constexpr int kMostGroups = 256;                    // of consecutive tiles, a workgroup each
 constexpr int kHeadGroups = 512;
 constexpr int kFillBlocks = 2048;
-constexpr int kMostChunks = 8192;                   // of a list of more than kSmall
+constexpr int kMostChunks = 4096;                   // of a list
 
 struct GradArgs {
     Count rows;
@@ -88,7 +94,7 @@ struct GradArgs {
     int64_t* n_distinct;                            // null: out is the whole table
     int32_t* err;
     // how the list is cut
-    bool small;
+    bool few;                                       // it is not sorted at all (few_kernel)
     uint32_t n_groups, group_tiles;                 // of the sort
     uint32_t chunk;                                 // entries of a chunk: a power of two, 16 or more
     uint32_t head_span;                             // entries that a workgroup of heads_kernel counts
@@ -118,38 +124,12 @@ __device__ __forceinline__ void clear_table(const GradArgs& a, uint32_t block) {
     const int64_t items = static_cast<int64_t>(a.n_table) * blocks;
     const float zeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int64_t base = static_cast<int64_t>(block) * kSortBlock; base < items; base += static_cast<int64_t>(a.fill_blocks) * kSortBlock) {
-        int64_t row;
+        const ItemPlaces places(base, blocks);
+        uint32_t down;
         int32_t col;
-        ItemPlaces(base, blocks).get(threadIdx.x, &row, &col);
-        if (base + threadIdx.x < items) store_8_of<TYPE>(a.out, row * a.out_ld + col, a.width - col, zeros);
+        places.get(threadIdx.x, &down, &col);
+        if (base + threadIdx.x < items) store_8_of<TYPE>(a.out, places.row(a.out_ld, down) + col, a.width - col, zeros);
     }
-}
-
-// Short lists: a workgroup ranks 64 of the IDs, each of its waves against a share of all of them.
-constexpr uint32_t kRanked = kWave;
-template <int TYPE>
-__global__ __launch_bounds__(kSortBlock) void rank_kernel(GradArgs a, uint32_t rank_blocks) {
-    __shared__ uint32_t s_key[kSmall];
-    __shared__ uint32_t s_rank[kSortWaves][kRanked];
-    if (blockIdx.x >= rank_blocks) {
-        clear_table<TYPE>(a, blockIdx.x - rank_blocks);
-        return;
-    }
-    const uint32_t n = static_cast<uint32_t>(a.rows.get());
-    for (uint32_t i = threadIdx.x; i < n; i += kSortBlock) s_key[i] = key_of(a, i);
-    __syncthreads();
-    const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, first = blockIdx.x * kRanked, mine = first + lane;
-    const uint32_t share = (n + kSortWaves - 1) / kSortWaves, from = wave * share, to = min(from + share, n);
-    const uint32_t key = mine < n ? s_key[mine] : 0;
-    uint32_t rank = 0;
-    for (uint32_t j = from; j < to; ++j) rank += s_key[j] < key + (j < mine ? 1u : 0u) ? 1u : 0u;      // (equal IDs: those in front)
-    s_rank[wave][lane] = rank;
-    __syncthreads();
-    if (wave != 0 || mine >= n) return;
-    rank = 0;
-#pragma unroll
-    for (int w = 0; w < kSortWaves; ++w) rank += s_rank[w][lane];
-    a.list[0][rank] = static_cast<Entry>(key) << 32 | mine;
 }
 
 // A digit of the radix sort: `bits` bits of the ID from `shift` on.
@@ -194,57 +174,54 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* s_wave, uin
     __syncthreads();
     uint32_t before = inc - v;
     *all = 0;
-    for (int w = 0; w < static_cast<int>(blockDim.x) / kWave; ++w) {
-        if (w < wave_id()) before += s_wave[w];
-        *all += s_wave[w];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        const uint32_t c = s_wave[w];
+        if (w < wave_id()) before += c;
+        *all += c;
     }
     return before;
 }
 
 // Puts a group's entries where they belong.  Every workgroup adds up the groups' counts itself: all of them for where a digit begins, those of
-// the groups before for where its own entries of it go.
+// the groups before for where its own entries of it go.  The entries of a tile are ranked among each other while the counts are on their way.
 __global__ __launch_bounds__(kSortBlock) void place_kernel(GradArgs a, Digit d) {
-    __shared__ uint32_t s_next[kMostBins];          // where the next entry of a digit goes
-    __shared__ uint32_t s_count[kSortWaves][kMostBins];
+    __shared__ uint32_t s_next[kMostBins];          // entries of the digit in the groups before; then where the next one of it goes
+    __shared__ uint32_t s_total[kMostBins];
+    __shared__ uint32_t s_count[kSortWaves * kMostBins];      // [waves][bins]
     __shared__ uint32_t s_wave[kSortWaves];
-    __shared__ uint32_t s_total[kSortBlock][4], s_before[kSortBlock][4];
     typedef uint32_t words4 __attribute__((ext_vector_type(4)));
     const uint32_t n = static_cast<uint32_t>(a.rows.get()), bins = d.bins(), t = threadIdx.x, lane = t % kWave, wave = t / kWave;
-    {
-        const uint32_t quads = bins / 4, shares = kSortBlock / quads, quad = t % quads, share = t / quads;
-        words4 total = {0, 0, 0, 0}, before = {0, 0, 0, 0};
-#pragma unroll 8
-        for (uint32_t g = share; g < a.n_groups; g += shares) {
-            const words4 c = reinterpret_cast<const words4*>(a.counts + g * bins)[quad];
-            total += c;
-            if (g < blockIdx.x) before += c;
-        }
+    // a wave has kSortItems times 64 neighbouring entries of a tile
+    const uint32_t first = blockIdx.x * a.group_tiles * kSortTile + wave * (kSortItems * kWave) + lane;
+    Entry entry[kSortItems];
+    const auto load = [&](uint32_t tile) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s_total[t][e] = total[e], s_before[t][e] = before[e];
-        __syncthreads();
-        uint32_t sum = 0, at = 0;
-        if (t < bins)
-            for (uint32_t s = 0; s < shares; ++s) sum += s_total[s * quads + t / 4][t % 4], at += s_before[s * quads + t / 4][t % 4];
-        uint32_t all;
-        const uint32_t digit_begin = sum_before(sum, s_wave, &all);
-        if (t < bins) s_next[t] = digit_begin + at;
+        for (int k = 0; k < kSortItems; ++k) {
+            const uint32_t i = first + tile * kSortTile + k * kWave;
+            entry[k] = i < n ? entry_at(a, d, i) : ~Entry{0};
+        }
+    };
+    load(0);
+    const uint32_t quads = bins / 4, shares = kSortBlock / quads, quad = t % quads, share = t / quads;
+    words4 total = {0, 0, 0, 0}, before = {0, 0, 0, 0};
+#pragma unroll 8
+    for (uint32_t g = share; g < a.n_groups; g += shares) {
+        const words4 c = reinterpret_cast<const words4*>(a.counts + g * bins)[quad];
+        total += c;
+        if (g < blockIdx.x) before += c;
     }
+    for (uint32_t b = t; b < bins; b += kSortBlock) s_next[b] = s_total[b] = 0;
     for (uint32_t tile = 0; tile < a.group_tiles; ++tile) {
-        const uint32_t begin = (blockIdx.x * a.group_tiles + tile) * kSortTile;
-        if (begin >= n) break;
-        for (uint32_t b = t; b < kSortWaves * bins; b += kSortBlock) s_count[b / bins][b % bins] = 0;
+        const uint32_t at = first + tile * kSortTile;
+        if (tile > 0) load(tile);
+        for (uint32_t b = t; b < kSortWaves * bins; b += kSortBlock) s_count[b] = 0;
         __syncthreads();
-        // a wave has kSortItems times 64 neighbouring entries; a lane's rank among those of its digit: lanes below and rounds before
-        Entry entry[kSortItems];
+        // a lane's rank among those of its digit: lanes below and rounds before
         uint32_t rank[kSortItems];
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k) {
-            const uint32_t i = begin + wave * (kSortItems * kWave) + k * kWave + lane;
-            entry[k] = i < n ? entry_at(a, d, i) : ~Entry{0};
-        }
-#pragma unroll
-        for (int k = 0; k < kSortItems; ++k) {
-            const bool there = begin + wave * (kSortItems * kWave) + k * kWave + lane < n;
+            const bool there = at + k * kWave < n;
             const uint32_t digit = d.of(id_of(entry[k]));
             uint64_t peers = __ballot(there);
             for (uint32_t b = 0; b < d.bits; ++b) {
@@ -253,27 +230,45 @@ __global__ __launch_bounds__(kSortBlock) void place_kernel(GradArgs a, Digit d) 
                 peers &= one ? ones : ~ones;
             }
             const uint32_t below = rank_in_mask(peers);
-            volatile uint32_t* word = &s_count[wave][digit];
+            volatile uint32_t* word = s_count + wave * bins + digit;
             rank[k] = *word + below;
             __builtin_amdgcn_wave_barrier();
             if (there && below == 0) *word = *word + static_cast<uint32_t>(__popcll(peers));
             __builtin_amdgcn_wave_barrier();
         }
-        __syncthreads();
-        if (t < bins) {
-            uint32_t at = s_next[t];
-            for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t c = s_count[w][t];
-                s_count[w][t] = at;
-                at += c;
+        if (tile == 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                atomicAdd(s_total + 4 * quad + e, static_cast<uint32_t>(total[e]));
+                atomicAdd(s_next + 4 * quad + e, static_cast<uint32_t>(before[e]));
             }
-            s_next[t] = at;
+        }
+        __syncthreads();
+        if (tile == 0) {
+            uint32_t run = 0;                       // entries of the digits before
+            for (uint32_t from = 0; from < bins; from += kSortBlock) {
+                const uint32_t b = from + t;
+                uint32_t all;
+                const uint32_t digit_begin = sum_before(b < bins ? s_total[b] : 0, s_wave, &all);
+                if (b < bins) s_next[b] += run + digit_begin;
+                run += all;
+            }
+        }
+        for (uint32_t b = t; b < bins; b += kSortBlock) {
+            uint32_t to = s_next[b];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t c = s_count[w * bins + b];
+                s_count[w * bins + b] = to;
+                to += c;
+            }
+            s_next[b] = to;
         }
         __syncthreads();
         Entry* to = d.to == 0 ? a.list[0] : a.list[1];
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k)
-            if (begin + wave * (kSortItems * kWave) + k * kWave + lane < n) to[s_count[wave][d.of(id_of(entry[k]))] + rank[k]] = entry[k];
+            if (at + k * kWave < n) to[s_count[wave * bins + d.of(id_of(entry[k]))] + rank[k]] = entry[k];
         __syncthreads();
     }
 }
@@ -295,7 +290,7 @@ __global__ __launch_bounds__(kSortBlock) void heads_kernel(GradArgs a, const Ent
     __shared__ uint32_t s_wave[kSortWaves];
     const uint32_t n = static_cast<uint32_t>(a.rows.get());
     uint32_t run = 0;
-    for (uint32_t from = 0; from < a.head_span; from += kSortTile) {
+    for (uint32_t from = 0; from < a.head_span; from += kSortBlock * 8) {
         const uint32_t at = blockIdx.x * a.head_span + from + threadIdx.x * 8;
         uint32_t all;
         const uint32_t before = sum_before(heads_of_8(list, at, n, a.n_table), s_wave, &all);
@@ -305,145 +300,364 @@ __global__ __launch_bounds__(kSortBlock) void heads_kernel(GradArgs a, const Ent
     if (threadIdx.x == 0) a.group_heads[blockIdx.x] = run;
 }
 
-// The bits of a wave's mask that belong to this group of G lanes.
-template <int G>
-__device__ __forceinline__ uint64_t group_bits(uint64_t mask) {
-    if (G == kWave) return mask;
-    return mask >> (threadIdx.x % kWave / G * G) & ((uint64_t{1} << (G % 64)) - 1);
+// Where a row's elements are, V neighbouring ones to a lane of a wave (the fewest that reach over the row, at most 16 bytes), in blocks of 64 V columns.
+// A lane whose columns would reach beyond the last takes the last V, and so reads, adds and writes what another does, too: no load depends on a
+// branch, and so none waits for the one before it (with a branch around each: 281 600 rows of 128 in single precision 81 us).
+template <int V>
+struct LaneColumns {
+    uint32_t at;                                    // the first of them
+    bool any;                                       // a lane of which no column exists reads like the last that has some, and writes nothing
+    __device__ __forceinline__ LaneColumns(uint32_t lane, uint32_t first, int32_t width) {
+        const uint32_t w = static_cast<uint32_t>(width);
+        any = first + lane * V < w;
+        at = min(first + lane * V, w - V);
+    }
+};
+// V neighbouring elements of a row, as they are in memory (rows start anywhere an element may).
+template <int TYPE, int V>
+struct Few {
+    typedef typename ElementOf<TYPE>::type T;
+    typedef T vector __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    T v[V];
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (V == 1) {
+            v[0] = *p;
+        } else {
+            const vector x = *reinterpret_cast<const vector*>(p);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = x[e];
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const {
+        if constexpr (V == 1) {
+            *p = v[0];
+        } else {
+            vector x;
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = v[e];
+            *reinterpret_cast<vector*>(p) = x;
+        }
+    }
+    __device__ __forceinline__ void add(bool there, float (&to)[V]) const {
+#pragma unroll
+        for (int e = 0; e < V; ++e) to[e] += there ? static_cast<float>(v[e]) : 0.0f;
+    }
+};
+// (one rounding to TYPE, to nearest, ties to even)
+template <int TYPE, int V>
+__device__ __forceinline__ void store_scaled(void* base, int64_t at, const float (&v)[V], float by) {
+    typedef typename ElementOf<TYPE>::type T;
+    Few<TYPE, V> o;
+#pragma unroll
+    for (int e = 0; e < V; ++e) o.v[e] = static_cast<T>(v[e] * by);
+    o.store(static_cast<T*>(base) + at);
 }
 
-// A chunk to a group of G lanes, eight columns to a lane.
-constexpr int kRowsAhead = 8;
-template <int TYPE, int Y, int G>
-__global__ __launch_bounds__(kBlock) void sum_kernel(GradArgs a, const Entry* list, uint32_t n_tasks) {
-    __shared__ uint32_t s_wave[kBlock / kWave];
-    __shared__ uint32_t s_rank[kSmall / 16];
-    constexpr uint32_t kGroups = kBlock / G;
-    const uint32_t n = static_cast<uint32_t>(a.rows.get()), n_chunks = (n + a.chunk - 1) / a.chunk, lane = threadIdx.x % G;
-    if (a.n_distinct && a.small) {
-        uint32_t all;
-        const uint32_t before = sum_before(heads_of_8(list, threadIdx.x * 8, n, a.n_table), s_wave, &all);
-        if (threadIdx.x * 8 < n && threadIdx.x * 8 % a.chunk == 0) s_rank[threadIdx.x * 8 / a.chunk] = before;
+// ---- short lists
+
+// The distinct IDs of a short list, in LDS: where an ID is first.
+struct FewLds {
+    uint32_t key[kFew];
+    uint32_t slot_key[2 * kFew], slot_first[2 * kFew];
+    unsigned long long heads[kFew / kWave];         // a bit for every position: the first one of an ID that has a row
+};
+constexpr uint32_t kNoKey = ~0u;
+__device__ __forceinline__ uint32_t few_slot(uint32_t key) { return key * 0x9e3779b1u >> 20; }
+static_assert(2 * kFew == 1 << 12, "few_slot has twelve bits");
+__device__ __forceinline__ void find_distinct(const GradArgs& a, uint32_t n, FewLds& s) {
+    constexpr int kMine = kFew / kSortBlock;
+    uint32_t slot[kMine];
+    for (uint32_t i = threadIdx.x; i < 2 * kFew; i += kSortBlock) s.slot_key[i] = s.slot_first[i] = kNoKey;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+        const uint32_t i = k * kSortBlock + threadIdx.x;
+        s.key[i] = i < n ? key_of(a, i) : a.n_table;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+        const uint32_t i = k * kSortBlock + threadIdx.x, key = s.key[i];
+        slot[k] = few_slot(key);
+        if (key >= a.n_table) continue;
+        for (;;) {                                  // (at most half of the slots are ever taken)
+            const uint32_t there = atomicCAS(s.slot_key + slot[k], kNoKey, key);
+            if (there == kNoKey || there == key) break;
+            slot[k] = (slot[k] + 1) % (2 * kFew);
+        }
+        atomicMin(s.slot_first + slot[k], i);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+        const uint32_t i = k * kSortBlock + threadIdx.x;
+        const unsigned long long heads = __ballot(s.key[i] < a.n_table && s.slot_first[slot[k]] == i);
+        if (lane_id() == 0) s.heads[i / kWave] = heads;
+    }
+    __syncthreads();
+}
+__device__ __forceinline__ bool is_met(const FewLds& s, uint32_t key) {
+    for (uint32_t slot = few_slot(key);; slot = (slot + 1) % (2 * kFew)) {
+        if (s.slot_key[slot] == key) return true;
+        if (s.slot_key[slot] == kNoKey) return false;
+    }
+}
+
+// A list of up to kFew IDs in one launch and without a sort: every workgroup finds the distinct IDs for itself; a wave has a position, and if
+// that is its ID's first one, looks through the whole list for the ID's other positions and for how many distinct IDs are less, which
+// is the row's number.  An ID with more than kLongRun positions is left to all waves of its workgroup.  Rows of dtable that are not met are cleared by
+// workgroups of their own.
+constexpr int kLongRun = 64, kRowsAhead = 8;
+template <int TYPE, int Y, int V>
+__global__ __launch_bounds__(kSortBlock) void few_kernel(GradArgs a, uint32_t sum_blocks) {
+    typedef typename ElementOf<Y>::type T;
+    __shared__ FewLds s;
+    __shared__ uint32_t s_position[kSortWaves][kLongRun];
+    __shared__ uint32_t s_long[kSortWaves];         // the ID of a wave's long run, and its row
+    __shared__ uint32_t s_row[kSortWaves];
+    __shared__ float s_part[kSortWaves][V][kWave];
+    const uint32_t n = static_cast<uint32_t>(a.rows.get());
+    find_distinct(a, n, s);
+    if (blockIdx.x >= sum_blocks) {
+        const uint32_t blocks = static_cast<uint32_t>(a.width + 7) / 8;
+        const int64_t items = static_cast<int64_t>(a.n_table) * blocks;
+        const float zeros[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int64_t base = static_cast<int64_t>(blockIdx.x - sum_blocks) * kSortBlock; base < items; base += static_cast<int64_t>(a.fill_blocks) * kSortBlock) {
+            const ItemPlaces places(base, blocks);
+            uint32_t down;
+            int32_t col;
+            places.get(threadIdx.x, &down, &col);
+            if (base + threadIdx.x < items && !is_met(s, static_cast<uint32_t>(places.row0 + down)))
+                store_8_of<TYPE>(a.out, places.row(a.out_ld, down) + col, a.width - col, zeros);
+        }
+        return;
+    }
+    const uint32_t wave = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(wave_id())), lane = lane_id(), words = (n + kWave - 1) / kWave;
+    const uint32_t column_block = blockIdx.x % a.column_blocks, mine = blockIdx.x / a.column_blocks * kSortWaves + wave;
+    const LaneColumns<V> columns(lane, column_block * (kWave * V), a.width);
+    const T* dy = static_cast<const T*>(a.dy) + columns.at;
+    if (a.n_distinct && blockIdx.x == 0 && threadIdx.x == 0) {
+        int64_t u = 0;
+        for (uint32_t w = 0; w < words; ++w) u += __popcll(s.heads[w]);
+        *a.n_distinct = u;
+    }
+    float acc[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] = 0;
+    const auto to_row = [&](uint32_t row) {
+        if (columns.any) store_scaled<TYPE, V>(a.out, row * a.out_ld + columns.at, acc, a.scale);
+    };
+    if (lane == 0) s_long[wave] = kNoKey;
+    if (mine < n && (s.heads[mine / kWave] >> (mine % kWave) & 1)) {
+        const uint32_t id = s.key[mine];
+        uint32_t found = 0, row = id;
+        if (a.n_distinct) row = 0;
+        for (uint32_t w = 0; w < words; ++w) {
+            const uint32_t key = s.key[w * kWave + lane];
+            const uint64_t same = __ballot(key == id);
+            if (a.n_distinct) row += __popcll(__ballot(key < id) & s.heads[w]);
+            const uint32_t at = found + rank_in_mask(same);
+            if (key == id && at < kLongRun) s_position[wave][at] = w * kWave + lane;
+            found += __popcll(same);
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (a.n_distinct && column_block == 0 && lane == 0) a.row_id[row] = static_cast<int32_t>(id);
+        if (found > kLongRun) {
+            if (lane == 0) s_long[wave] = id, s_row[wave] = row;
+        } else {
+            for (uint32_t q = 0; q < found; q += kRowsAhead) {
+                Few<Y, V> rows[kRowsAhead];
+#pragma unroll
+                for (int k = 0; k < kRowsAhead; ++k) rows[k].load(dy + s_position[wave][min(q + k, found - 1)] * a.dy_ld);
+#pragma unroll
+                for (int k = 0; k < kRowsAhead; ++k) rows[k].add(q + k < found, acc);
+            }
+            to_row(row);
+        }
+    }
+    __syncthreads();
+    for (int run = 0; run < kSortWaves; ++run) {
+        const uint32_t id = s_long[run];
+        if (id == kNoKey) continue;
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = 0;
+        for (uint32_t w = wave; w < words; w += kSortWaves) {
+            uint64_t left = __ballot(s.key[w * kWave + lane] == id);
+            while (left) {
+                Few<Y, V> rows[kRowsAhead];
+                int in = 0;
+                uint32_t at = 0;
+#pragma unroll
+                for (int k = 0; k < kRowsAhead; ++k) {
+                    if (left) at = w * kWave + static_cast<uint32_t>(__ffsll(static_cast<long long>(left)) - 1), ++in;
+                    left &= left - 1;
+                    rows[k].load(dy + at * a.dy_ld);
+                }
+#pragma unroll
+                for (int k = 0; k < kRowsAhead; ++k) rows[k].add(k < in, acc);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) s_part[wave][e][lane] = acc[e];
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                acc[e] = 0;
+#pragma unroll
+                for (int w = 0; w < kSortWaves; ++w) acc[e] += s_part[w][e][lane];
+            }
+            to_row(s_row[run]);
+        }
         __syncthreads();
     }
-    for (uint32_t task = blockIdx.x; task < n_tasks; task += gridDim.x) {
-        const uint32_t column_block = task % a.column_blocks, chunk = task / a.column_blocks * kGroups + threadIdx.x / G;
-        const int32_t col = static_cast<int32_t>(column_block * G + lane) * 8, valid = a.width - col;
-        const uint32_t begin = chunk < n_chunks ? chunk * a.chunk : n, end = min(begin + a.chunk, n);
+}
+
+// ---- sums of the sorted list
+
+// A chunk to a wave: what it does next is the same for all lanes, so that the list, the places of rows and the branches are the scalar unit's, and
+// an entry costs a lane a load and V additions.
+constexpr int kAhead = 16;
+template <int TYPE, int Y, int V>
+__global__ __launch_bounds__(kBlock) void sum_kernel(GradArgs a, const Entry* list, uint32_t n_tasks) {
+    typedef typename ElementOf<Y>::type T;
+    const uint32_t n = static_cast<uint32_t>(a.rows.get()), n_chunks = (n + a.chunk - 1) / a.chunk, lane = lane_id();
+    const uint32_t wave = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(wave_id()));
+    for (uint32_t task = blockIdx.x * kWavesPerBlock + wave; task < n_tasks; task += gridDim.x * kWavesPerBlock) {
+        const uint32_t column_block = task % a.column_blocks, chunk = task / a.column_blocks;
+        if (chunk >= n_chunks) {
+            if (a.n_distinct && n_chunks == 0 && task == 0 && lane == 0) *a.n_distinct = 0;
+            continue;
+        }
+        const LaneColumns<V> columns(lane, column_block * (kWave * V), a.width);
+        const T* dy = static_cast<const T*>(a.dy) + columns.at;
+        const uint32_t begin = chunk * a.chunk, end = min(begin + a.chunk, n);
 
         // the row of drow of the first run that begins here
         uint32_t rank = 0;
-        if (a.n_distinct && a.small) {
-            if (begin < n) rank = s_rank[chunk];
-        } else if (a.n_distinct) {
-            if (begin < n)
-                for (uint32_t g = lane; g < begin / a.head_span; g += G) rank += a.group_heads[g];
-#pragma unroll
-            for (int d = G / 2; d >= 1; d >>= 1) rank += __shfl_xor(rank, d, kWave);
-            if (begin < n) rank += a.chunk_rank[chunk];
+        if (a.n_distinct) {
+            for (uint32_t g = lane; g < begin / a.head_span; g += kWave) rank += a.group_heads[g];
+            rank = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(wave_sum(rank)))) + a.chunk_rank[chunk];
         }
-
-        float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        bool any = false, headless = true;              // something in acc; no run has begun here so far
-        int32_t row = 0;                                // of the run in acc
-        const auto to_part = [&](int which) { store_8_of<kF32>(a.part, (static_cast<int64_t>(chunk) * 2 + which) * a.width + col, valid, acc); };
-        const auto to_row = [&] {
-            float v[8];
+        float acc[V];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = acc[e] * a.scale;
-            store_8_of<TYPE>(a.out, row * a.out_ld + col, valid, v);
+        for (int e = 0; e < V; ++e) acc[e] = 0;
+        bool any = false, headless = true;          // something in acc; no run has begun here so far
+        uint32_t row = 0;                           // of the run in acc
+        const auto to_part = [&](int which) {
+            if (columns.any) store_scaled<kF32, V>(a.part, (static_cast<int64_t>(chunk) * 2 + which) * a.width + columns.at, acc, 1.0f);
         };
-        const uint32_t batch = a.chunk < G ? a.chunk : G;
-        for (uint32_t from = 0; from < a.chunk; from += batch) {
-            const uint32_t at = begin + from + lane;
-            const bool in = lane < batch && at < end;
-            const Entry mine = in ? list[at] : 0;
-            const bool there = in && id_of(mine) < a.n_table, head = there && (at == 0 || id_of(list[at - 1]) != id_of(mine));
-            const uint64_t theres = group_bits<G>(__ballot(there)), heads = group_bits<G>(__ballot(head));
-            if (head && a.n_distinct && column_block == 0) a.row_id[rank + __popcll(heads & ((uint64_t{1} << lane) - 1))] = static_cast<int32_t>(id_of(mine));
-            for (uint32_t q = 0; q < batch; q += kRowsAhead) {
-                Raw8<Y> raw[kRowsAhead];
-                int32_t id[kRowsAhead];
+        const auto to_row = [&] {
+            if (columns.any) store_scaled<TYPE, V>(a.out, row * a.out_ld + columns.at, acc, a.scale);
+        };
+        for (uint32_t from = begin; from < end; from += kWave) {
+            const uint32_t at = from + lane;
+            const Entry mine = list[min(at, end - 1)], before = list[at > 0 ? min(at, end) - 1 : 0];
+            const bool there = at < end && id_of(mine) < a.n_table, head = there && (at == 0 || id_of(before) != id_of(mine));
+            const uint64_t heads = __ballot(head);
+            if (head && a.n_distinct && column_block == 0) a.row_id[rank + rank_in_mask(heads)] = static_cast<int32_t>(id_of(mine));
+            const uint32_t in = static_cast<uint32_t>(__popcll(__ballot(there)));        // (those that have a row come first)
+            for (uint32_t q = 0; q < in; q += kAhead) {
+                Few<Y, V> rows[kAhead];
 #pragma unroll
-                for (int k = 0; k < kRowsAhead; ++k) {
-                    const uint32_t position = __shfl(position_of(mine), q + k, G);
-                    id[k] = __shfl(static_cast<int32_t>(id_of(mine)), q + k, G);
-                    raw[k].load(a.dy, position * a.dy_ld + col, theres >> (q + k) & 1 ? valid : 0);
-                }
+                for (int k = 0; k < kAhead; ++k) rows[k].load(dy + lane_value(position_of(mine), min(q + k, in - 1)) * a.dy_ld);
 #pragma unroll
-                for (int k = 0; k < kRowsAhead; ++k) {
-                    if (!(theres >> (q + k) & 1)) continue;
+                for (int k = 0; k < kAhead; ++k) {
                     if (heads >> (q + k) & 1) {
                         if (any && headless) to_part(0);
                         else if (any) to_row();
                         headless = false;
-                        row = a.n_distinct ? static_cast<int32_t>(rank) : id[k];
+                        row = a.n_distinct ? rank : lane_value(id_of(mine), q + k);
                         ++rank;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) acc[e] = 0;
+                        for (int e = 0; e < V; ++e) acc[e] = 0;
                     }
                     any = true;
-                    float v[8];
-                    widen_8<Y>(raw[k].v, v);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) acc[e] += v[e];
+                    rows[k].add(q + k < in, acc);
                 }
             }
         }
-        if (begin < n) {
-            const uint32_t last = id_of(list[end - 1]);
-            const bool goes_on = last < a.n_table && end < n && id_of(list[end]) == last;
-            if (any && headless) to_part(0);
-            else if (any && goes_on) to_part(1);
-            else if (any) to_row();
-            if (column_block == 0 && lane == 0) a.info[chunk] = !any || !goes_on ? kNothing : headless ? kThrough : row;
+        const uint32_t last = id_of(list[end - 1]);
+        const bool goes_on = last < a.n_table && end < n && id_of(list[end]) == last;
+        if (any && headless) to_part(0);
+        else if (any && goes_on) to_part(1);
+        else if (any) to_row();
+        if (column_block == 0 && lane == 0) {
+            a.info[chunk] = !any || !goes_on ? kNothing : headless ? kThrough : static_cast<int32_t>(row);
+            if (a.n_distinct && chunk + 1 == n_chunks) *a.n_distinct = rank;
         }
-        if (a.n_distinct && column_block == 0 && lane == 0 && chunk + 1 == (n_chunks > 0 ? n_chunks : 1)) *a.n_distinct = rank;
     }
 }
 
-// Adds the parts of a run that begins in a chunk and goes on: eight lanes to 64 columns, and as many parts at a time as there are such lanes.
-constexpr int kMergeColumns = 64, kMergeSubs = kBlock / (kMergeColumns / 8);
-template <int TYPE>
-__global__ __launch_bounds__(kBlock) void merge_kernel(GradArgs a, uint32_t column_blocks, uint32_t n_tasks) {
-    __shared__ float s[kMergeSubs][kMergeColumns + 1];
-    __shared__ uint32_t s_last;
+// Adds the parts of a run that begins in a chunk and goes on.  A wave has 16 V columns of a chunk, 16 lanes to a part and four parts at a time; a run
+// that goes through the next 63 chunks is left to all waves of the workgroup.
+constexpr int kMergeLanes = 16, kMergeSubs = kWave / kMergeLanes, kMergeWaves = 8, kMergeBlock = kMergeWaves * kWave;
+template <int TYPE, int V>
+__global__ __launch_bounds__(kMergeBlock) void merge_kernel(GradArgs a, uint32_t column_blocks, uint32_t n_tasks) {
+    __shared__ float s[kMergeWaves][V][kMergeLanes];
+    __shared__ uint32_t s_long[kMergeWaves], s_last;
     const uint32_t n = static_cast<uint32_t>(a.rows.get()), n_chunks = (n + a.chunk - 1) / a.chunk;
-    for (uint32_t task = blockIdx.x; task < n_tasks; task += gridDim.x) {
-        const uint32_t chunk = task / column_blocks;
-        const int32_t row = chunk < n_chunks ? a.info[chunk] : kNothing;
-        if (row < 0) continue;
-        if (threadIdx.x == 0) s_last = n_chunks;
-        __syncthreads();
-        for (uint32_t from = chunk + 1; from < n_chunks; from += kBlock) {       // the first chunk that the run does not go through
-            const uint32_t c = from + threadIdx.x;
-            if (c < n_chunks && a.info[c] != kThrough) atomicMin(&s_last, c);
-            __syncthreads();
-            const bool found = s_last < n_chunks;
-            __syncthreads();
-            if (found) break;
-        }
-        const uint32_t last = min(s_last, n_chunks - 1), sub = threadIdx.x / 8;
-        const int32_t first_col = static_cast<int32_t>(task % column_blocks) * kMergeColumns, at = threadIdx.x % 8 * 8, col = first_col + at, valid = a.width - col;
-        float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (valid > 0) {
-            if (sub == 0) load_8_of<kF32>(a.part, (static_cast<int64_t>(chunk) * 2 + 1) * a.width + col, valid, acc);
-#pragma unroll 4
-            for (uint32_t c = chunk + 1 + sub; c <= last; c += kMergeSubs) {
-                float v[8];
-                load_8_of<kF32>(a.part, static_cast<int64_t>(c) * 2 * a.width + col, valid, v);
+    const uint32_t wave = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(wave_id())), lane = lane_id() % kMergeLanes, sub = lane_id() / kMergeLanes;
+    float acc[V];
+    // the part of the chunk where the run begins, if there is one to be had for this lane, and those of first, first + step, ... up to `last`
+    const auto add_parts = [&](uint32_t chunk, bool begins, uint32_t first, uint32_t last, uint32_t step, uint32_t col) {
+        Few<kF32, V> begin;
+        begin.load(a.part + (static_cast<int64_t>(chunk) * 2 + 1) * a.width + col);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) acc[e] += v[e];
+        for (int e = 0; e < V; ++e) acc[e] = begins ? begin.v[e] : 0.0f;
+        for (uint32_t c = first; c <= last; c += step * kRowsAhead) {
+            Few<kF32, V> parts[kRowsAhead];
+#pragma unroll
+            for (int k = 0; k < kRowsAhead; ++k) parts[k].load(a.part + static_cast<int64_t>(min(c + k * step, last)) * 2 * a.width + col);
+#pragma unroll
+            for (int k = 0; k < kRowsAhead; ++k) parts[k].add(c + k * step <= last, acc);
+        }
+        // over the lanes that share a column
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            acc[e] += __shfl_xor(acc[e], 16, kWave);
+            acc[e] += __shfl_xor(acc[e], 32, kWave);
+        }
+    };
+    const auto columns_of = [&](uint32_t task) { return LaneColumns<V>(lane, (task % column_blocks) * (kMergeLanes * V), a.width); };
+    for (uint32_t base = blockIdx.x * kMergeWaves; base < n_tasks; base += gridDim.x * kMergeWaves) {
+        const uint32_t task = base + wave, chunk = task / column_blocks;
+        const uint32_t c = chunk + lane_id();
+        const int32_t info = task < n_tasks && c < n_chunks ? a.info[c] : kNothing, row = __builtin_amdgcn_readfirstlane(info);
+        const uint64_t ends = ~__ballot(info == kThrough) & ~uint64_t{1};        // chunks that a run from the first one does not go through
+        if (lane_id() == 0) s_long[wave] = row >= 0 && ends == 0 ? task : kNoKey;
+        if (row >= 0 && ends != 0) {
+            const LaneColumns<V> columns = columns_of(task);
+            add_parts(chunk, sub == 0, chunk + 1 + sub, chunk + static_cast<uint32_t>(__ffsll(static_cast<long long>(ends)) - 1), kMergeSubs, columns.at);
+            if (sub == 0 && columns.any) store_scaled<TYPE, V>(a.out, row * a.out_ld + columns.at, acc, a.scale);
+        }
+        __syncthreads();
+        for (int w = 0; w < kMergeWaves; ++w) {
+            const uint32_t task = s_long[w], chunk = task / column_blocks;
+            if (task == kNoKey) continue;
+            if (threadIdx.x == 0) s_last = n_chunks;
+            __syncthreads();
+            for (uint32_t from = chunk + kWave; from < n_chunks; from += kMergeBlock) {       // the first chunk that the run does not go through
+                const uint32_t c = from + threadIdx.x;
+                if (c < n_chunks && a.info[c] != kThrough) atomicMin(&s_last, c);
+                __syncthreads();
+                const bool found = s_last < n_chunks;
+                __syncthreads();
+                if (found) break;
             }
-        }
+            const LaneColumns<V> columns = columns_of(task);
+            add_parts(chunk, wave == 0 && sub == 0, chunk + 1 + wave * kMergeSubs + sub, min(s_last, n_chunks - 1), kMergeSubs * kMergeWaves, columns.at);
+            if (sub == 0)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[sub][at + e] = acc[e];
-        __syncthreads();
-        if (threadIdx.x < kMergeColumns && first_col + static_cast<int32_t>(threadIdx.x) < a.width) {
-            float v = 0;
+                for (int e = 0; e < V; ++e) s[wave][e][lane] = acc[e];
+            __syncthreads();
+            if (wave == 0 && sub == 0 && columns.any) {
 #pragma unroll
-            for (int k = 0; k < kMergeSubs; ++k) v += s[k][threadIdx.x];
-            store_1(TYPE, a.out, row * a.out_ld + first_col + static_cast<int32_t>(threadIdx.x), v * a.scale);
+                for (int e = 0; e < V; ++e)
+#pragma unroll
+                    for (int k = 1; k < kMergeWaves; ++k) acc[e] += s[k][e][lane];
+                store_scaled<TYPE, V>(a.out, a.info[chunk] * a.out_ld + columns.at, acc, a.scale);
+            }
+            __syncthreads();
         }
         __syncthreads();
     }
@@ -451,13 +665,13 @@ __global__ __launch_bounds__(kBlock) void merge_kernel(GradArgs a, uint32_t colu
 
 // ---- launches
 
-int lanes_for(int32_t width) { return width <= 128 ? 16 : width <= 256 ? 32 : 64; }
 uint32_t ceil_div(int64_t a, int64_t b) { return static_cast<uint32_t>((a + b - 1) / b); }
 
 // How a list is cut, and how much scratch it takes.
 struct GradPlan {
     GradArgs a;
     uint32_t n_chunks, head_groups;
+    int per_lane;                                   // neighbouring columns of a row
     size_t bytes;
     GradPlan(const EmbeddingGradJob& job, char* scratch) {
         const int64_t n = job.rows.host;
@@ -466,14 +680,16 @@ struct GradPlan {
         a.width = job.width, a.scale = job.scale, a.n_table = static_cast<uint32_t>(job.n_table);
         a.ids = job.ids, a.dy = job.dy, a.dy_ld = job.dy_ld, a.out = job.out, a.out_ld = job.out_ld;
         a.row_id = job.row_id, a.n_distinct = job.n_distinct, a.err = job.err;
-        a.small = n <= kSmall;
+        a.few = n <= kFew;
+        per_lane = 1;
+        while (per_lane * type_bytes(job.y_type) < 16 && per_lane * kWave < job.width) per_lane *= 2;
         const int64_t tiles = (n + kSortTile - 1) / kSortTile;
         a.group_tiles = std::max<uint32_t>(1, ceil_div(tiles, kMostGroups));
         a.n_groups = ceil_div(tiles, a.group_tiles);
-        a.chunk = a.small ? 16 : 32;
+        a.chunk = 32;
         while (n > static_cast<int64_t>(a.chunk) * kMostChunks) a.chunk *= 2;
-        a.head_span = std::max<uint32_t>(1, ceil_div(tiles, kHeadGroups)) * kSortTile;
-        a.column_blocks = ceil_div(a.width, 8 * lanes_for(a.width));
+        a.head_span = std::max<uint32_t>(1, ceil_div(n, int64_t{kHeadGroups} * kSortBlock * 8)) * kSortBlock * 8;
+        a.column_blocks = ceil_div(job.width, per_lane * kWave);
         a.fill_blocks = job.n_distinct ? 0 : static_cast<uint32_t>(std::min<int64_t>(kFillBlocks, ceil_div(job.n_table * ((job.width + 7) / 8), kSortBlock)));
         n_chunks = ceil_div(n, a.chunk);
         head_groups = ceil_div(n, a.head_span);
@@ -482,9 +698,10 @@ struct GradPlan {
             *to = reinterpret_cast<std::remove_reference_t<decltype(**to)>*>(scratch + bytes);
             bytes = (bytes + count * sizeof(**to) + 255) / 256 * 256;
         };
+        if (a.few) return;
         take(&a.list[0], n);
-        take(&a.list[1], a.small ? 0 : n);
-        take(&a.counts, a.small ? 0 : static_cast<size_t>(a.n_groups) * kMostBins);
+        take(&a.list[1], n);
+        take(&a.counts, static_cast<size_t>(a.n_groups) * kMostBins);
         take(&a.chunk_rank, n_chunks);
         take(&a.group_heads, head_groups);
         take(&a.info, n_chunks);
@@ -492,16 +709,27 @@ struct GradPlan {
     }
 };
 
+template <int TYPE, int Y, int V>
+void launch_sums(hipStream_t stream, const GradPlan& plan, const Entry* list) {
+    const GradArgs& a = plan.a;
+    if (a.few) {
+        const uint32_t sum_blocks = std::max<uint32_t>(ceil_div(a.rows.host, kSortWaves), a.n_distinct ? 1 : 0) * a.column_blocks;
+        hipLaunchKernelGGL((few_kernel<TYPE, Y, V>), dim3(sum_blocks + a.fill_blocks), dim3(kSortBlock), 0, stream, a, sum_blocks);
+        return;
+    }
+    const uint32_t tasks = plan.n_chunks * a.column_blocks;      // (fewer than 2^31: kMostChunks)
+    hipLaunchKernelGGL((sum_kernel<TYPE, Y, V>), dim3(std::min<uint32_t>(ceil_div(tasks, kWavesPerBlock), kMostBlocks)), dim3(kBlock), 0, stream, a, list, tasks);
+}
+template <int TYPE, int V>
+void launch_merge(hipStream_t stream, const GradPlan& plan) {
+    const uint32_t columns = ceil_div(plan.a.width, V * kMergeLanes), tasks = plan.n_chunks * columns;
+    hipLaunchKernelGGL((merge_kernel<TYPE, V>), dim3(std::min<uint32_t>(ceil_div(tasks, kMergeWaves), kMostBlocks)), dim3(kMergeBlock), 0, stream, plan.a, columns, tasks);
+}
 template <int TYPE, int Y>
 hipError_t run_grad(hipStream_t stream, const GradPlan& plan) {
     const GradArgs& a = plan.a;
-    const int64_t n = a.rows.host;
-    const Entry* list = a.list[0];
-    if (a.small) {
-        const uint32_t rank_blocks = ceil_div(n, kRanked);
-        if (rank_blocks + a.fill_blocks > 0)
-            hipLaunchKernelGGL(rank_kernel<TYPE>, dim3(rank_blocks + a.fill_blocks), dim3(kSortBlock), 0, stream, a, rank_blocks);
-    } else {
+    const Entry* list = nullptr;
+    if (!a.few) {
         const uint32_t id_bits = 32 - static_cast<uint32_t>(__builtin_clz(a.n_table | 1)), passes = ceil_div(id_bits, kMostDigitBits);
         const uint32_t bits = std::max<uint32_t>(kLeastDigitBits, ceil_div(id_bits, passes));
         for (uint32_t p = 0; p < passes; ++p) {
@@ -512,31 +740,35 @@ hipError_t run_grad(hipStream_t stream, const GradPlan& plan) {
         list = a.list[(passes - 1) % 2];
         if (a.n_distinct) hipLaunchKernelGGL(heads_kernel, dim3(plan.head_groups), dim3(kSortBlock), 0, stream, a, list);
     }
-    if (n < 1 && !a.n_distinct) return hipGetLastError();
-    const int lanes = lanes_for(a.width);
-    const uint32_t tasks = std::max<uint32_t>(1, ceil_div(plan.n_chunks, kBlock / lanes)) * a.column_blocks;      // (fewer than 2^31: kMostChunks)
-    const dim3 grid(std::min<uint32_t>(tasks, kMostBlocks));
-    if (lanes == 16) hipLaunchKernelGGL((sum_kernel<TYPE, Y, 16>), grid, dim3(kBlock), 0, stream, a, list, tasks);
-    else if (lanes == 32) hipLaunchKernelGGL((sum_kernel<TYPE, Y, 32>), grid, dim3(kBlock), 0, stream, a, list, tasks);
-    else hipLaunchKernelGGL((sum_kernel<TYPE, Y, 64>), grid, dim3(kBlock), 0, stream, a, list, tasks);
-    if (plan.n_chunks > 1) {
-        const uint32_t columns = ceil_div(a.width, kMergeColumns), merges = plan.n_chunks * columns;
-        hipLaunchKernelGGL(merge_kernel<TYPE>, dim3(std::min<uint32_t>(merges, kMostBlocks)), dim3(kBlock), 0, stream, a, columns, merges);
+    if (plan.per_lane == 1) launch_sums<TYPE, Y, 1>(stream, plan, list);
+    else if (plan.per_lane == 2) launch_sums<TYPE, Y, 2>(stream, plan, list);
+    else if (plan.per_lane == 4) launch_sums<TYPE, Y, 4>(stream, plan, list);
+    else if constexpr (Y != kF32) launch_sums<TYPE, Y, 8>(stream, plan, list);
+    if (!a.few) {
+        if (a.width >= 4) launch_merge<TYPE, 4>(stream, plan);
+        else launch_merge<TYPE, 1>(stream, plan);
     }
     return hipGetLastError();
+}
+
+template <int TABLE, int Y>
+void run_lookup(hipStream_t stream, const EmbeddingJob& job) {
+    const int64_t items = job.rows.host * ((job.width + 7) / 8);
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((items + kBlock * kItems - 1) / (kBlock * kItems), kMostBlocks)));
+    if (job.width % 8 == 0) hipLaunchKernelGGL((embedding_kernel<TABLE, Y, kWholeRows>), grid, dim3(kBlock), 0, stream, job);
+    else if (job.width > 8) hipLaunchKernelGGL((embedding_kernel<TABLE, Y, kRowsWithRest>), grid, dim3(kBlock), 0, stream, job);
+    else hipLaunchKernelGGL((embedding_kernel<TABLE, Y, kShortRows>), grid, dim3(kBlock), 0, stream, job);
 }
 
 }  // namespace
 
 hipError_t launch_embedding(hipStream_t stream, const EmbeddingJob& job) {
     if (job.rows.host < 1) return hipSuccess;
-    const int64_t items = job.rows.host * ((job.width + 7) / 8);
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((items + kBlock * kItems - 1) / (kBlock * kItems), kMostBlocks))), block(kBlock);
-    if (job.table_type == kF16) hipLaunchKernelGGL((embedding_kernel<kF16, kF16>), grid, block, 0, stream, job);
-    else if (job.table_type == kBF16) hipLaunchKernelGGL((embedding_kernel<kBF16, kBF16>), grid, block, 0, stream, job);
-    else if (job.y_type == kF16) hipLaunchKernelGGL((embedding_kernel<kF32, kF16>), grid, block, 0, stream, job);
-    else if (job.y_type == kBF16) hipLaunchKernelGGL((embedding_kernel<kF32, kBF16>), grid, block, 0, stream, job);
-    else hipLaunchKernelGGL((embedding_kernel<kF32, kF32>), grid, block, 0, stream, job);
+    if (job.table_type == kF16) run_lookup<kF16, kF16>(stream, job);
+    else if (job.table_type == kBF16) run_lookup<kBF16, kBF16>(stream, job);
+    else if (job.y_type == kF16) run_lookup<kF32, kF16>(stream, job);
+    else if (job.y_type == kBF16) run_lookup<kF32, kBF16>(stream, job);
+    else run_lookup<kF32, kF32>(stream, job);
     return hipGetLastError();
 }
 

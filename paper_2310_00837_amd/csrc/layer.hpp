@@ -1,5 +1,5 @@
 // Launchers of the operators of a model's layer on a prepared mini-batch (linear.hip, norm.hip, neighbours.hip,
-// embedding.hip, join.hip).
+// embedding.hip, join.hip, join_grad.hip).
 // Every launcher enqueues on `stream` and returns the hipError_t of the launch.
 #pragma once
 #include "common.hpp"
@@ -175,7 +175,7 @@ struct EmbeddingGradJob {
 size_t embedding_grad_scratch_bytes(const EmbeddingGradJob& job);
 hipError_t launch_embedding_grad(hipStream_t stream, const EmbeddingGradJob& job, void* scratch);
 
-// ---- join.hip
+// ---- join.hip, join_grad.hip
 struct Drop {
     uint64_t seed;
     const uint64_t* seed_dev;                     // nullable: read in place of seed

@@ -2,6 +2,8 @@
 #pragma once
 #include "common.hpp"
 
+#include <type_traits>
+
 namespace helios {
 
 // element types, same values as helios_dtype
@@ -67,6 +69,8 @@ __device__ __forceinline__ void widen_8(const i32x4 (&raw)[type_bytes(TYPE) / 2]
         }
     }
 }
+// Rows that are taken eight elements at a time: their width is a multiple of eight, is not, or is less than eight.
+enum Rows { kWholeRows = 0, kRowsWithRest = 1, kShortRows = 2 };
 // Eight elements as they are in memory, in half the registers where they have 16 bits; zeros where there are none.
 template <int TYPE>
 struct Raw8 {
@@ -83,6 +87,47 @@ struct Raw8 {
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int k = 0; k < type_bytes(TYPE) / 2; ++k) v[k] = i32x4{0, 0, 0, 0};
+    }
+    // The elements from column `col` (a multiple of eight) on of the row of `width` elements that begins at `at`, without a branch that differs from lane
+    // to lane, so that no load waits for those before it: where fewer than eight are left, the row's last eight are loaded, and align()
+    // puts them in their places.  A lane beyond the row holds values of its end.  (Short rows are loaded with branches.)
+    template <int ROWS>
+    __device__ __forceinline__ void load_row(const void* base, int64_t at, int32_t col, int32_t width) {
+        if (ROWS == kShortRows) {
+            load(base, at + col, width - col);
+            return;
+        }
+        const char* p = static_cast<const char*>(base) + (at + (col < width - 8 ? col : width - 8)) * type_bytes(TYPE);
+#pragma unroll
+        for (int k = 0; k < type_bytes(TYPE) / 2; ++k) v[k] = load_16(p + 16 * k);
+    }
+    template <int ROWS>
+    __device__ __forceinline__ void align(int32_t col, int32_t width) {
+        if (ROWS != kRowsWithRest) return;
+        const int rest = width & 7;                       // the same for all lanes: the branches are the scalar unit's
+        constexpr int kWords = type_bytes(TYPE) * 2, kPerWord = 4 / type_bytes(TYPE);
+        const bool moves = col + 8 > width;
+        const int words = (8 - rest) / kPerWord;          // to go down by
+        uint32_t w[kWords];
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) w[k] = static_cast<uint32_t>(v[k / 4][k % 4]);
+        const auto down = [&](auto by) {
+            constexpr int kBy = decltype(by)::value;
+            if (words & kBy)
+#pragma unroll
+                for (int k = 0; k < kWords; ++k) {
+                    const uint32_t from = k + kBy < kWords ? w[(k + kBy) % kWords] : 0u;
+                    w[k] = moves ? from : w[k];
+                }
+        };
+        if (kWords == 8) down(std::integral_constant<int, 4>());
+        down(std::integral_constant<int, 2>());
+        down(std::integral_constant<int, 1>());
+        if (kPerWord == 2 && (rest & 1))
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) w[k] = !moves ? w[k] : w[k] >> 16 | (k + 1 < kWords ? w[k + 1] : 0u) << 16;
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) v[k / 4][k % 4] = static_cast<int32_t>(w[k]);
     }
 };
 // ... or from memory
@@ -130,6 +175,36 @@ __device__ __forceinline__ void store_8_of(void* base, int64_t at, int valid, co
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (e < valid) p[e] = static_cast<T>(v[e]);
+}
+// ... from column `col` (a multiple of eight) on of a row of `width` elements that begins at `at`: the row's last ones, where they are fewer than eight,
+// as four, two and one of them.
+template <int TYPE, int ROWS>
+__device__ __forceinline__ void store_row_8(void* base, int64_t at, int32_t col, int32_t width, const float (&v)[8]) {
+    typedef typename ElementOf<TYPE>::type T;
+    typedef T tx2 __attribute__((ext_vector_type(2), aligned(sizeof(T))));
+    typedef T tx4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    if (col + 8 <= width) {
+        store_8_of<TYPE>(base, at + col, 8, v);
+    } else if (ROWS != kWholeRows && col < width) {
+        T* p = static_cast<T*>(base) + at + col;
+        const int rest = width & 7;
+        const auto two = [&](int e, float a, float b) { *reinterpret_cast<tx2*>(p + e) = tx2{static_cast<T>(a), static_cast<T>(b)}; };
+        // (branches to the end: elements chosen by conditions would make an array in memory of v)
+        if (rest & 4) {
+            *reinterpret_cast<tx4*>(p) = tx4{static_cast<T>(v[0]), static_cast<T>(v[1]), static_cast<T>(v[2]), static_cast<T>(v[3])};
+            if (rest & 2) {
+                two(4, v[4], v[5]);
+                if (rest & 1) p[6] = static_cast<T>(v[6]);
+            } else if (rest & 1) {
+                p[4] = static_cast<T>(v[4]);
+            }
+        } else if (rest & 2) {
+            two(0, v[0], v[1]);
+            if (rest & 1) p[2] = static_cast<T>(v[2]);
+        } else {
+            p[0] = static_cast<T>(v[0]);
+        }
+    }
 }
 // (the type is an argument of the kernel: the branches are the same for all lanes)
 __device__ __forceinline__ void store_1(int type, void* base, int64_t at, float v) {
@@ -247,17 +322,35 @@ __device__ __forceinline__ float group_max(float v) {
 }
 
 // Where the items of a workgroup are, from number `base` on: an item is eight neighbouring columns of a row, items are numbered along the rows
-// (of `blocks` items each, fewer than 2^22).
+// (of `blocks` items each, at most 2^21).  What is the same for all threads is the scalar unit's; the division by `blocks` goes by its
+// reciprocal (off by one at most: at and blocks are below 2^22, which 32-bit floats and 24-bit products hold).
 struct ItemPlaces {
     int64_t row0;
     uint32_t rem0, blocks;
-    __device__ __forceinline__ ItemPlaces(int64_t base, uint32_t row_blocks) : row0(base / row_blocks), rem0(static_cast<uint32_t>(base % row_blocks)), blocks(row_blocks) {}
-    __device__ __forceinline__ void get(uint32_t i, int64_t* row, int32_t* col) const {
-        const uint32_t at = rem0 + i, down = at / blocks;
-        *row = row0 + down;
-        *col = static_cast<int32_t>(at - down * blocks) * 8;
+    float inverse;
+    __device__ __forceinline__ ItemPlaces(int64_t base, uint32_t row_blocks)
+        : row0(base / row_blocks), rem0(static_cast<uint32_t>(base % row_blocks)), blocks(row_blocks), inverse(1.0f / static_cast<float>(row_blocks)) {}
+    // item i's row is row0 + down
+    __device__ __forceinline__ void get(uint32_t i, uint32_t* down, int32_t* col) const {
+        const uint32_t at = rem0 + i;
+        uint32_t q = static_cast<uint32_t>(static_cast<float>(at) * inverse);
+        int32_t left = static_cast<int32_t>(at - (q & 0xffffffu) * (blocks & 0xffffffu));
+        if (left < 0) q -= 1, left += static_cast<int32_t>(blocks);
+        else if (left >= static_cast<int32_t>(blocks)) q += 1, left -= static_cast<int32_t>(blocks);
+        *down = q;
+        *col = left * 8;
     }
+    // the element of a matrix where its row begins
+    __device__ __forceinline__ int64_t row(int64_t ld, uint32_t down) const { return row0 * ld + static_cast<int64_t>(down) * ld; }
 };
+
+// Which of a workgroup's rows is a thread's, if LANES share one: the same for a whole wave where it is.  (Where it is not, the lanes of a wave go through
+// their rows in step all the same: those that have none left take the last one, and write nothing.)
+template <int LANES>
+__device__ __forceinline__ int row_of_lanes() {
+    const int sub = static_cast<int>(threadIdx.x) / LANES;
+    return LANES >= kWave ? __builtin_amdgcn_readfirstlane(sub) : sub;
+}
 
 // Lanes that share a row: LANES (a power of two), each with CHUNKS times eight elements; up to a wave several rows to a workgroup, else
 // the workgroup has one.
@@ -269,7 +362,7 @@ struct RowShape {
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float* s) {
     v = group_sum<(LANES < kWave ? LANES : kWave)>(v);
-    if (LANES > kWave) {
+    if constexpr (LANES > kWave) {
         constexpr int kWaves = LANES / kWave;
         __syncthreads();
         if (lane_id() == 0) s[wave_id()] = v;
@@ -281,10 +374,51 @@ __device__ __forceinline__ float row_sum(float v, float* s) {
     }
     return v;
 }
+// The sum over a group of lanes (16, or a wave), with the additions in group_sum's order: every step within 16 lanes is one instruction, and for a
+// wave two more carry the rows' sums to the last lane (32 instructions fewer for the four sums of a row of the join's gradient).
+template <int G>
+__device__ __forceinline__ float lanes_sum(float v) {
+    static_assert(G == 16 || G == 64, "a row of lanes, or a wave");
+    const auto add = [&](auto control) {
+        v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
+    };
+    add(std::integral_constant<int, 0xb1>());
+    add(std::integral_constant<int, 0x4e>());
+    add(std::integral_constant<int, 0x141>());
+    add(std::integral_constant<int, 0x140>());
+    if (G == 16) return v;
+    // (a lane's value may be read by such a move two cycles after it was written)
+    asm volatile("s_nop 1\n\tv_add_f32_dpp %0, %0, %0 row_bcast:15 row_mask:0xa bank_mask:0xf\n\ts_nop 1\n\tv_add_f32_dpp %0, %0, %0 row_bcast:31 row_mask:0xc bank_mask:0xf"
+        : "+v"(v));
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kWave - 1));
+}
+// N sums at once, by one exchange; `s` has room for two of them, which take turns, so that one barrier does.
+template <int LANES, int N>
+struct RowSums {
+    static constexpr int kWaves = LANES < kWave ? 1 : LANES / kWave;
+    float (*s)[N][kWaves];                          // [2], in LDS; one row to a workgroup where it is used
+    int turn = 0;
+    __device__ __forceinline__ void run(float (&v)[N]) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = lanes_sum<(LANES < kWave ? LANES : kWave)>(v[k]);
+        if (LANES <= kWave) return;
+        if (lane_id() == 0)
+#pragma unroll
+            for (int k = 0; k < N; ++k) s[turn][k][wave_id()] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v[k] += s[turn][k][w];
+        }
+        turn ^= 1;
+    }
+};
 template <int LANES>
 __device__ __forceinline__ float row_max(float v, float* s) {
     v = group_max<(LANES < kWave ? LANES : kWave)>(v);
-    if (LANES > kWave) {
+    if constexpr (LANES > kWave) {
         constexpr int kWaves = LANES / kWave;
         __syncthreads();
         if (lane_id() == 0) s[wave_id()] = v;
@@ -359,7 +493,8 @@ __device__ __forceinline__ void finish_row(float (&t)[CHUNKS][8], int32_t width,
 // them share a part's columns and 64 go through the parts, so that few loads follow on one another; the order of the additions
 // is the same in every call.
 constexpr int kSumColumns = 16;
-__device__ __forceinline__ void sum_columns(const float* part, int n_parts, int32_t n, int32_t first, void* out, int type) {
+template <class STORE>                            // store(column, sum)
+__device__ __forceinline__ void sum_columns(const float* part, int n_parts, int32_t n, int32_t first, STORE store) {
     constexpr int kSubs = kBlock / 4;
     __shared__ float s[kSubs][kSumColumns + 1], s2[16][kSumColumns + 1];
     const int c = threadIdx.x % 4 * 4, sub = threadIdx.x / 4, valid = n - first - c;
@@ -376,8 +511,11 @@ __device__ __forceinline__ void sum_columns(const float* part, int n_parts, int3
         float v = 0;
 #pragma unroll
         for (int k = 0; k < 16; ++k) v += s2[k][col];
-        store_1(type, out, first + col, v);
+        store(first + col, v);
     }
+}
+__device__ __forceinline__ void sum_columns(const float* part, int n_parts, int32_t n, int32_t first, void* out, int type) {
+    sum_columns(part, n_parts, n, first, [=](int32_t col, float v) { store_1(type, out, col, v); });
 }
 
 }  // namespace helios

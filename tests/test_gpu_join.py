@@ -265,12 +265,13 @@ def test_join_of_one_output_and_in_place(h):
         h.join_norm(c["x"], EPS, y=c[y_in], total=c[total_in], residual=c["residual"], gain=g["gain"], **args)
         h.sync()
         assert torch.equal(c[y_in], want[0]) and torch.equal(c[total_in], want[1])
-    # without a layer's norm, dropout, gate and scale it is the norm with a residual
+    # without a layer's norm, dropout, gate and scale it is the norm with a residual (the mean by a reciprocal: 2 U, its root 1, a root to two units in the last
+    # place 4, two products 2; the other call as much: 16 U)
     y, t, y2, t2 = (torch.empty((n, d), device="cuda") for _ in range(4))
     h.join_norm(g["x"], EPS, y=y, total=t, norm_x=False, residual=g["residual"], gain=g["gain"])
     h.rms_norm(g["x"], y2, EPS, gain=g["gain"], residual=g["residual"], total=t2)
     h.sync()
-    assert torch.equal(y, y2) and torch.equal(t, t2)
+    assert bool(((y - y2).abs() <= 16 * U32 * y2.abs()).all()) and torch.equal(t, t2)
 
 
 @gpu

@@ -11,10 +11,13 @@ CLANG = "/opt/rocm/llvm/bin/clang++"
 PROGRAM = r"""
 #include <hip/hip_runtime.h>
 #include <math.h>
+#undef __builtin_amdgcn_readfirstlane
+#define __builtin_amdgcn_readfirstlane(v) on_host_readlane(v, 0)
 // what layer_dev.hpp names and the gradient does not use
 template <class... T> int on_host_none(T...) { abort(); }
 #define __builtin_amdgcn_permlane16_swap(...) (long long)(on_host_none(__VA_ARGS__))
 #define __builtin_amdgcn_permlane32_swap(...) (long long)(on_host_none(__VA_ARGS__))
+#define __builtin_amdgcn_mov_dpp(...) on_host_none(__VA_ARGS__)
 #define __builtin_amdgcn_rcpf(x) (1.0f / (x))
 #define __builtin_amdgcn_fmed3f(x, lo, hi) fminf(fmaxf(x, lo), hi)
 #define __builtin_amdgcn_cvt_pk_fp8_f32(...) on_host_none(__VA_ARGS__)
