@@ -434,12 +434,13 @@ int helios_join_norm(helios_ctx* c, const helios_join_norm_args* a) {
     if (!a->y && (a->gain || a->inv_rms)) return fail(c, HELIOS_EINVAL, "helios_join_norm: gain and inv_rms go with y");
     if ((a->y_scale != nullptr) != to_8_bits) return fail(c, HELIOS_EINVAL, "helios_join_norm: y_scale goes with an output in 8 bits, and only with it");
     const int xb = bytes_of(a->x_type), yb = bytes_of(a->y ? a->y_type : a->x_type);
+    const int64_t gate_ld = a->gate ? a->gate_ld : 0;
     const Matrix m[] = {{"x", a->x, a->n_rows, a->width, a->x_ld, xb, false},
                         {"residual", a->residual, a->n_rows, a->width, a->residual_ld, xb, false},
                         {"total", a->total, a->n_rows, a->width, a->total_ld, xb, true},
                         {"y", a->y, a->n_rows, a->width, a->y_ld, yb, true},
                         {"gain_x", a->gain_x, 1, a->width, a->width, xb, false},
-                        {"gate", a->gate, a->gate_ld ? a->n_rows : 1, a->width, a->gate_ld ? a->gate_ld : a->width, xb, false},
+                        {"gate", a->gate, gate_ld ? a->n_rows : 1, a->width, gate_ld ? gate_ld : a->width, xb, false},
                         {"gain", a->gain, 1, a->width, a->width, xb, false},
                         {"y_scale", a->y_scale, 1, a->n_rows, a->n_rows, 4, true},
                         {"inv_rms_x", a->inv_rms_x, 1, a->n_rows, a->n_rows, 4, true},
@@ -449,7 +450,7 @@ int helios_join_norm(helios_ctx* c, const helios_join_norm_args* a) {
     TRY(check(c, m, 11, twins));
     DeviceGuard guard(c->device);
     const JoinJob job{Count{a->n_rows_dev, a->n_rows}, static_cast<int32_t>(a->width), a->x_type, a->norm_x != 0, a->eps, a->residual_scale, drop, a->x, a->x_ld,
-                      a->gain_x, a->gate, a->gate_ld, a->residual, a->residual_ld, a->gain, a->total, a->total_ld, a->y, a->y_ld, a->y_scale, a->inv_rms_x, a->inv_rms};
+                      a->gain_x, a->gate, gate_ld, a->residual, a->residual_ld, a->gain, a->total, a->total_ld, a->y, a->y_ld, a->y_scale, a->inv_rms_x, a->inv_rms};
     HIP_TRY(c, launch_join(c->stream, job));
     return HELIOS_OK;
 }
@@ -467,6 +468,7 @@ int helios_join_norm_grad(helios_ctx* c, const helios_join_norm_grad_args* a) {
     if (a->n_rows > 0 && (!a->x || !a->dx || (!a->dy && !a->dtotal) || (a->dy && !a->total))) return fail(c, HELIOS_EINVAL, "helios_join_norm_grad: NULL pointer");
     if (a->n_rows > 0 && !a->dy && (a->gain || a->inv_rms || a->dgain)) return fail(c, HELIOS_EINVAL, "helios_join_norm_grad: gain, inv_rms and dgain go with dy");
     if (a->dgate && !a->gate && a->n_rows > 0) return fail(c, HELIOS_EINVAL, "helios_join_norm_grad: dgate goes with a gate");
+    const int64_t gate_ld = a->gate ? a->gate_ld : 0;
     const bool one_gate = a->gate_ld == 0;
     if (a->n_rows == 0 && !a->dgain && !a->dgain_x && !(a->dgate && one_gate)) return HELIOS_OK;
     const int xb = bytes_of(a->x_type);
@@ -480,7 +482,7 @@ int helios_join_norm_grad(helios_ctx* c, const helios_join_norm_grad_args* a) {
                         {"dgain_x", a->dgain_x, 1, a->width, a->width, xb, true},
                         {"dgain", a->dgain, 1, a->width, a->width, xb, true},
                         {"gain_x", a->gain_x, 1, a->width, a->width, xb, false},
-                        {"gate", a->gate, one_gate ? 1 : a->n_rows, a->width, one_gate ? a->width : a->gate_ld, xb, false},
+                        {"gate", a->gate, gate_ld ? a->n_rows : 1, a->width, gate_ld ? gate_ld : a->width, xb, false},
                         {"gain", a->gain, 1, a->width, a->width, xb, false},
                         {"inv_rms_x", a->inv_rms_x, 1, a->n_rows, a->n_rows, 4, false},
                         {"inv_rms", a->inv_rms, 1, a->n_rows, a->n_rows, 4, false},
@@ -489,8 +491,8 @@ int helios_join_norm_grad(helios_ctx* c, const helios_join_norm_grad_args* a) {
     TRY(check(c, m, 15, twins));
     DeviceGuard guard(c->device);
     const JoinGradJob job{Count{a->n_rows_dev, a->n_rows}, static_cast<int32_t>(a->width), a->x_type, a->norm_x != 0, a->eps, a->residual_scale, drop, a->x, a->x_ld,
-                          a->gain_x, a->gate, a->gate_ld, a->gain, a->total, a->total_ld, a->dy, a->dy_ld, a->dtotal, a->dtotal_ld, a->inv_rms_x, a->inv_rms, a->dx,
-                          a->dx_ld, a->dresidual, a->dresidual_ld, a->dgate, a->dgate_ld, a->dgain_x, a->dgain};
+                          a->gain_x, a->gate, gate_ld, a->gain, a->total, a->total_ld, a->dy, a->dy_ld, a->dtotal, a->dtotal_ld, a->inv_rms_x, a->inv_rms, a->dx,
+                          a->dx_ld, a->dresidual, a->dresidual_ld, one_gate || gate_ld ? a->dgate : nullptr, a->dgate_ld, a->dgain_x, a->dgain};
     char* at = nullptr;
     TRY(scratch(c, join_grad_scratch_bytes(job), &at));
     HIP_TRY(c, launch_join_grad(c->stream, job, at));

@@ -522,6 +522,66 @@ def test_a_capture_that_would_have_to_allocate_is_refused(helios):
 
 
 @gpu
+@pytest.mark.parametrize("d", [16, 13])
+def test_a_distance_between_rows_of_a_gate_that_is_not_there(helios, h, d):
+    """It is not looked at: the gate is ones."""
+    x, dy = _rand(8, d, 1).float().cuda(), _rand(8, d, 2).float().cuda()
+    want, got, dx, got_dx = (torch.empty_like(x) for _ in range(4))
+    h.join_norm(x, EPS, y=want)
+    h.join_norm_grad(x, dx, EPS, dtotal=dy)
+    p, q = x.data_ptr(), dy.data_ptr()
+    args = dict(n_rows=8, width=d, norm_x=1, eps=EPS, residual_scale=1.0, x=p, x_ld=d, gate_ld=d)
+    assert helios._lib.helios_join_norm(h._h, helios.JoinNormArgs(y=got.data_ptr(), y_ld=d, **args)) == helios.OK
+    assert helios._lib.helios_join_norm_grad(h._h, helios.JoinNormGradArgs(dtotal=q, dtotal_ld=d, dx=got_dx.data_ptr(), dx_ld=d, **args)) == helios.OK
+    dgate, dgain_x = (torch.full((d,), -7.0, device="cuda") for _ in range(2))
+    args = dict(args, n_rows=0, dgate=dgate.data_ptr(), dgate_ld=d, dgain_x=dgain_x.data_ptr())
+    assert helios._lib.helios_join_norm_grad(h._h, helios.JoinNormGradArgs(**args)) == helios.OK
+    h.sync()
+    assert torch.equal(got, want) and torch.equal(got_dx, dx)
+    assert bool((dgate == -7.0).all()) and bool((dgain_x == 0).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+def test_large_calls_give_the_bits_of_small_ones(h, dtype):
+    """Calls of more than 128 MB, which may go past the caches, and their first rows by themselves."""
+    d, few = 512, 100
+    n = (150 << 20) // (2 * d * torch.empty(0, dtype=dtype).element_size())
+    x, dy, dtotal, residual, gate = (torch.randn((n, d), device="cuda").to(dtype) for _ in range(5))
+    gain_x, gain, one_gate = (torch.randn(d, device="cuda").to(dtype) for _ in range(3))
+
+    def run(m, with_gates):
+        out = {k: torch.full((m, d), -7.0, dtype=dtype, device="cuda") for k in ("dropout", "total", "y", "dx", "dresidual")}
+        out["dgate"] = torch.empty((m, d) if with_gates else d, dtype=dtype, device="cuda")
+        out["dgain"] = torch.empty(d, dtype=dtype, device="cuda")
+        out["y8"], out["y_scale"] = torch.empty((m, d), dtype=E4M3, device="cuda"), torch.empty(m, device="cuda")
+        g = gate[:m] if with_gates else one_gate
+        h.dropout(x[:m], out["dropout"], 0.1, 5, 1)
+        h.join_norm(x[:m], EPS, y=out["y"], total=out["total"], gain_x=gain_x, p=0.1, seed=5, gate=g, residual=residual[:m], gain=gain)
+        h.join_norm(x[:m], EPS, y=out["y8"], y_scale=out["y_scale"], gain_x=gain_x, p=0.1, seed=5, gate=g, residual=residual[:m])
+        h.join_norm_grad(x[:m], out["dx"], EPS, total=out["total"], dy=dy[:m], dtotal=dtotal[:m], gain_x=gain_x, p=0.1, seed=5, gate=g, gain=gain,
+                         dresidual=out["dresidual"], dgate=out["dgate"], dgain=out["dgain"])
+        h.sync()
+        return out
+
+    for with_gates in (False, True):
+        large, small = run(n, with_gates), run(few, with_gates)
+        for k in ("dropout", "total", "y", "y_scale", "dx", "dresidual") + (("dgate",) if with_gates else ()):
+            assert torch.equal(large[k][:few], small[k]), k
+            assert bool(torch.isfinite(large[k]).all()), k
+        assert torch.equal(large["y8"].view(torch.uint8)[:few], small["y8"].view(torch.uint8))
+        last = {k: v[-few:].float() for k, v in large.items() if v.dim() == 2}
+        assert bool((last["dropout"] != -7.0).all()) and float((last["dropout"] == 0).float().mean()) < 0.2
+        # the last rows, and a sum over all.  (y is made from the unrounded total, whose elements and root are each off by half a step of the type.)
+        t = large["total"].double()
+        q = _root(t)
+        y = (t * q * gain.double())[-few:].cpu()
+        _close(large["y"][-few:], y, (2.1 * ROUND[dtype] + 60 * U32) * y.abs(), dtype, "y")
+        terms = dy.double() * t * q
+        _close(large["dgain"], terms.sum(0).cpu(), ((n + 108) * U32 * terms.abs().sum(0)).cpu(), dtype, "dgain")
+
+
+@gpu
 def test_refusals(helios, h):
     x, z, one = torch.zeros((8, 16), device="cuda"), torch.zeros((8, 16), device="cuda"), torch.ones(16, device="cuda")
 
