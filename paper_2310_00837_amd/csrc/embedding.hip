@@ -319,24 +319,18 @@ struct Few {
     typedef typename ElementOf<TYPE>::type T;
     typedef T vector __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     T v[V];
-    __device__ __forceinline__ void load(const T* p) {
-        if constexpr (V == 1) {
-            v[0] = *p;
-        } else {
-            const vector x = *reinterpret_cast<const vector*>(p);
+    __device__ __forceinline__ void load(const T* p) { take(*reinterpret_cast<const vector*>(p)); }
+    // hinted to leave the caches to others
+    __device__ __forceinline__ void load_once(const T* p) { take(__builtin_nontemporal_load(reinterpret_cast<const vector*>(p))); }
+    __device__ __forceinline__ void take(vector x) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = x[e];
-        }
+        for (int e = 0; e < V; ++e) v[e] = x[e];
     }
     __device__ __forceinline__ void store(T* p) const {
-        if constexpr (V == 1) {
-            *p = v[0];
-        } else {
-            vector x;
+        vector x;
 #pragma unroll
-            for (int e = 0; e < V; ++e) x[e] = v[e];
-            *reinterpret_cast<vector*>(p) = x;
-        }
+        for (int e = 0; e < V; ++e) x[e] = v[e];
+        *reinterpret_cast<vector*>(p) = x;
     }
     __device__ __forceinline__ void add(bool there, float (&to)[V]) const {
 #pragma unroll
@@ -559,7 +553,7 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(GradArgs a, const Entry* li
             for (uint32_t q = 0; q < in; q += kAhead) {
                 Few<Y, V> rows[kAhead];
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) rows[k].load(dy + lane_value(position_of(mine), min(q + k, in - 1)) * a.dy_ld);
+                for (int k = 0; k < kAhead; ++k) rows[k].load_once(dy + lane_value(position_of(mine), min(q + k, in - 1)) * a.dy_ld);
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
                     if (heads >> (q + k) & 1) {
@@ -751,13 +745,20 @@ hipError_t run_grad(hipStream_t stream, const GradPlan& plan) {
     return hipGetLastError();
 }
 
-template <int TABLE, int Y>
+template <int TABLE, int Y, int ROWS>
 void run_lookup(hipStream_t stream, const EmbeddingJob& job) {
     const int64_t items = job.rows.host * ((job.width + 7) / 8);
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>((items + kBlock * kItems - 1) / (kBlock * kItems), kMostBlocks)));
-    if (job.width % 8 == 0) hipLaunchKernelGGL((embedding_kernel<TABLE, Y, kWholeRows>), grid, dim3(kBlock), 0, stream, job);
-    else if (job.width > 8) hipLaunchKernelGGL((embedding_kernel<TABLE, Y, kRowsWithRest>), grid, dim3(kBlock), 0, stream, job);
-    else hipLaunchKernelGGL((embedding_kernel<TABLE, Y, kShortRows>), grid, dim3(kBlock), 0, stream, job);
+    hipLaunchKernelGGL((embedding_kernel<TABLE, Y, ROWS>), grid, dim3(kBlock), 0, stream, job);
+}
+template <int TABLE, int Y>
+void run_lookup(hipStream_t stream, const EmbeddingJob& job) {
+    const int64_t met = std::min(job.rows.host, job.n_table);            // rows of the table, at most
+    const Rows rows = rows_of(job.width, job.width * (met * type_bytes(TABLE) + job.rows.host * type_bytes(Y) * (job.add ? 2 : 1)));
+    if (rows == kWholeRows) run_lookup<TABLE, Y, kWholeRows>(stream, job);
+    else if (rows == kStreamedRows) run_lookup<TABLE, Y, kStreamedRows>(stream, job);
+    else if (rows == kRowsWithRest) run_lookup<TABLE, Y, kRowsWithRest>(stream, job);
+    else run_lookup<TABLE, Y, kShortRows>(stream, job);
 }
 
 }  // namespace

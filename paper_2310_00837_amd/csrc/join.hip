@@ -57,7 +57,7 @@ struct JoinShape {                                  // up to a wave several rows
 template <int TYPE, int LANES, int CHUNKS, int ROWS, bool GATES>
 __global__ __launch_bounds__(JoinShape<LANES>::kThreads) void join_kernel(JoinJob p) {
     constexpr int kThreads = JoinShape<LANES>::kThreads, kRows = JoinShape<LANES>::kRows;
-    const bool gates = GATES || (ROWS != kWholeRows && p.gate_ld != 0);
+    const bool gates = GATES || ((ROWS == kRowsWithRest || ROWS == kShortRows) && p.gate_ld != 0);
     constexpr bool kKeep = LANES * CHUNKS <= 1024;      // registers for the next row and what is the same for all (1024 threads with more have none)
     __shared__ float s[kThreads / kWave];
     __shared__ float s_sums[2][1][RowSums<LANES, 1>::kWaves];
@@ -221,18 +221,28 @@ struct RunJoin {
 };
 template <int TYPE>
 hipError_t run_join(const RunJoin& run) {
-    if (run.job.width < 8) return run.go<TYPE, 16, 1, kShortRows, false>();
-    if (run.job.width % 8 != 0) return by_width<TYPE, kRowsWithRest, false>(run.job.width, run);
-    return run.job.gate_ld ? by_width<TYPE, kWholeRows, true>(run.job.width, run) : by_width<TYPE, kWholeRows, false>(run.job.width, run);
+    const JoinJob& job = run.job;
+    const int arrays = 1 + (job.residual != nullptr) + (job.gate_ld != 0) + (job.total != nullptr) + (job.y && !job.y_scale);
+    const Rows rows = rows_of(job.width, job.rows.host * job.width * (arrays * type_bytes(TYPE) + (job.y_scale != nullptr)));
+    if (rows == kShortRows) return run.go<TYPE, 16, 1, kShortRows, false>();
+    if (rows == kRowsWithRest) return by_width<TYPE, kRowsWithRest, false>(job.width, run);
+    if (rows == kStreamedRows) return job.gate_ld ? by_width<TYPE, kStreamedRows, true>(job.width, run) : by_width<TYPE, kStreamedRows, false>(job.width, run);
+    return job.gate_ld ? by_width<TYPE, kWholeRows, true>(job.width, run) : by_width<TYPE, kWholeRows, false>(job.width, run);
 }
 
-template <int TYPE>
+template <int TYPE, int ROWS>
 void run_dropout(hipStream_t stream, const DropoutJob& job) {
     const int64_t items = job.rows.host * ((job.width + 7) / 8);
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>((items + kBlock * kItems - 1) / (kBlock * kItems), kMostBlocks)));
-    if (job.width % 8 == 0) hipLaunchKernelGGL((dropout_kernel<TYPE, kWholeRows>), grid, dim3(kBlock), 0, stream, job);
-    else if (job.width > 8) hipLaunchKernelGGL((dropout_kernel<TYPE, kRowsWithRest>), grid, dim3(kBlock), 0, stream, job);
-    else hipLaunchKernelGGL((dropout_kernel<TYPE, kShortRows>), grid, dim3(kBlock), 0, stream, job);
+    hipLaunchKernelGGL((dropout_kernel<TYPE, ROWS>), grid, dim3(kBlock), 0, stream, job);
+}
+template <int TYPE>
+void run_dropout(hipStream_t stream, const DropoutJob& job) {
+    const Rows rows = rows_of(job.width, job.rows.host * job.width * 2 * type_bytes(TYPE));
+    if (rows == kWholeRows) run_dropout<TYPE, kWholeRows>(stream, job);
+    else if (rows == kStreamedRows) run_dropout<TYPE, kStreamedRows>(stream, job);
+    else if (rows == kRowsWithRest) run_dropout<TYPE, kRowsWithRest>(stream, job);
+    else run_dropout<TYPE, kShortRows>(stream, job);
 }
 
 }  // namespace

@@ -359,7 +359,12 @@ struct RunGrad {
     }
     template <int TYPE>
     hipError_t all() const {
-        const hipError_t e = job.width < 8 ? go<TYPE, 16, kShortRows, kWithAny>() : job.width % 8 ? with<TYPE, kRowsWithRest>() : with<TYPE, kWholeRows>();
+        const int arrays = 2 + 2 * (job.dy != nullptr) + (job.dtotal != nullptr) + (job.gate_ld != 0) + (job.dgate && job.gate_ld) + (job.dresidual != nullptr);
+        const Rows rows = rows_of(job.width, job.rows.host * job.width * arrays * type_bytes(TYPE));
+        const hipError_t e = rows == kShortRows ? go<TYPE, 16, kShortRows, kWithAny>()
+                           : rows == kRowsWithRest ? with<TYPE, kRowsWithRest>()
+                           : rows == kStreamedRows ? with<TYPE, kStreamedRows>()
+                           : with<TYPE, kWholeRows>();
         if (e != hipSuccess || places.n == 0) return e;
         const dim3 grid(static_cast<unsigned>((job.width + kSumColumns - 1) / kSumColumns), static_cast<unsigned>(places.n));
         hipLaunchKernelGGL(join_sum_kernel<TYPE>, grid, dim3(kBlock), 0, stream, job, places, part, static_cast<int>(blocks_of(job)));

@@ -93,6 +93,18 @@ def test_lookup_of_rows_that_are_not_finite(h):
     assert bool((y[0] == 0).all()) and bool((y[1] == 0.5).all()) and bool(torch.isnan(y[2]).all()) and bool(torch.isinf(y[3]).all())
 
 
+@pytest.mark.parametrize("types", TYPES, ids=str)
+def test_a_large_lookup(h, types):
+    """One of more than 128 MB, which may go past the caches."""
+    n, n_table, d = 120_000, 40_000, 256
+    table, add, ids = torch.randn((n_table, d), device="cuda").to(types[0]), torch.randn((n, d), device="cuda").to(types[1]), _ids(n, n_table, 1.0, 0.1, 5).cuda()
+    y = torch.full((n, d), -7.0, dtype=types[1], device="cuda")
+    h.embedding(table, ids, y, add=add)
+    h.sync()
+    want = torch.where((ids >= 0)[:, None], table[ids.clamp_min(0).long()].float() + add.float(), add.float())
+    assert torch.equal(y, want.to(types[1]))
+
+
 def test_rows_beyond_32_bits(h):
     """A table of 5 000 000 x 1024 in half precision (elements and bytes past 2^32), few rows of which are looked up and get a gradient."""
     n_table, d = 5_000_000, 1024
