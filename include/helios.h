@@ -730,10 +730,11 @@ int helios_embedding(helios_ctx *ctx, const helios_embedding_args *args);
  *    behind the last one that is written stays as it was.
  * dtable and drow are of table_type, dy [n_rows x width] of y_type (types as in
  * helios_embedding).  Positions with -1 count for nothing, with any other ID
- * outside [0, n_table) neither, and are reported.  The sums are taken in the order
- * of the sorted list, which keeps the positions of an ID in theirs.  add's
- * gradient is dy itself.  Needs scratch: 16 bytes for a row of dy, and 8 (width + 1)
- * for every 16 of them, at most 8192 times that, and 1 MB. */
+ * outside [0, n_table) neither, and are reported.  The order in which an ID's rows
+ * are added depends on the list and the sizes only: the same call gives the same
+ * bits.  add's gradient is dy itself.  Needs scratch for more than 4096 rows: 16
+ * bytes for each, 8 (width + 1) for every 32 of them, at most 4096 times that, and
+ * 1 MB. */
 typedef struct {
     int64_t n_rows;
     const int64_t *n_rows_dev;

@@ -2,12 +2,14 @@
 //
 //   y[i] = add[i] + scale * table[id_i];   dtable[k] = scale * sum of dy[i] over the positions i with id_i = k
 //
-// The lookup is bound by memory: every row that is met once, add and y.  The gradient sorts {ID, position} (stable, so that an ID's positions
-// keep their order), cuts the sorted list into chunks of equal length whatever the IDs, and lets a group of lanes sum a chunk, run of
-// equal IDs by run: a run that lies in one chunk is finished there, one that goes on leaves a part for every chunk it meets, and a last
-// kernel adds these.  So a list of one ID costs what a list of distinct ones does, no sum is made by atomics, and the same list gives the
-// same bits.  What bounds it is the rows of dy, read once, and in front of that the chain of short launches that sorts the list:
-// lists of up to 2048 are ranked by comparing all with all, longer ones go through a radix sort of two launches for every digit.
+// The lookup is bound by memory: every row that is met once, add and y (281 600 rows of 256, the table in single precision, add and y in half:
+// 71 us, of which 66 would do at 5.6 TB/s, what a stream of reads and writes reaches).
+// The gradient of a longer list sorts {ID, position} (stable), cuts the sorted list into chunks of equal length whatever the IDs, and lets a wave sum a
+// chunk, run of equal IDs by run: a run that lies in one chunk is finished there, one that goes on leaves a part for every chunk it meets, and a
+// last kernel adds these.  So a list of one ID costs what a list of distinct ones does, no sum is made by atomics, and the same list gives
+// the same bits.  What bounds it is the rows of dy, read once, and in front of that the chain of short launches that sorts the list, two for every
+// digit: 281 600 rows of 128 in single precision, IDs below two million, are 104 us, 50 for the rows, 4 for the parts, and 46 for the list.
+// Lists of up to 4096 are not sorted (few_kernel).
 #include "layer.hpp"
 #include "layer_dev.hpp"
 
@@ -72,7 +74,7 @@ typedef unsigned long long Entry;
 __device__ __forceinline__ uint32_t id_of(Entry e) { return static_cast<uint32_t>(e >> 32); }
 __device__ __forceinline__ uint32_t position_of(Entry e) { return static_cast<uint32_t>(e); }
 
-constexpr int kFew = 2048;                          // lists that are not sorted (few_kernel)
+constexpr int kFew = 4096;                          // the longest list that is not sorted (few_kernel)
 constexpr int kSortBlock = 512, kSortItems = 4, kSortTile = kSortBlock * kSortItems, kSortWaves = kSortBlock / kWave;
 constexpr int kMostDigitBits = 9, kMostBins = 1 << kMostDigitBits, kLeastDigitBits = 4;
 constexpr int kMostGroups = 256;                    // of consecutive tiles, a workgroup each
@@ -185,6 +187,8 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* s_wave, uin
 
 // Puts a group's entries where they belong.  Every workgroup adds up the groups' counts itself: all of them for where a digit begins, those of
 // the groups before for where its own entries of it go.  The entries of a tile are ranked among each other while the counts are on their way.
+// A chain of loads, 9 us for 281 600 entries and digits of 7 bits: with digits of 10 or 11 bits, for a pass less, the whole gradient took twice as long;
+// with at most 8, for which the 349 IDs of the other case take two passes, 44 us in place of 40.
 __global__ __launch_bounds__(kSortBlock) void place_kernel(GradArgs a, Digit d) {
     __shared__ uint32_t s_next[kMostBins];          // entries of the digit in the groups before; then where the next one of it goes
     __shared__ uint32_t s_total[kMostBins];
@@ -302,7 +306,7 @@ __global__ __launch_bounds__(kSortBlock) void heads_kernel(GradArgs a, const Ent
 
 // Where a row's elements are, V neighbouring ones to a lane of a wave (the fewest that reach over the row, at most 16 bytes), in blocks of 64 V columns.
 // A lane whose columns would reach beyond the last takes the last V, and so reads, adds and writes what another does, too: no load depends on a
-// branch, and so none waits for the one before it (with a branch around each: 281 600 rows of 128 in single precision 81 us).
+// branch, and so none waits for the one before it (sum_kernel on 281 600 rows of 128 in single precision: 50 us, with a branch around each 81).
 template <int V>
 struct LaneColumns {
     uint32_t at;                                    // the first of them
@@ -349,57 +353,68 @@ __device__ __forceinline__ void store_scaled(void* base, int64_t at, const float
 
 // ---- short lists
 
-// The distinct IDs of a short list, in LDS: where an ID is first.
+// The distinct IDs of a short list, in LDS.  A slot of the table holds a position, which stands for its ID; in the end the ID's first one.
 struct FewLds {
     uint32_t key[kFew];
-    uint32_t slot_key[2 * kFew], slot_first[2 * kFew];
+    uint32_t slot[2 * kFew];                        // twice as many as there are entries, so that a search ends soon, and ends
     unsigned long long heads[kFew / kWave];         // a bit for every position: the first one of an ID that has a row
 };
-constexpr uint32_t kNoKey = ~0u;
-__device__ __forceinline__ uint32_t few_slot(uint32_t key) { return key * 0x9e3779b1u >> 20; }
-static_assert(2 * kFew == 1 << 12, "few_slot has twelve bits");
-__device__ __forceinline__ void find_distinct(const GradArgs& a, uint32_t n, FewLds& s) {
+constexpr uint32_t kNone = ~0u;
+struct Slots {
+    uint32_t bits;
+    __device__ __forceinline__ explicit Slots(uint32_t n) : bits(n > kWave ? 33 - static_cast<uint32_t>(__builtin_clz(n - 1)) : 7) {}
+    __device__ __forceinline__ uint32_t count() const { return 1u << bits; }
+    __device__ __forceinline__ uint32_t first(uint32_t key) const { return key * 0x9e3779b1u >> (32 - bits); }
+    __device__ __forceinline__ uint32_t next(uint32_t slot) const { return (slot + 1) & (count() - 1); }
+};
+__device__ __forceinline__ void find_distinct(const GradArgs& a, uint32_t n, const Slots& slots, FewLds& s) {
     constexpr int kMine = kFew / kSortBlock;
     uint32_t slot[kMine];
-    for (uint32_t i = threadIdx.x; i < 2 * kFew; i += kSortBlock) s.slot_key[i] = s.slot_first[i] = kNoKey;
+    for (uint32_t i = threadIdx.x; i < slots.count(); i += kSortBlock) s.slot[i] = kNone;
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
         const uint32_t i = k * kSortBlock + threadIdx.x;
+        if (k * kSortBlock >= n) break;
         s.key[i] = i < n ? key_of(a, i) : a.n_table;
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
+        if (k * kSortBlock >= n) break;
         const uint32_t i = k * kSortBlock + threadIdx.x, key = s.key[i];
-        slot[k] = few_slot(key);
+        slot[k] = slots.first(key);
         if (key >= a.n_table) continue;
-        for (;;) {                                  // (at most half of the slots are ever taken)
-            const uint32_t there = atomicCAS(s.slot_key + slot[k], kNoKey, key);
-            if (there == kNoKey || there == key) break;
-            slot[k] = (slot[k] + 1) % (2 * kFew);
+        for (;;) {
+            const uint32_t there = atomicCAS(s.slot + slot[k], kNone, i);
+            if (there == kNone) break;
+            if (s.key[there] == key) {
+                atomicMin(s.slot + slot[k], i);
+                break;
+            }
+            slot[k] = slots.next(slot[k]);
         }
-        atomicMin(s.slot_first + slot[k], i);
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
+        if (k * kSortBlock >= n) break;
         const uint32_t i = k * kSortBlock + threadIdx.x;
-        const unsigned long long heads = __ballot(s.key[i] < a.n_table && s.slot_first[slot[k]] == i);
+        const unsigned long long heads = __ballot(s.key[i] < a.n_table && s.slot[slot[k]] == i);
         if (lane_id() == 0) s.heads[i / kWave] = heads;
     }
     __syncthreads();
 }
-__device__ __forceinline__ bool is_met(const FewLds& s, uint32_t key) {
-    for (uint32_t slot = few_slot(key);; slot = (slot + 1) % (2 * kFew)) {
-        if (s.slot_key[slot] == key) return true;
-        if (s.slot_key[slot] == kNoKey) return false;
-    }
+__device__ __forceinline__ bool is_met(const FewLds& s, const Slots& slots, uint32_t key) {
+    for (uint32_t at = slots.first(key); s.slot[at] != kNone; at = slots.next(at))
+        if (s.key[s.slot[at]] == key) return true;
+    return false;
 }
 
 // A list of up to kFew IDs in one launch and without a sort: every workgroup finds the distinct IDs for itself; a wave has a position, and if
 // that is its ID's first one, looks through the whole list for the ID's other positions and for how many distinct IDs are less, which
 // is the row's number.  An ID with more than kLongRun positions is left to all waves of its workgroup.  Rows of dtable that are not met are cleared by
-// workgroups of their own.
+// workgroups of their own.  What bounds it is the chain of steps in LDS: 777 rows of 200 take 7 us, 2600 of 128 17 (sorted: 38), 4000 28 (39); at 6000,
+// for which LDS has room for one workgroup on a CU, 87 and 40, so that kFew is 4096.
 constexpr int kLongRun = 64, kRowsAhead = 8;
 template <int TYPE, int Y, int V>
 __global__ __launch_bounds__(kSortBlock) void few_kernel(GradArgs a, uint32_t sum_blocks) {
@@ -410,7 +425,8 @@ __global__ __launch_bounds__(kSortBlock) void few_kernel(GradArgs a, uint32_t su
     __shared__ uint32_t s_row[kSortWaves];
     __shared__ float s_part[kSortWaves][V][kWave];
     const uint32_t n = static_cast<uint32_t>(a.rows.get());
-    find_distinct(a, n, s);
+    const Slots slots(n);
+    find_distinct(a, n, slots, s);
     if (blockIdx.x >= sum_blocks) {
         const uint32_t blocks = static_cast<uint32_t>(a.width + 7) / 8;
         const int64_t items = static_cast<int64_t>(a.n_table) * blocks;
@@ -420,7 +436,7 @@ __global__ __launch_bounds__(kSortBlock) void few_kernel(GradArgs a, uint32_t su
             uint32_t down;
             int32_t col;
             places.get(threadIdx.x, &down, &col);
-            if (base + threadIdx.x < items && !is_met(s, static_cast<uint32_t>(places.row0 + down)))
+            if (base + threadIdx.x < items && !is_met(s, slots, static_cast<uint32_t>(places.row0 + down)))
                 store_8_of<TYPE>(a.out, places.row(a.out_ld, down) + col, a.width - col, zeros);
         }
         return;
@@ -440,7 +456,7 @@ __global__ __launch_bounds__(kSortBlock) void few_kernel(GradArgs a, uint32_t su
     const auto to_row = [&](uint32_t row) {
         if (columns.any) store_scaled<TYPE, V>(a.out, row * a.out_ld + columns.at, acc, a.scale);
     };
-    if (lane == 0) s_long[wave] = kNoKey;
+    if (lane == 0) s_long[wave] = kNone;
     if (mine < n && (s.heads[mine / kWave] >> (mine % kWave) & 1)) {
         const uint32_t id = s.key[mine];
         uint32_t found = 0, row = id;
@@ -471,7 +487,7 @@ __global__ __launch_bounds__(kSortBlock) void few_kernel(GradArgs a, uint32_t su
     __syncthreads();
     for (int run = 0; run < kSortWaves; ++run) {
         const uint32_t id = s_long[run];
-        if (id == kNoKey) continue;
+        if (id == kNone) continue;
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] = 0;
         for (uint32_t w = wave; w < words; w += kSortWaves) {
@@ -509,7 +525,8 @@ __global__ __launch_bounds__(kSortBlock) void few_kernel(GradArgs a, uint32_t su
 // ---- sums of the sorted list
 
 // A chunk to a wave: what it does next is the same for all lanes, so that the list, the places of rows and the branches are the scalar unit's, and
-// an entry costs a lane a load and V additions.
+// an entry costs a lane a load and V additions.  281 600 rows of 128 in single precision: 50 us, 2.9 TB/s of rows that lie anywhere; 16 or 32 lanes to
+// a chunk took 65.  100 003 rows of 256 in bfloat16, 349 IDs: 11.6 us.
 constexpr int kAhead = 16;
 template <int TYPE, int Y, int V>
 __global__ __launch_bounds__(kBlock) void sum_kernel(GradArgs a, const Entry* list, uint32_t n_tasks) {
@@ -583,7 +600,8 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(GradArgs a, const Entry* li
 }
 
 // Adds the parts of a run that begins in a chunk and goes on.  A wave has 16 V columns of a chunk, 16 lanes to a part and four parts at a time; a run
-// that goes through the next 63 chunks is left to all waves of the workgroup.
+// that goes through the next 63 chunks is left to all waves of the workgroup.  4.8 us and 14 in the two cases above, a chain of dependent loads; with a list
+// of the runs to be added, taken by a counter, it took 18.
 constexpr int kMergeLanes = 16, kMergeSubs = kWave / kMergeLanes, kMergeWaves = 8, kMergeBlock = kMergeWaves * kWave;
 template <int TYPE, int V>
 __global__ __launch_bounds__(kMergeBlock) void merge_kernel(GradArgs a, uint32_t column_blocks, uint32_t n_tasks) {
@@ -618,7 +636,7 @@ __global__ __launch_bounds__(kMergeBlock) void merge_kernel(GradArgs a, uint32_t
         const uint32_t c = chunk + lane_id();
         const int32_t info = task < n_tasks && c < n_chunks ? a.info[c] : kNothing, row = __builtin_amdgcn_readfirstlane(info);
         const uint64_t ends = ~__ballot(info == kThrough) & ~uint64_t{1};        // chunks that a run from the first one does not go through
-        if (lane_id() == 0) s_long[wave] = row >= 0 && ends == 0 ? task : kNoKey;
+        if (lane_id() == 0) s_long[wave] = row >= 0 && ends == 0 ? task : kNone;
         if (row >= 0 && ends != 0) {
             const LaneColumns<V> columns = columns_of(task);
             add_parts(chunk, sub == 0, chunk + 1 + sub, chunk + static_cast<uint32_t>(__ffsll(static_cast<long long>(ends)) - 1), kMergeSubs, columns.at);
@@ -627,7 +645,7 @@ __global__ __launch_bounds__(kMergeBlock) void merge_kernel(GradArgs a, uint32_t
         __syncthreads();
         for (int w = 0; w < kMergeWaves; ++w) {
             const uint32_t task = s_long[w], chunk = task / column_blocks;
-            if (task == kNoKey) continue;
+            if (task == kNone) continue;
             if (threadIdx.x == 0) s_last = n_chunks;
             __syncthreads();
             for (uint32_t from = chunk + kWave; from < n_chunks; from += kMergeBlock) {       // the first chunk that the run does not go through

@@ -8,7 +8,8 @@
 // A row is held in registers in 32 bits and read once; lanes go through rows and keep their sums of columns until the end; a second launch adds the
 // workgroups' sums.  What bounds it is the vector unit as much as memory: some 390 instructions for eight elements of a wave, of which the generator
 // is a quarter, so registers are kept for a second workgroup on a CU and not for the next row (asked for ahead it took 24.7 us in place of 23.4
-// for 11 264 x 256 in single precision, 73.6 in place of 70 for 6000 x 4096 in bfloat16).
+// for 11 264 x 256 in single precision, 73.6 in place of 70 for 6000 x 4096 in bfloat16).  26 624 rows of 512 in bfloat16 with a gate for all: 35 us,
+// 31 and 4 for the second launch, 4.1 TB/s; 11 264 of 256 in single precision with a gate each: 24, of which 18 and 4.
 #include "drop_dev.hpp"
 
 #include <algorithm>
@@ -65,7 +66,7 @@ struct GradShape {
 };
 // A lane beyond the last chunk loads what is there, too, and adds nothing to the sums over a row.
 // WITH: what there is, where that is known: branches for it cost copies of what is loaded, and registers for a gate's rows that there are none of
-// (26 624 x 512 in bfloat16: 43 us with them, 35 without).
+// (26 624 x 512 in bfloat16, without the second launch: 43 us with them, 35 without, before its rows were streamed).
 enum With { kWithAny = 0, kWithOneGate = 1, kWithGates = 2 };       // any; dy, dtotal, and a gate of one row or none; dy, dtotal and a gate for every row
 template <int TYPE, int LANES, int ROWS, int WITH>
 __global__ __launch_bounds__(GradShape<LANES>::kThreads) void join_grad_kernel(JoinGradJob p, SumPlaces places, float* part) {

@@ -182,6 +182,15 @@ def test_gradient_with_the_count_on_the_device(h, n, count):
     _grad_case(h, n, 700, 40, (F32, F32), ids, 0.5, n, count=count)
 
 
+@pytest.mark.parametrize("n,count", [(4095, None), (4096, None), (4097, None), (4096, 4095), (4097, 4096), (3000, 65)])
+def test_gradient_of_the_longest_lists_that_are_not_sorted(h, n, count):
+    """Distinct IDs only; one ID only; few; a few that are met often among many."""
+    some = torch.from_numpy(np.random.default_rng(n).permutation(9000)[:n].astype(np.int32))
+    mixed = torch.where(torch.arange(n) % 3 == 0, some, some % 5)
+    for k, ids in enumerate((some, torch.full((n,), 8999, dtype=torch.int32), some % 70, mixed)):
+        _grad_case(h, n, 9000, 72, (F32, BF16), ids, 1.5, n + k, **({} if count is None else dict(count=count)))
+
+
 @pytest.mark.parametrize("d", [8, 200, 1000])
 @pytest.mark.parametrize("n", [50, 2000, 9000, 40_000])
 def test_gradient_of_long_runs(h, n, d):

@@ -137,7 +137,8 @@ def program(tmp_path_factory):
     (100, 10, 130, "few", -1), (777, 1000, 24, "skewed", -1), (1000, 12, 300, "skewed", 0), (1000, 12, 20, "skewed", 333), (2048, 2048, 8, "any", -1),
     (2048, 5, 17, "one", -1), (2048, 3000, 8, "bad", 2047), (2049, 3, 8, "few", -1), (2049, 100_000, 9, "any", 2048), (4097, 2, 12, "one", -1),
     (9000, 70_000, 5, "skewed", -1), (9000, 400, 8, "bad", -1), (12_289, 2_000_000, 2, "any", 12_288), (5000, 260, 136, "few", 1),
-    (20_000, 20, 1, "skewed", -1), (5000, 30, 4, "none", -1)])
+    (20_000, 20, 1, "skewed", -1), (5000, 30, 4, "none", -1), (4096, 9000, 4, "any", -1), (4096, 3, 4, "one", 4095),
+    (4097, 9000, 4, "any", 4096), (3000, 2, 9, "bad", -1), (100, 5, 8, "few", 0)])
 def test_gradient_of_learnt_rows(program, n, n_table, width, ids, count):
     r = subprocess.run([program, str(n), str(n_table), str(width), ids, str(count)], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0 and r.stdout == "ok\n", (r.returncode, r.stdout[-500:], r.stderr[-500:])
