@@ -20,7 +20,8 @@ constexpr int64_t kMostBlocks = 1 << 21;            // of a launch
 constexpr int kItems = 2;                           // of a thread of the dropout kernel, in flight together
 
 // An item is eight neighbouring columns of a row; items are numbered along the rows.  Bound by memory and the generator: 26 624 rows of 512 in bfloat16
-// 10.6 us (floor 8.6), 262 MB and more at 5.6 TB/s.
+// 10.6 us, 5.1 TB/s, 100 003 of 1024 in
+// half precision 64 us, 6.4 TB/s, what a large copy reaches.
 template <int TYPE, int ROWS>
 __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutJob p) {
     const uint32_t blocks = static_cast<uint32_t>(p.width + 7) / 8;

@@ -9,7 +9,7 @@
 // workgroups' sums.  What bounds it is the vector unit as much as memory: some 390 instructions for eight elements of a wave, of which the generator
 // is a quarter, so registers are kept for a second workgroup on a CU and not for the next row (asked for ahead it took 24.7 us in place of 23.4
 // for 11 264 x 256 in single precision, 73.6 in place of 70 for 6000 x 4096 in bfloat16).  26 624 rows of 512 in bfloat16 with a gate for all: 35 us,
-// 31 and 4 for the second launch, 4.1 TB/s; 11 264 of 256 in single precision with a gate each: 24, of which 18 and 4.
+// 31 and 4 for the second launch, 4.7 TB/s; 11 264 of 256 in single precision with a gate each: 24, of which 18 and 4.
 #include "drop_dev.hpp"
 
 #include <algorithm>
