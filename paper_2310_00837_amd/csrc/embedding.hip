@@ -601,11 +601,12 @@ __global__ __launch_bounds__(kBlock) void sum_kernel(GradArgs a, const Entry* li
 }
 
 // Adds the parts of a run that begins in a chunk and goes on.  A wave has 16 V columns of a chunk, 16 lanes to a part and four parts at a time; a run
-// that goes through the next 63 chunks is left to all waves of the workgroup.  4.8 us and 14 in the two cases above, a chain of dependent loads; with a list
-// of the runs to be added, taken by a counter, it took 18.
+// that goes through the next 63 chunks is left to all waves of the workgroup, which have neighbouring chunks and so at most one of these among them (four, with
+// the same chunk's blocks of columns beside one another, took twice as long).  4.8 us and 8 in the two cases above, a chain of dependent loads; with a
+// list of the runs to be added, taken by a counter, it took 18.
 constexpr int kMergeLanes = 16, kMergeSubs = kWave / kMergeLanes, kMergeWaves = 8, kMergeBlock = kMergeWaves * kWave;
 template <int TYPE, int V>
-__global__ __launch_bounds__(kMergeBlock) void merge_kernel(GradArgs a, uint32_t column_blocks, uint32_t n_tasks) {
+__global__ __launch_bounds__(kMergeBlock) void merge_kernel(GradArgs a, uint32_t all_chunks, uint32_t n_tasks) {
     __shared__ float s[kMergeWaves][V][kMergeLanes];
     __shared__ uint32_t s_long[kMergeWaves], s_last;
     const uint32_t n = static_cast<uint32_t>(a.rows.get()), n_chunks = (n + a.chunk - 1) / a.chunk;
@@ -631,9 +632,9 @@ __global__ __launch_bounds__(kMergeBlock) void merge_kernel(GradArgs a, uint32_t
             acc[e] += __shfl_xor(acc[e], 32, kWave);
         }
     };
-    const auto columns_of = [&](uint32_t task) { return LaneColumns<V>(lane, (task % column_blocks) * (kMergeLanes * V), a.width); };
+    const auto columns_of = [&](uint32_t task) { return LaneColumns<V>(lane, task / all_chunks * (kMergeLanes * V), a.width); };
     for (uint32_t base = blockIdx.x * kMergeWaves; base < n_tasks; base += gridDim.x * kMergeWaves) {
-        const uint32_t task = base + wave, chunk = task / column_blocks;
+        const uint32_t task = base + wave, chunk = task % all_chunks;
         const uint32_t c = chunk + lane_id();
         const int32_t info = task < n_tasks && c < n_chunks ? a.info[c] : kNothing, row = __builtin_amdgcn_readfirstlane(info);
         const uint64_t ends = ~__ballot(info == kThrough) & ~uint64_t{1};        // chunks that a run from the first one does not go through
@@ -645,7 +646,7 @@ __global__ __launch_bounds__(kMergeBlock) void merge_kernel(GradArgs a, uint32_t
         }
         __syncthreads();
         for (int w = 0; w < kMergeWaves; ++w) {
-            const uint32_t task = s_long[w], chunk = task / column_blocks;
+            const uint32_t task = s_long[w], chunk = task % all_chunks;
             if (task == kNone) continue;
             if (threadIdx.x == 0) s_last = n_chunks;
             __syncthreads();
@@ -736,7 +737,7 @@ void launch_sums(hipStream_t stream, const GradPlan& plan, const Entry* list) {
 template <int TYPE, int V>
 void launch_merge(hipStream_t stream, const GradPlan& plan) {
     const uint32_t columns = ceil_div(plan.a.width, V * kMergeLanes), tasks = plan.n_chunks * columns;
-    hipLaunchKernelGGL((merge_kernel<TYPE, V>), dim3(std::min<uint32_t>(ceil_div(tasks, kMergeWaves), kMostBlocks)), dim3(kMergeBlock), 0, stream, plan.a, columns, tasks);
+    hipLaunchKernelGGL((merge_kernel<TYPE, V>), dim3(std::min<uint32_t>(ceil_div(tasks, kMergeWaves), kMostBlocks)), dim3(kMergeBlock), 0, stream, plan.a, plan.n_chunks, tasks);
 }
 template <int TYPE, int Y>
 hipError_t run_grad(hipStream_t stream, const GradPlan& plan) {
