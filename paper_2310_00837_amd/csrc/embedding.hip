@@ -8,7 +8,7 @@
 // chunk, run of equal IDs by run: a run that lies in one chunk is finished there, one that goes on leaves a part for every chunk it meets, and a
 // last kernel adds these.  So a list of one ID costs what a list of distinct ones does, no sum is made by atomics, and the same list gives
 // the same bits.  What bounds it is the rows of dy, read once, and in front of that the chain of short launches that sorts the list, two for every
-// digit: 281 600 rows of 128 in single precision, IDs below two million, are 104 us, 50 for the rows, 4 for the parts, and 46 for the list.
+// digit: 281 600 rows of 128 in single precision, IDs below two million, are 101 us, 50 for the rows, 5 for the parts, and 46 for the list.
 // Lists of up to 4096 are not sorted (few_kernel).
 #include "layer.hpp"
 #include "layer_dev.hpp"
@@ -112,10 +112,10 @@ struct GradArgs {
 };
 constexpr int32_t kNothing = -1, kThrough = -2;     // (kThrough: all of the chunk is one run that comes from before it and goes on)
 
-__device__ __forceinline__ uint32_t key_of(const GradArgs& a, uint32_t position) {
-    const int32_t id = a.ids[position];
-    if (id >= 0 && static_cast<uint32_t>(id) < a.n_table) return static_cast<uint32_t>(id);
-    if (id != -1) raise(a.err, kErrData);
+// The ID an entry has, if it is there.
+__device__ __forceinline__ uint32_t key_of(const GradArgs& a, int32_t id, bool there) {
+    if (there && id >= 0 && static_cast<uint32_t>(id) < a.n_table) return static_cast<uint32_t>(id);
+    if (there && id != -1) raise(a.err, kErrData);
     return a.n_table;
 }
 
@@ -142,9 +142,24 @@ struct Digit {
     __device__ __forceinline__ uint32_t bins() const { return 1u << bits; }
     __device__ __forceinline__ uint32_t of(uint32_t key) const { return key >> shift & (bins() - 1); }
 };
-__device__ __forceinline__ Entry entry_at(const GradArgs& a, const Digit& d, uint32_t i) {
-    if (d.from < 0) return static_cast<Entry>(key_of(a, i)) << 32 | i;
-    return d.from == 0 ? a.list[0][i] : a.list[1][i];
+// kSortItems entries, `step` apart from `first` on; all ones where there are none.  (No load depends on a branch: what is not there reads the last entry,
+// or the first place of an empty list.)
+__device__ __forceinline__ void load_entries(const GradArgs& a, const Digit& d, uint32_t first, uint32_t step, uint32_t n, Entry (&entry)[kSortItems]) {
+    const uint32_t last = n > 0 ? n - 1 : 0;
+    if (d.from < 0) {
+        int32_t id[kSortItems];
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) id[k] = a.ids[min(first + k * step, last)];
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) entry[k] = static_cast<Entry>(key_of(a, id[k], first + k * step < n)) << 32 | (first + k * step);
+    } else {
+        const Entry* list = d.from == 0 ? a.list[0] : a.list[1];
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) entry[k] = list[min(first + k * step, last)];
+    }
+#pragma unroll
+    for (int k = 0; k < kSortItems; ++k)
+        if (first + k * step >= n) entry[k] = ~Entry{0};
 }
 
 // How many entries of every digit a group of tiles has.
@@ -160,9 +175,11 @@ __global__ __launch_bounds__(kSortBlock) void count_kernel(GradArgs a, Digit d) 
     __syncthreads();
     for (uint32_t tile = 0; tile < a.group_tiles; ++tile) {
         const uint32_t first = (blockIdx.x * a.group_tiles + tile) * kSortTile + threadIdx.x;
+        Entry entry[kSortItems];
+        load_entries(a, d, first, kSortBlock, n, entry);
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k)
-            if (first + k * kSortBlock < n) atomicAdd(s_count + d.of(id_of(entry_at(a, d, first + k * kSortBlock))), 1u);
+            if (first + k * kSortBlock < n) atomicAdd(s_count + d.of(id_of(entry[k])), 1u);
     }
     __syncthreads();
     for (uint32_t b = threadIdx.x; b < d.bins(); b += kSortBlock) a.counts[blockIdx.x * d.bins() + b] = s_count[b];
@@ -187,8 +204,9 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* s_wave, uin
 
 // Puts a group's entries where they belong.  Every workgroup adds up the groups' counts itself: all of them for where a digit begins, those of
 // the groups before for where its own entries of it go.  The entries of a tile are ranked among each other while the counts are on their way.
-// A chain of loads, 9 us for 281 600 entries and digits of 7 bits: with digits of 10 or 11 bits, for a pass less, the whole gradient took twice as long;
+// A chain of loads, 7.5 us for 281 600 entries and digits of 7 bits (9 with loads of entries and counts behind branches): with digits of 10 or 11 bits, for a pass less, the whole gradient took twice as long;
 // with at most 8, for which the 349 IDs of the other case take two passes, 44 us in place of 40.
+constexpr int kCountsAhead = 8;
 __global__ __launch_bounds__(kSortBlock) void place_kernel(GradArgs a, Digit d) {
     __shared__ uint32_t s_next[kMostBins];          // entries of the digit in the groups before; then where the next one of it goes
     __shared__ uint32_t s_total[kMostBins];
@@ -199,21 +217,20 @@ __global__ __launch_bounds__(kSortBlock) void place_kernel(GradArgs a, Digit d) 
     // a wave has kSortItems times 64 neighbouring entries of a tile
     const uint32_t first = blockIdx.x * a.group_tiles * kSortTile + wave * (kSortItems * kWave) + lane;
     Entry entry[kSortItems];
-    const auto load = [&](uint32_t tile) {
-#pragma unroll
-        for (int k = 0; k < kSortItems; ++k) {
-            const uint32_t i = first + tile * kSortTile + k * kWave;
-            entry[k] = i < n ? entry_at(a, d, i) : ~Entry{0};
-        }
-    };
+    const auto load = [&](uint32_t tile) { load_entries(a, d, first + tile * kSortTile, kWave, n, entry); };
     load(0);
     const uint32_t quads = bins / 4, shares = kSortBlock / quads, quad = t % quads, share = t / quads;
     words4 total = {0, 0, 0, 0}, before = {0, 0, 0, 0};
-#pragma unroll 8
-    for (uint32_t g = share; g < a.n_groups; g += shares) {
-        const words4 c = reinterpret_cast<const words4*>(a.counts + g * bins)[quad];
-        total += c;
-        if (g < blockIdx.x) before += c;
+    for (uint32_t from = share; from < a.n_groups; from += kCountsAhead * shares) {
+        words4 c[kCountsAhead];
+#pragma unroll
+        for (int k = 0; k < kCountsAhead; ++k) c[k] = reinterpret_cast<const words4*>(a.counts + min(from + k * shares, a.n_groups - 1) * bins)[quad];
+#pragma unroll
+        for (int k = 0; k < kCountsAhead; ++k) {
+            const uint32_t g = from + k * shares;
+            if (g < a.n_groups) total += c[k];
+            if (g < blockIdx.x) before += c[k];
+        }
     }
     for (uint32_t b = t; b < bins; b += kSortBlock) s_next[b] = s_total[b] = 0;
     for (uint32_t tile = 0; tile < a.group_tiles; ++tile) {
@@ -259,12 +276,13 @@ __global__ __launch_bounds__(kSortBlock) void place_kernel(GradArgs a, Digit d) 
             }
         }
         for (uint32_t b = t; b < bins; b += kSortBlock) {
-            uint32_t to = s_next[b];
+            uint32_t to = s_next[b], c[kSortWaves];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) c[w] = s_count[w * bins + b];
 #pragma unroll
             for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t c = s_count[w * bins + b];
                 s_count[w * bins + b] = to;
-                to += c;
+                to += c[w];
             }
             s_next[b] = to;
         }
@@ -281,13 +299,12 @@ __global__ __launch_bounds__(kSortBlock) void place_kernel(GradArgs a, Digit d) 
 
 // The heads of runs among the eight entries from `at` on (those of IDs that have a row).
 __device__ __forceinline__ uint32_t heads_of_8(const Entry* list, uint32_t at, uint32_t n, uint32_t n_table) {
-    uint32_t heads = 0, before = at > 0 && at < n ? id_of(list[at - 1]) : ~0u;
+    const uint32_t last = n > 0 ? n - 1 : 0;
+    uint32_t heads = 0, id[9];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t id = at + e < n ? id_of(list[at + e]) : n_table;
-        heads += id < n_table && id != before ? 1u : 0u;
-        before = id;
-    }
+    for (int e = 0; e < 9; ++e) id[e] = id_of(list[min(at + e > 0 ? at + e - 1 : 0, last)]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) heads += at + e < n && id[e + 1] < n_table && (at + e == 0 || id[e] != id[e + 1]) ? 1u : 0u;
     return heads;
 }
 __global__ __launch_bounds__(kSortBlock) void heads_kernel(GradArgs a, const Entry* list) {
@@ -370,12 +387,18 @@ struct Slots {
 __device__ __forceinline__ void find_distinct(const GradArgs& a, uint32_t n, const Slots& slots, FewLds& s) {
     constexpr int kMine = kFew / kSortBlock;
     uint32_t slot[kMine];
+    int32_t id[kMine];
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+        if (k * kSortBlock >= n) break;
+        id[k] = a.ids[min(k * kSortBlock + threadIdx.x, n - 1)];
+    }
     for (uint32_t i = threadIdx.x; i < slots.count(); i += kSortBlock) s.slot[i] = kNone;
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
         const uint32_t i = k * kSortBlock + threadIdx.x;
         if (k * kSortBlock >= n) break;
-        s.key[i] = i < n ? key_of(a, i) : a.n_table;
+        s.key[i] = key_of(a, id[k], i < n);
     }
     __syncthreads();
 #pragma unroll
