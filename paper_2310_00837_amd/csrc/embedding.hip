@@ -98,7 +98,7 @@ struct GradArgs {
     // how the list is cut
     bool few;                                       // it is not sorted at all (few_kernel)
     uint32_t n_groups, group_tiles;                 // of the sort
-    uint32_t chunk;                                 // entries of a chunk: a power of two, 16 or more
+    uint32_t chunk;                                 // entries of a chunk: a power of two, 32 or more
     uint32_t head_span;                             // entries that a workgroup of heads_kernel counts
     uint32_t column_blocks;                         // of sum_kernel
     uint32_t fill_blocks;                           // workgroups of the first launch that clear dtable

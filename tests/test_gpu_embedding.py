@@ -390,6 +390,46 @@ def test_a_capture_that_would_have_to_allocate_is_refused(helios):
         h.close()
 
 
+def test_two_contexts_at_once(helios):
+    """Long lists and a join's gradient on two streams, call by call in turn: scratch is a context's own."""
+    n, n_table, d = 30_000, 500, 64
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    contexts = [helios.Helios(0, stream=s) for s in streams]
+    try:
+        cases = []
+        for k in range(2):
+            ids, dy = _ids(n, n_table, 2, 0.1, 70 + k).cuda(), torch.randn((n, d), device="cuda")
+            cases.append(dict(ids=ids, dy=dy, dtable=torch.empty((n_table, d), device="cuda"), dx=torch.empty_like(dy), dgain_x=torch.empty(d, device="cuda"),
+                              x=torch.randn((n, d), device="cuda")))
+        torch.cuda.synchronize()
+
+        def call(h, c):
+            h.embedding_grad(c["ids"], c["dy"], n_table, dtable=c["dtable"])
+            h.join_norm_grad(c["x"], c["dx"], EPS, dtotal=c["dy"], p=0.3, seed=9, dgain_x=c["dgain_x"])
+
+        want = []
+        for h, c in zip(contexts, cases):
+            call(h, c)
+            h.sync()
+            want.append([c[k].clone() for k in ("dtable", "dx", "dgain_x")])
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for c in cases:
+                for k in ("dtable", "dx", "dgain_x"):
+                    c[k].fill_(-7.0)
+            torch.cuda.synchronize()
+            for _ in range(3):
+                for h, c in zip(contexts, cases):
+                    call(h, c)
+            for h in contexts:
+                h.sync()
+            for c, w in zip(cases, want):
+                assert all(torch.equal(c[k], v) for k, v in zip(("dtable", "dx", "dgain_x"), w))
+    finally:
+        for h in contexts:
+            h.close()
+
+
 # ------------------------------------------------------------------ together
 
 
