@@ -792,8 +792,8 @@ int helios_dropout(helios_ctx *ctx, const helios_dropout_args *args);
  *     total = residual_scale * residual + gate * drop(u)
  *     y     = total * gain / sqrt(mean(total^2) + eps)
  * x, residual, total [n_rows x width], gain_x, gain [width] and gate are of x_type;
- * gate [n_rows x width], or with gate_ld 0 one row for all (not looked at where
- * there is no gate, nor in the gradient).  y is of y_type =
+ * gate [n_rows x width], or with gate_ld 0 one row for all (gate_ld is not looked
+ * at where gate is NULL).  y is of y_type =
  * x_type, or HELIOS_E4M3 with y_scale [n_rows] as in helios_rms_norm.  gain_x and
  * gain (ones), gate (ones), residual (zeros), inv_rms_x and inv_rms (float
  * [n_rows]: 1 / sqrt(mean + eps), for the gradient) are nullable, and one of
