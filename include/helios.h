@@ -797,8 +797,11 @@ int helios_dropout(helios_ctx *ctx, const helios_dropout_args *args);
  * x_type, or HELIOS_E4M3 with y_scale [n_rows] as in helios_rms_norm.  gain_x and
  * gain (ones), gate (ones), residual (zeros), inv_rms_x and inv_rms (float
  * [n_rows]: 1 / sqrt(mean + eps), for the gradient) are nullable, and one of
- * total and y is.  Everything is made from unrounded values.  total and y (if of
- * x_type) may each be the matrix of x or of residual, but not both the same. */
+ * total and y is.  Everything is made from unrounded values (gain_x and a gate of
+ * one row are multiplied with each other first).  drop(u) is 0 where elements are
+ * dropped, whatever u is there; a gate that is not finite makes NaN of it.  total
+ * and y (if of x_type) may each be the matrix of x or of residual, but not both
+ * the same. */
 typedef struct {
     int64_t n_rows;
     const int64_t *n_rows_dev;
@@ -832,6 +835,9 @@ int helios_join_norm(helios_ctx *ctx, const helios_join_norm_args *args);
  *     w         = drop(dt) * gate
  *     dx        = qx (w gain_x - x qx^2 mean(w gain_x x))        (norm_x 0: dx = w)
  *     dgain_x   = the sum over the rows of w x qx,  dgain = that of dy total q
+ * An element that is dropped has w = 0 and adds 0 to dgate and dgain_x, whatever
+ * dt, x and gate hold there.  What is the same for all rows (gain_x; gate, with
+ * gate_ld 0) is multiplied into a sum over the rows when that is complete.
  * dy is the gradient of y (NULL: y was not used; total, gain and dgain are not
  * either), dtotal that which reaches total by other ways; one of them is nullable.
  * dgate [n_rows x width], or with gate_ld 0 [width] (dgate_ld is not read).  gain_x,

@@ -95,7 +95,13 @@ __global__ __launch_bounds__(JoinShape<LANES>::kThreads) void join_kernel(JoinJo
     // gain_x times a gate of one row times the scale of what is kept; and gain
     constexpr int kKept = kKeep ? CHUNKS : 1;
     float front[kKept][8], gain[kKept][8];
-    const auto load_front = [&](int c, float (&v)[8]) {
+    // 0 times that gate, NaN where it is not finite: what becomes of a dropped element.  (Eight registers that cost no call time; a branch for such gates
+    // took the scalar unit's: 100 003 rows of 3 in single precision 22.7 us in place of 20.3.)
+    float nothing[kKept][8];
+    const auto load_front = [&](int c, int kept) {
+        float(&v)[8] = front[kept];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) nothing[kept][e] = 0;
         Raw8<TYPE> raw;
         float f[8];
 #pragma unroll
@@ -110,7 +116,10 @@ __global__ __launch_bounds__(JoinShape<LANES>::kThreads) void join_kernel(JoinJo
             load(raw, p.gate, 0, c);
             widen(raw, c, f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= f[e];
+            for (int e = 0; e < 8; ++e) {
+                v[e] *= f[e];
+                nothing[kept][e] = 0.0f * f[e];
+            }
         }
     };
     const auto load_gain = [&](int c, float (&v)[8]) {
@@ -128,7 +137,7 @@ __global__ __launch_bounds__(JoinShape<LANES>::kThreads) void join_kernel(JoinJo
     if (kKeep)
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            load_front(c, front[c % kKept]);
+            load_front(c, c % kKept);
             load_gain(c, gain[c % kKept]);
         }
     for (; first < count; first += stride) {
@@ -161,14 +170,14 @@ __global__ __launch_bounds__(JoinShape<LANES>::kThreads) void join_kernel(JoinJo
             const int col = (c * LANES + lane) * 8;
             const Kept8 kept = kept_8(p.drop, seed, row, col);
             if (!kKeep) {
-                load_front(c, front[0]);
+                load_front(c, 0);
                 if (p.residual) widen(r_raw[c], c, r[c]);
                 if (gates) widen(g_raw[c], c, g[c]);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float v = t[c][e] * q * front[c % kKept][e];
-                v = kept.on[e] ? v : 0.0f;          // (what is dropped becomes 0 whatever it was)
+                v = kept.on[e] ? v : GATES ? 0.0f : nothing[c % kKept][e];          // (what is dropped becomes 0 whatever it was)
                 if (gates) v *= g[c][e];
                 if (p.residual) v += p.residual_scale * r[c][e];
                 t[c][e] = col < p.width ? v : 0.0f;

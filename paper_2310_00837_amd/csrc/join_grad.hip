@@ -4,6 +4,7 @@
 //   dt = dtotal + q (a - total q^2 mean(a total));  dresidual = r dt;  dgate = s k dt x qx gain_x;  w = s k dt gate
 //   dx = qx (w gain_x - x qx^2 mean(w gain_x x));  dgain_x = sum over rows of w x qx;  dgain = sum of dy total q
 //
+// (k = 0 selects: an element that is dropped adds 0 to these whatever is multiplied there.)
 // With a gate of one row, dgate and dgain_x are one sum, S = sum over rows of k dt x qx: dgate = s gain_x S, dgain_x = s gate S.
 // A row is held in registers in 32 bits and read once; lanes go through rows and keep their sums of columns until the end; a second launch adds the
 // workgroups' sums.  What bounds it is the vector unit as much as memory: some 390 instructions for eight elements of a wave, of which the generator
@@ -41,7 +42,6 @@ struct RowFactors {
 // What becomes of eight elements before the sum over the row that dx needs.
 struct GradOf8 {
     float dt[8];
-    float kept_x[8];                              // k dt x
     float w[8];                                   // w gain_x
 };
 // front: gain_x times s times the gate
@@ -51,7 +51,6 @@ __device__ __forceinline__ GradOf8 grad_of_8(const RowFactors& r, const Kept8& k
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         o.dt[e] = __builtin_fmaf(r.q, __builtin_fmaf(-t[e], r.f, dy[e] * gain[e]), dtotal[e]);
-        o.kept_x[e] = kept.on[e] ? o.dt[e] * x[e] : 0.0f;
         o.w[e] = kept.on[e] ? o.dt[e] * front[e] : 0.0f;
     }
     return o;
@@ -148,11 +147,13 @@ __global__ __launch_bounds__(GradShape<LANES>::kThreads) void join_grad_kernel(J
         const GradOf8 o = grad_of_8(f, kept, t, d, r, x, gain, whole_front);
         float v1[1] = {0};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v1[0] += o.w[e] * x[e];
-            sum_gain[e] += there ? d[e] * t[e] * f.q : 0.0f;
-            sum_s[e] += there ? o.kept_x[e] * (gates ? g[e] * f.qx : f.qx) : 0.0f;
-        }
+        for (int e = 0; e < 8; ++e) v1[0] += o.w[e] * x[e];
+        if (there)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                sum_gain[e] += d[e] * t[e] * f.q;
+                sum_s[e] += kept.on[e] ? o.dt[e] * x[e] * (gates ? g[e] * f.qx : f.qx) : 0.0f;
+            }
         if (p.dresidual && there) {
             float v[8];
 #pragma unroll
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(GradShape<LANES>::kThreads) void join_grad_kernel(J
         if (p.dgate && gates && there) {
             float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = o.kept_x[e] * (f.qx * front[e]);
+            for (int e = 0; e < 8; ++e) v[e] = kept.on[e] ? o.dt[e] * x[e] * (f.qx * front[e]) : 0.0f;
             store_row_8<TYPE, ROWS>(p.dgate, row * p.dgate_ld, col, p.width, v);
         }
         float out[8];
@@ -259,7 +260,8 @@ __global__ __launch_bounds__(kWideThreads) void join_grad_wide_kernel(JoinGradJo
                     front[e] *= p.drop.scale;
                     whole_front[e] = front[e] * gate[e];
                 }
-                const GradOf8 o = grad_of_8(f, kept_8(p.drop, seed, row, col), t, d, r, x, gain, whole_front);
+                const Kept8 kept = kept_8(p.drop, seed, row, col);
+                const GradOf8 o = grad_of_8(f, kept, t, d, r, x, gain, whole_front);
                 if (pass == 0) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) dot_x += o.w[e] * x[e];
@@ -268,7 +270,7 @@ __global__ __launch_bounds__(kWideThreads) void join_grad_wide_kernel(JoinGradJo
                 float sum[kSums][8], v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    sum[kSumS][e] = o.kept_x[e] * (p.gate_ld ? gate[e] * f.qx : f.qx);
+                    sum[kSumS][e] = kept.on[e] ? o.dt[e] * x[e] * (p.gate_ld ? gate[e] * f.qx : f.qx) : 0.0f;
                     sum[kSumGain][e] = d[e] * t[e] * f.q;
                 }
 #pragma unroll
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(kWideThreads) void join_grad_wide_kernel(JoinGradJo
                 }
                 if (p.dgate && p.gate_ld) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = o.kept_x[e] * (f.qx * front[e]);
+                    for (int e = 0; e < 8; ++e) v[e] = kept.on[e] ? o.dt[e] * x[e] * (f.qx * front[e]) : 0.0f;
                     store_8_of<TYPE>(p.dgate, row * p.dgate_ld + col, valid, v);
                 }
                 if (p.dresidual) {
