@@ -95,40 +95,39 @@ __global__ __launch_bounds__(JoinShape<LANES>::kThreads) void join_kernel(JoinJo
     // gain_x times a gate of one row times the scale of what is kept; and gain
     constexpr int kKept = kKeep ? CHUNKS : 1;
     float front[kKept][8], gain[kKept][8];
-    // 0 times that gate, NaN where it is not finite: what becomes of a dropped element.  (Eight registers that cost no call time; a branch for such gates
-    // took the scalar unit's: 100 003 rows of 3 in single precision 22.7 us in place of 20.3.)
+    // 0 times that gate, NaN where it is not finite: what becomes of a dropped element.  (Eight registers; a branch for such gates took the scalar unit's:
+    // 100 003 rows of 3 in single precision 22.7 us in place of 20.3.)
     float nothing[kKept][8];
-    const auto load_front = [&](int c, int kept) {
-        float(&v)[8] = front[kept];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) nothing[kept][e] = 0;
-        Raw8<TYPE> raw;
+    const bool one_gate = p.gate && !gates;
+    // All three are on their way before the first is waited for: 20 000 rows of 1001 in half precision 43.4 us, 48.2 with each waited for in its turn.  (Not where no
+    // register is left: 2048 rows of 8200 in single precision 423 us, 320 in turn.)
+    Raw8<TYPE> gain_x_raw, gate_raw, gain_raw;
+    const auto make_front = [&](int c, int kept) {
         float f[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = p.drop.scale;
+        for (int e = 0; e < 8; ++e) front[kept][e] = p.drop.scale, nothing[kept][e] = 0;
         if (p.gain_x) {
-            load(raw, p.gain_x, 0, c);
-            widen(raw, c, f);
+            if (!kKeep) load(gain_x_raw, p.gain_x, 0, c);
+            widen(gain_x_raw, c, f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= f[e];
+            for (int e = 0; e < 8; ++e) front[kept][e] *= f[e];
         }
-        if (p.gate && !gates) {
-            load(raw, p.gate, 0, c);
-            widen(raw, c, f);
+        if (one_gate) {
+            if (!kKeep) load(gate_raw, p.gate, 0, c);
+            widen(gate_raw, c, f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                v[e] *= f[e];
+                front[kept][e] *= f[e];
                 nothing[kept][e] = 0.0f * f[e];
             }
         }
     };
-    const auto load_gain = [&](int c, float (&v)[8]) {
-        Raw8<TYPE> raw;
+    const auto make_gain = [&](int c, float (&v)[8]) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = 1;
         if (p.gain) {
-            load(raw, p.gain, 0, c);
-            widen(raw, c, v);
+            if (!kKeep) load(gain_raw, p.gain, 0, c);
+            widen(gain_raw, c, v);
         }
     };
     const int64_t last = count - 1;
@@ -137,8 +136,10 @@ __global__ __launch_bounds__(JoinShape<LANES>::kThreads) void join_kernel(JoinJo
     if (kKeep)
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            load_front(c, c % kKept);
-            load_gain(c, gain[c % kKept]);
+            if (p.gain_x) load(gain_x_raw, p.gain_x, 0, c);
+            if (one_gate) load(gate_raw, p.gate, 0, c);
+            if (p.gain) load(gain_raw, p.gain, 0, c);
+            make_front(c, c % kKept), make_gain(c, gain[c % kKept]);
         }
     for (; first < count; first += stride) {
         const bool there = first + sub < count;
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(JoinShape<LANES>::kThreads) void join_kernel(JoinJo
             const int col = (c * LANES + lane) * 8;
             const Kept8 kept = kept_8(p.drop, seed, row, col);
             if (!kKeep) {
-                load_front(c, 0);
+                make_front(c, 0);
                 if (p.residual) widen(r_raw[c], c, r[c]);
                 if (gates) widen(g_raw[c], c, g[c]);
             }
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(JoinShape<LANES>::kThreads) void join_kernel(JoinJo
             if (p.inv_rms && lane == 0 && there) p.inv_rms[row] = q;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
-                if (!kKeep) load_gain(c, gain[0]);
+                if (!kKeep) make_gain(c, gain[0]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) t[c][e] *= q * gain[c % kKept][e];
             }
