@@ -129,6 +129,10 @@ __global__ __launch_bounds__(JoinShape<LANES>::kThreads) void join_kernel(JoinJo
             if (!kKeep) load(gain_raw, p.gain, 0, c);
             widen(gain_raw, c, v);
         }
+        // (zeros behind the row, whatever was loaded there: they take part in the maximum of a row in 8 bits.  Short rows have them.)
+        const bool in = ROWS == kShortRows || (c * LANES + lane) * 8 < p.width;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = in ? v[e] : 0.0f;
     };
     const int64_t last = count - 1;
     int64_t first = static_cast<int64_t>(blockIdx.x) * kRows;

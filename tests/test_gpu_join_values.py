@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from test_gpu_join import _factor, _kept, _root
-from test_gpu_layer import BF16, EPS, F16, F32, U32, _close, _rand
+from test_gpu_layer import BF16, E4M3, EPS, F16, F32, U32, _close, _rand
 
 pytestmark = pytest.mark.gpu
 INF, NAN = float("inf"), float("nan")
@@ -121,3 +121,26 @@ def test_what_is_dropped_adds_nothing_to_gradients(h, d):
     assert bool((got[~kept] == 0).all()) and bool(torch.isfinite(got).all())
     got = dgate.cpu()
     assert bool((got[~kept] == 0).all()) and bool(torch.isfinite(got[[0, 2, 3]]).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=str)
+@pytest.mark.parametrize("d", WIDTHS + [16, 200, 264, 1024, 8192, 20_000])
+def test_8_bits_with_a_gain_that_is_not_finite(h, d, dtype):
+    """The scale of a row with an infinity is infinite, whatever lanes behind the row's end have loaded: what is finite becomes 0, and infinity over infinity
+    NaN, as in the norm.  A gain that is NaN makes the scale NaN."""
+    n = 3
+    x = (_rand(n, d, 1).abs() + 0.5).to(dtype).cuda()
+    for value, at in ((INF, d - 1), (-INF, max(0, d - 6)), (INF, 0), (NAN, d - 1)):
+        gain = torch.ones(d, dtype=dtype, device="cuda")
+        gain[at] = value
+        y, y2 = (torch.zeros((n, d), dtype=E4M3, device="cuda") for _ in range(2))
+        scale, scale2 = (torch.full((n,), -7.0, device="cuda") for _ in range(2))
+        h.join_norm(x, EPS, y=y, norm_x=False, gain=gain, y_scale=scale)
+        h.rms_norm(x, y2, EPS, gain=gain, y_scale=scale2)
+        h.sync()
+        for s, o in ((scale, y.float()), (scale2, y2.float())):
+            if value != value:
+                assert bool(torch.isnan(s).all()) and bool(torch.isnan(o).all()), (value, at)
+                continue
+            assert bool((s == INF).all()), (value, at)
+            assert bool(torch.isnan(o[:, at]).all()) and float(o.nan_to_num(0.0).abs().max()) == 0 and int(torch.isnan(o).sum()) == n, (value, at)
