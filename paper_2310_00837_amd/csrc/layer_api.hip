@@ -494,7 +494,8 @@ int helios_join_norm_grad(helios_ctx* c, const helios_join_norm_grad_args* a) {
                           a->gain_x, a->gate, gate_ld, a->gain, a->total, a->total_ld, a->dy, a->dy_ld, a->dtotal, a->dtotal_ld, a->inv_rms_x, a->inv_rms, a->dx,
                           a->dx_ld, a->dresidual, a->dresidual_ld, one_gate || gate_ld ? a->dgate : nullptr, a->dgate_ld, a->dgain_x, a->dgain};
     char* at = nullptr;
-    TRY(scratch(c, join_grad_scratch_bytes(job), &at));
+    const size_t bytes = join_grad_scratch_bytes(job);
+    if (bytes > 0) TRY(scratch(c, bytes, &at));
     HIP_TRY(c, launch_join_grad(c->stream, job, at));
     return HELIOS_OK;
 }
