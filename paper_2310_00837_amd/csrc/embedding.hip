@@ -9,7 +9,7 @@
 // last kernel adds these.  So a list of one ID costs what a list of distinct ones does, no sum is made by atomics, and the same list gives
 // the same bits.  What bounds it is the rows of dy, read once, and in front of that the chain of short launches that sorts the list, two for every
 // digit: 281 600 rows of 128 in single precision, IDs below two million, are 100 us, 50 for the rows, 5 for the parts, and 41 for the list.
-// Lists of up to 4096 are not sorted (few_kernel).
+// Lists of up to 4096 are not sorted (few_kernel) unless their rows are wide.
 #include "layer.hpp"
 #include "layer_dev.hpp"
 
@@ -74,12 +74,21 @@ typedef unsigned long long Entry;
 __device__ __forceinline__ uint32_t id_of(Entry e) { return static_cast<uint32_t>(e >> 32); }
 __device__ __forceinline__ uint32_t position_of(Entry e) { return static_cast<uint32_t>(e); }
 
-constexpr int kFew = 4096;                          // the longest list that is not sorted (few_kernel)
+// A list that is not sorted (few_kernel) has kFew entries at most, and its rows few columns: every workgroup of few_kernel goes through the whole list, so
+// that what it takes grows with (entries + 1000) for every 512 workgroups, where the sorted list is paid for once.  Distinct IDs, single
+// precision, us for both: 4096 of 256 (512 workgroups) 26 and 33, of 512 49 and 34, of 1024 96 and 36; 2048 of 1024 (1024 workgroups) 29 and 32, of 2048 60 and 33;
+// 1000 of 2048 (1000) 19 and 30, of 4096 38 and 32; 300 of 8192 (1216) 14 and 28.
+constexpr int kFew = 4096;
+constexpr int64_t kFewWork = 3'900'000;             // workgroups times (entries + 1000)
 constexpr int kSortBlock = 512, kSortItems = 4, kSortTile = kSortBlock * kSortItems, kSortWaves = kSortBlock / kWave;
 constexpr int kMostDigitBits = 9, kMostBins = 1 << kMostDigitBits, kLeastDigitBits = 4;
 constexpr int kMostGroups = 256;                    // of consecutive tiles, a workgroup each
 constexpr int kHeadGroups = 512;
 constexpr int kFillBlocks = 2048;
+// Workgroups that clear dtable times (entries + 1000) beside few_kernel's others, where they go through the list too, to see which rows are met; more are a launch
+// in front, for 2.5 us.  The larger the table, the more of this hides behind memory.  Of 256 columns in single precision, us beside and in front: 4096 entries
+// and 2000 rows 18.5 and 18.2, 16 000 rows 42 and 26, 200 000 rows 116 and 62; 1000 entries 7.5 and 9.9, 22 and 16, 53 and 45; 300 entries and 200 000 rows 39 and 43.
+constexpr int64_t kFillWork = 1 << 20, kFillHidden = 100;             // (and a workgroup times an entry for every 100 bytes of the table)
 constexpr int kMostChunks = 4096;                   // of a list
 
 struct GradArgs {
@@ -102,6 +111,7 @@ struct GradArgs {
     uint32_t head_span;                             // entries that a workgroup of heads_kernel counts
     uint32_t column_blocks;                         // of sum_kernel
     uint32_t fill_blocks;                           // workgroups of the first launch that clear dtable
+    bool fill_first;                                // ... which is a launch of its own, in front of few_kernel
     // scratch
     Entry* list[2];
     uint32_t* counts;                               // [n_groups][bins]
@@ -133,6 +143,9 @@ __device__ __forceinline__ void clear_table(const GradArgs& a, uint32_t block) {
         if (base + threadIdx.x < items) store_8_of<TYPE>(a.out, places.row(a.out_ld, down) + col, a.width - col, zeros);
     }
 }
+
+template <int TYPE>
+__global__ __launch_bounds__(kSortBlock) void clear_kernel(GradArgs a) { clear_table<TYPE>(a, blockIdx.x); }
 
 // A digit of the radix sort: `bits` bits of the ID from `shift` on.
 struct Digit {
@@ -436,7 +449,7 @@ __device__ __forceinline__ bool is_met(const FewLds& s, const Slots& slots, uint
 // A list of up to kFew IDs in one launch and without a sort: every workgroup finds the distinct IDs for itself; a wave has a position, and if
 // that is its ID's first one, looks through the whole list for the ID's other positions and for how many distinct IDs are less, which
 // is the row's number.  An ID with more than kLongRun positions is left to all waves of its workgroup.  Rows of dtable that are not met are cleared by
-// workgroups of their own.  What bounds it is the chain of steps in LDS: 777 rows of 200 take 7 us, 2600 of 128 17 (sorted: 38), 4000 28 (39); at 6000,
+// workgroups of their own, or by a launch in front (kFillWork).  What bounds it is the chain of steps in LDS: 777 rows of 200 take 7 us, 2600 of 128 17 (sorted: 38), 4000 28 (39); at 6000,
 // for which LDS has room for one workgroup on a CU, 87 and 40, so that kFew is 4096.
 constexpr int kLongRun = 64, kRowsAhead = 8;
 template <int TYPE, int Y, int V>
@@ -708,6 +721,7 @@ uint32_t ceil_div(int64_t a, int64_t b) { return static_cast<uint32_t>((a + b - 
 struct GradPlan {
     GradArgs a;
     uint32_t n_chunks, head_groups;
+    int64_t few_blocks;                             // workgroups of few_kernel that sum
     int per_lane;                                   // neighbouring columns of a row
     size_t bytes;
     GradPlan(const EmbeddingGradJob& job, char* scratch) {
@@ -717,7 +731,6 @@ struct GradPlan {
         a.width = job.width, a.scale = job.scale, a.n_table = static_cast<uint32_t>(job.n_table);
         a.ids = job.ids, a.dy = job.dy, a.dy_ld = job.dy_ld, a.out = job.out, a.out_ld = job.out_ld;
         a.row_id = job.row_id, a.n_distinct = job.n_distinct, a.err = job.err;
-        a.few = n <= kFew;
         per_lane = 1;
         while (per_lane * type_bytes(job.y_type) < 16 && per_lane * kWave < job.width) per_lane *= 2;
         const int64_t tiles = (n + kSortTile - 1) / kSortTile;
@@ -728,6 +741,9 @@ struct GradPlan {
         a.head_span = std::max<uint32_t>(1, ceil_div(n, int64_t{kHeadGroups} * kSortBlock * 8)) * kSortBlock * 8;
         a.column_blocks = ceil_div(job.width, per_lane * kWave);
         a.fill_blocks = job.n_distinct ? 0 : static_cast<uint32_t>(std::min<int64_t>(kFillBlocks, ceil_div(job.n_table * ((job.width + 7) / 8), kSortBlock)));
+        few_blocks = std::max<int64_t>(ceil_div(n, kSortWaves), a.n_distinct ? 1 : 0) * a.column_blocks;
+        a.few = n == 0 || (n <= kFew && few_blocks * (n + 1000) <= kFewWork);
+        a.fill_first = a.few && a.fill_blocks * (n + 1000) > kFillWork + job.n_table * a.width * type_bytes(job.table_type) / kFillHidden;
         n_chunks = ceil_div(n, a.chunk);
         head_groups = ceil_div(n, a.head_span);
         bytes = 0;
@@ -750,8 +766,10 @@ template <int TYPE, int Y, int V>
 void launch_sums(hipStream_t stream, const GradPlan& plan, const Entry* list) {
     const GradArgs& a = plan.a;
     if (a.few) {
-        const uint32_t sum_blocks = std::max<uint32_t>(ceil_div(a.rows.host, kSortWaves), a.n_distinct ? 1 : 0) * a.column_blocks;
-        hipLaunchKernelGGL((few_kernel<TYPE, Y, V>), dim3(sum_blocks + a.fill_blocks), dim3(kSortBlock), 0, stream, a, sum_blocks);
+        const uint32_t sum_blocks = static_cast<uint32_t>(plan.few_blocks);
+        if (a.fill_first) hipLaunchKernelGGL(clear_kernel<TYPE>, dim3(a.fill_blocks), dim3(kSortBlock), 0, stream, a);
+        const uint32_t blocks = sum_blocks + (a.fill_first ? 0 : a.fill_blocks);
+        if (blocks > 0) hipLaunchKernelGGL((few_kernel<TYPE, Y, V>), dim3(blocks), dim3(kSortBlock), 0, stream, a, sum_blocks);
         return;
     }
     const uint32_t tasks = plan.n_chunks * a.column_blocks;      // (fewer than 2^31: kMostChunks)
