@@ -732,10 +732,11 @@ int helios_embedding(helios_ctx *ctx, const helios_embedding_args *args);
  * helios_embedding).  Positions with -1 count for nothing, with any other ID
  * outside [0, n_table) neither, and are reported.  The order in which an ID's rows
  * are added depends on the list and the sizes only: the same call gives the same
- * bits.  add's gradient is dy itself.  Needs scratch for more than 4096 rows, and
- * for fewer wide ones (more than 3.9 million for n_rows / 8, rounded up, times the
- * blocks of 256 columns of dy, 512 of 16 bits, times n_rows + 1000): 16 bytes for
- * each, 8 (width + 1) for every 32 of them, at most 4096 times that, and 1 MB. */
+ * bits.  add's gradient is dy itself.  Needs scratch: 1 MB, whatever the list; for
+ * more than 4096 rows, and for fewer wide ones (more than 3.9 million for n_rows /
+ * 8, rounded up, times the blocks of 256 columns of dy, 512 of 16 bits, times
+ * n_rows + 1000), 16 bytes for each besides, and 8 (width + 1) for every 32 of
+ * them, at most 4096 times that. */
 typedef struct {
     int64_t n_rows;
     const int64_t *n_rows_dev;

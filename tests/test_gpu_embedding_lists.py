@@ -59,3 +59,34 @@ def test_gradient_of_rows_of_millions_of_columns(helios):
         assert bool((dtable[2] == 0).all()) and bool((drow[2] == -7.0).all())
     finally:
         h.close()
+
+
+def test_scratch_of_a_short_list_is_what_the_first_call_takes(helios):
+    """After a call with one row a capture takes lists of up to 4096, and refuses one whose sums need more than 1 MB."""
+    stream = torch.cuda.Stream()
+    h = helios.Helios(0, stream=stream)
+    try:
+        dy, ids = torch.ones((4096, 64), device="cuda"), torch.arange(4096, dtype=torch.int32, device="cuda") % 7
+        wide, dtable, wide_table = torch.ones((1, 4096), device="cuda").expand(4096, 4096), torch.zeros((9, 64), device="cuda"), torch.zeros((9, 4096), device="cuda")
+        torch.cuda.synchronize()
+        h.embedding_grad(ids[:1], dy[:1], 9, dtable=dtable)
+        h.sync()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            h.embedding_grad(ids, dy, 9, dtable=dtable)
+            with pytest.raises(helios.HeliosError) as e:
+                h.embedding_grad(ids, wide, 9, dtable=wide_table)
+        assert e.value.code == helios.ESTATE and "capture" in str(e.value)
+        want = torch.bincount(ids.long(), minlength=9)
+        for _ in range(3):
+            dtable.fill_(-7.0)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                graph.replay()
+            h.sync()
+            assert bool((dtable == want[:, None]).all())
+        h.embedding_grad(ids, wide, 9, dtable=wide_table)
+        h.sync()
+        assert bool((wide_table == want[:, None]).all())
+    finally:
+        h.close()
