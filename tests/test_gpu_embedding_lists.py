@@ -1,4 +1,5 @@
-"""The gradient of learnt rows: lists that are sorted though they are short, for their rows are wide; tables that are cleared by a launch of their own."""
+"""The gradient of learnt rows: lists that are sorted though they are short, for their rows are wide; tables that are cleared by a launch of their own; lists
+long enough that a workgroup sorts several tiles and counts several spans."""
 import pytest
 import torch
 
@@ -90,3 +91,11 @@ def test_scratch_of_a_short_list_is_what_the_first_call_takes(helios):
         assert bool((wide_table == want[:, None]).all())
     finally:
         h.close()
+
+
+@pytest.mark.parametrize("n,n_table,d,skew,count", [(600_000, 70_000, 3, 1, None), (600_000, 30, 8, 4, None), (600_000, 70_000, 5, 2, 550_001), (1_100_000, 1, 1, 1, None),
+                                                    (2_200_000, 70_000, 2, 1, None), (2_200_000, 600, 4, 3, None), (2_200_000, 600, 1, 3, 2_097_153)])
+def test_gradient_of_very_long_lists(h, n, n_table, d, skew, count):
+    """More than 524 288 entries, of which a workgroup sorts two tiles and more, and more than 2 097 152, of which it counts two spans."""
+    print("long lists", n, n_table, d, skew, count, flush=True)
+    _grad_case(h, n, n_table, d, (F32, F32), _ids(n, n_table, skew, 0.1, n), 0.5, n, count=count, runs=2)
