@@ -71,6 +71,10 @@ template <int TYPE, int LANES, int ROWS, int WITH>
 __global__ __launch_bounds__(GradShape<LANES>::kThreads) void join_grad_kernel(JoinGradJob p, SumPlaces places, float* part) {
     constexpr int kThreads = GradShape<LANES>::kThreads, kRows = GradShape<LANES>::kRows, kWidth = LANES * 8;
     constexpr bool kBoth = WITH != kWithAny;
+    // Where a row's columns are added up, which decides what 1024 threads have no registers for: both sums after everything else, 2048 rows of 8191 in bfloat16 77 us,
+    // that for dgain before the last sum over the row, 86; the other types and widths the other way about (8191 in single precision 125 and 116, 8192 in
+    // bfloat16 without dtotal 116 and 100).
+    constexpr bool kGainLast = TYPE == kBF16 && ROWS == kRowsWithRest;
     const bool gates = WITH == kWithGates || (WITH == kWithAny && p.gate_ld != 0);
     __shared__ float s3[2][3][RowSums<LANES, 3>::kWaves], s1[2][1][RowSums<LANES, 1>::kWaves];
     __shared__ float s_sum[kRows > 1 ? kRows : 1][kRows > 1 ? kWidth : 1];
@@ -115,7 +119,7 @@ __global__ __launch_bounds__(GradShape<LANES>::kThreads) void join_grad_kernel(J
     if (!gates) load_vector(p.gate, front);
     float sum_s[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum_gain[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < count; first += stride) {
-        const bool there = first + sub < count;
+        const bool there = kRows == 1 || first + sub < count;
         const int64_t row = there ? first + sub : count - 1;
         load_row(row);
         float t[8], d[8], r[8], x[8], g[8], whole_front[8];
@@ -148,12 +152,10 @@ __global__ __launch_bounds__(GradShape<LANES>::kThreads) void join_grad_kernel(J
         float v1[1] = {0};
 #pragma unroll
         for (int e = 0; e < 8; ++e) v1[0] += o.w[e] * x[e];
-        if (there)
+        const auto add_gain = [&] {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                sum_gain[e] += d[e] * t[e] * f.q;
-                sum_s[e] += kept.on[e] ? o.dt[e] * x[e] * (gates ? g[e] * f.qx : f.qx) : 0.0f;
-            }
+            for (int e = 0; e < 8; ++e) sum_gain[e] += d[e] * t[e] * f.q;
+        };
         if (p.dresidual && there) {
             float v[8];
 #pragma unroll
@@ -166,6 +168,7 @@ __global__ __launch_bounds__(GradShape<LANES>::kThreads) void join_grad_kernel(J
             for (int e = 0; e < 8; ++e) v[e] = kept.on[e] ? o.dt[e] * x[e] * (f.qx * front[e]) : 0.0f;
             store_row_8<TYPE, ROWS>(p.dgate, row * p.dgate_ld, col, p.width, v);
         }
+        if (!kGainLast && there) add_gain();
         float out[8];
         if (p.norm_x) {
             v1[0] = in ? v1[0] : 0.0f;
@@ -177,6 +180,10 @@ __global__ __launch_bounds__(GradShape<LANES>::kThreads) void join_grad_kernel(J
 #pragma unroll
             for (int e = 0; e < 8; ++e) out[e] = o.w[e];
         }
+        if (kGainLast && there) add_gain();
+        if (there)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum_s[e] += kept.on[e] ? o.dt[e] * x[e] * (gates ? g[e] * f.qx : f.qx) : 0.0f;
         if (there) store_row_8<TYPE, ROWS>(p.dx, row * p.dx_ld, col, p.width, out);
     }
 #pragma unroll
