@@ -6,8 +6,9 @@
 // the 8-bit output are one pass over what has to be read and written, with two sums over the row, the second of which needs the first.
 // Lanes go through rows and ask for the next one while they work on this one; what is the same for all rows stays in registers.
 // What bounds it is memory, and the vector unit close behind: 100 003 rows of 1024 in half precision with both norms, a gate, dropout and both outputs
-// are 145 us, 5.6 TB/s, for which a wave issues 484 vector instructions a row, of which the generator is a third.  (604 of them took 163 us:
-// products with the gains made again for every row, a division for the root, sums over lanes by moves of their own.)
+// are 144 us, 5.7 TB/s, for which each of a row's two waves issues 282 vector instructions, of which the generator is a third.
+// Rows of more than 8192 columns are more than the registers hold: 50 to 182 of them go to memory and back, and 2046 rows of 8200, which pay for the lanes of 32 768,
+// take 323 us in single precision and 196 in bfloat16, where 2048 of 8192 take 82 and 40.
 #include "drop_dev.hpp"
 
 #include <algorithm>
@@ -223,8 +224,9 @@ auto by_width(int32_t width, RUN run) {
     return run.template go<TYPE, 1024, 4, ROWS, GATES>();
 }
 // Threads of a launch, about: rows in turn after that, so that a row is asked for while another is worked on, but not so many that the last ones
-// keep few CUs busy (100 003 x 1024 in half precision: 166 us for half a million, 160, 152 for two, 165 with a row each; x 100 in
-// single precision, where four rows share a wave, 42, 40.6 for one million, 43.4 for two).
+// keep few CUs busy.  100 003 x 1024 in half precision: 153 us for one million, 144 for two, 139 for four, 156 with a row each; 20 000 x 2000 in single precision
+// 140, 140, 150, 162; 60 000 x 1000 in bfloat16 to 8 bits 91, 91, 97, 111.  Where four rows share a wave, for half a million, one and two: 100 003 x 100 in single
+// precision 36.4, 35.0, 34.8, x 64 in bfloat16 16.0, 16.1, 17.4.
 template <int LANES>
 constexpr int kJoinThreads = LANES < kWave ? 256 * 4096 : 256 * 8192;
 struct RunJoin {

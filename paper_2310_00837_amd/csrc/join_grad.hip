@@ -7,10 +7,12 @@
 // (k = 0 selects: an element that is dropped adds 0 to these whatever is multiplied there.)
 // With a gate of one row, dgate and dgain_x are one sum, S = sum over rows of k dt x qx: dgate = s gain_x S, dgain_x = s gate S.
 // A row is held in registers in 32 bits and read once; lanes go through rows and keep their sums of columns until the end; a second launch adds the
-// workgroups' sums.  What bounds it is the vector unit as much as memory: some 390 instructions for eight elements of a wave, of which the generator
-// is a quarter, so registers are kept for a second workgroup on a CU and not for the next row (asked for ahead it took 24.7 us in place of 23.4
-// for 11 264 x 256 in single precision, 73.6 in place of 70 for 6000 x 4096 in bfloat16).  26 624 rows of 512 in bfloat16 with a gate for all: 35 us,
-// 31 and 4 for the second launch, 4.7 TB/s; 11 264 of 256 in single precision with a gate each: 24, of which 18 and 4.
+// workgroups' sums.  26 624 rows of 512 in bfloat16 with a gate for all: 35 us, 31 and 4 for the second launch; 11 264 of 256 in single precision with
+// a gate each: 24, of which 18 and 4.  In the first of these the main launch moves 5.3 TB/s, 0.83 of a copy's rate, and its vector instructions (376 for eight elements of a
+// wave, of which the generator is a quarter) fill about half of its time: what is left is that a row's loads, two sums and stores follow one another.
+// Registers are kept for a second workgroup on a CU and not for the next row (asked for ahead it took 24.7 us in place of 23.4 for
+// 11 264 x 256 in single precision, 73.6 in place of 70 for 6000 x 4096 in bfloat16).  1024 threads, for 4097 to 8192 columns, have too few: 4 to 69 of
+// them go to memory and back, and 2048 x 8192 takes 112 us in single precision, 62 in bfloat16, for 63 and 32 us of bytes.
 #include "drop_dev.hpp"
 
 #include <algorithm>
